@@ -294,6 +294,73 @@ int psgd_profile_enable(psgd_ctx *ctx, int max_records);
 int psgd_profile_select(psgd_ctx *ctx, int tag_mask);
 int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
 
+/* ---- the training step around the compressor: the output head's loss, 8-bit activations, weight gradients -------------
+ *
+ * The calls below have no context.  Matrices are row-major device memory with a leading dimension in elements, a multiple of 8 (codes:
+ * of 16) that is at least the columns and at most 2^22; bases are 16-byte aligned.  Elements beyond the columns are never taken as data nor written,
+ * up to the next multiple of 8 they may be read, so the last row's are part of the buffer as well.  Work is enqueued on `stream`, nothing is kept from one call to the next, and a
+ * workspace (256-byte aligned, of the bytes that the call's _workspace_bytes function gives; 0 = the arguments are refused) holds nothing between calls.  The calls launch kernels only and
+ * may be recorded by a capturing stream at any time.  Where there are no rows (tokens) the matrices that have them may be NULL.  Results do not depend on the order in which the GPU runs their parts.  */
+
+/* The output head: logits l = X W^T of tokens x vocab, softmax cross entropy against labels, without logits in memory.
+ *   lse_t = log sum_v exp(l_tv);  loss_t = lse_t - l_t,label(t);
+ *   D_tv = c_t (exp(l_tv - lse_t) - [v = label(t)]);  dX = D W;  dW = D^T X.
+ * A token whose label lies outside [0, vocab) does not count: its loss and its row of dX are 0 and its row of X is not
+ * looked at.  Exponentials and D exist for one piece of the tokens at a time, in the workspace.
+ * Arithmetic: bf16 X and W are multiplied on the matrix cores as they are, fp32 ones as three bf16 planes (24 bits); sums, statistics and losses are fp32.  D is
+ * rounded once to bf16 for results in bf16; for dW in fp32 it has two bf16 planes (16 bits), with fp32 X and W three. */
+typedef struct {
+    int64_t tokens, d, vocab;   /* X: tokens x d, W: vocab x d; tokens may be 0                      */
+    int64_t ldx, ldw;           /* leading dimensions; 0 = d, which is then a multiple of 8          */
+    int64_t lddx, lddw;         /* of dX and dW; likewise                                            */
+    int32_t dtype;              /* PSGD_F32 or PSGD_BF16: X, W and dX                                */
+    int32_t grad_dtype;         /* PSGD_F32 or PSGD_BF16: dW                                         */
+    int64_t piece_tokens;       /* tokens per piece; 0 = as many as have their exponentials and D in 1 GiB, at least 256 */
+} psgd_head_desc;
+
+size_t psgd_head_workspace_bytes(const psgd_head_desc *desc, int gradients);
+
+/* loss: tokens fp32, out.  labels: tokens int64.  Errors: INVALID_ARG (null pointer, bad enum, negative piece), SHAPE
+ * (d or vocab < 1, tokens < 0, one of them or a leading dimension too large), ALIGN, HIP. */
+int psgd_head_loss(const psgd_head_desc *desc, void *workspace, void *stream, const void *x, const void *w,
+                   const int64_t *labels, float *loss);
+
+/* The same with gradients of sum_t c_t loss_t: c_t = weight[t] (fp32, tokens), or with weight = NULL one over the number of tokens that count (the mean).
+ * dX is written, dW written or, with accumulate != 0, added to. */
+int psgd_head_loss_grad(const psgd_head_desc *desc, void *workspace, void *stream, const void *x, const void *w,
+                        const int64_t *labels, const float *weight /* nullable */, float *loss, void *dx, void *dw,
+                        int accumulate);
+
+/* 8-bit checkpoints of an activation (rows x cols).  A row is cut into groups of 32 columns; a group's scale is the smallest power of two
+ * 2^e with max|x| <= 127 * 2^e (-126 <= e <= 121; kept as the byte e + 127, 0 for a group of zeros), an element's code is x / 2^e rounded to the nearest whole number, ties to even.  What is not
+ * finite has code -128, does not enter the maximum and comes back as NaN.  Values that come back are exact in bf16.
+ * codes: rows x ldc bytes (columns up to the next multiple of 16 are written, as zeros); scales: rows x ceil(cols / 32) bytes, contiguous.
+ * rows may be 0.  Errors: INVALID_ARG (null pointer, bad enum, one of a pair of pointers missing), SHAPE, ALIGN, HIP. */
+int psgd_act_store(void *stream, int64_t rows, int64_t cols, const void *x, int dtype, int64_t ld, int8_t *codes,
+                   int64_t ldc, uint8_t *scales);
+int psgd_act_restore(void *stream, int64_t rows, int64_t cols, const int8_t *codes, int64_t ldc, const uint8_t *scales,
+                     void *x, int dtype, int64_t ld);
+
+/* h = act(gate) * up, or with up = NULL h = act(gate), and in the same pass the checkpoints of gate and up that the backward pass needs (up_codes, up_scales: both NULL without up).
+ * SiLU: x / (1 + e^-x); GELU: x F(x) with the normal distribution function F.  gate, up: ld_in. */
+enum { PSGD_SILU = 0, PSGD_GELU = 1 };
+int psgd_act_glu(void *stream, int64_t rows, int64_t cols, int act, int dtype, const void *gate,
+                 const void *up /* nullable */, int64_t ld_in, void *h, int64_t ld_h, int8_t *gate_codes,
+                 uint8_t *gate_scales, int8_t *up_codes, uint8_t *up_scales, int64_t ldc);
+/* dgate = dh * up * act'(gate), dup = dh * act(gate) from the checkpoints; without up (up_codes, up_scales, dup all NULL)
+ * dgate = dh * act'(gate). */
+int psgd_act_glu_backward(void *stream, int64_t rows, int64_t cols, int act, int dtype, const int8_t *gate_codes,
+                          const uint8_t *gate_scales, const int8_t *up_codes, const uint8_t *up_scales, int64_t ldc,
+                          const void *dh, int64_t ld_h, void *dgate, void *dup, int64_t ld_out);
+
+/* The weight gradient of Y = X W^T from dY and the checkpoint of X:  G = dY^T X, or with accumulate != 0 G += dY^T X.
+ * dY: tokens x out_features (dtype, ldy); checkpoint: tokens x in_features; G: out_features x in_features (g_dtype, ldg), as psgd_compress takes it.
+ * tokens may be 0.  bf16 dY is multiplied as it is, fp32 as three bf16 planes; sums are fp32. */
+size_t psgd_act_wgrad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features, int dtype);
+int psgd_act_wgrad(void *workspace, void *stream, int64_t tokens, int64_t out_features, int64_t in_features,
+                   const void *dy, int dtype, int64_t ldy, const int8_t *codes, int64_t ldc, const uint8_t *scales,
+                   void *g, int g_dtype, int64_t ldg, int accumulate);
+
 int psgd_last_hip_error(const psgd_ctx *ctx);
 const char *psgd_strerror(int code);
 void psgd_destroy(psgd_ctx *ctx);

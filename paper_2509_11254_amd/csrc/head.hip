@@ -1,0 +1,501 @@
+// Softmax cross entropy at the output head, without logits in memory, and its gradients.
+//
+//   l_tv = x_t . w_v,  lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,y(t)
+//   D_tv = c_t (exp(l_tv - lse_t) - [v = y(t)]),  dX = D W,  dW = D^T X,   c_t: the token's weight, or 1 / (tokens that count)
+//
+// Tokens whose label lies outside [0, V) do not count: their rows are left out from the start (the others are copied together,
+// in order), so that what they hold, NaN or not, reaches neither sum nor product.
+//
+// The vocabulary is walked in tiles of 256.  A workgroup has the logits of 256 tokens and one tile in its accumulators, takes the
+// tile's maximum and its sum of exponentials (the label's left out) per token, and writes these two numbers; for the gradients it writes the exponentials
+// relative to the tile's maximum as well, for one piece of the tokens at a time.  One more pass over a piece joins the tiles'
+// numbers to lse_t and turns the exponentials into D in place, and the two products with D follow.
+#include "tile_dev.h"
+
+namespace psgd {
+
+typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+
+// what is kept of exp(l - tile's maximum): nothing, fp16 of 2^15 times it (the range of fp16 starts 2^29 below the maximum;
+// 11 bits, so that D is rounded once, to bf16), or fp32 (results in fp32)
+enum HeadKeep { KEEP_NONE = 0, KEEP_F16 = 1, KEEP_F32 = 2 };
+constexpr float kHalfScale = 32768.f;
+
+struct HeadDev {
+    const int64_t* labels;
+    const float* weight;
+    float* loss;
+    int tokens, d, vocab;
+    // in the workspace
+    int* count;          // tokens that count
+    int* rows;           // which they are
+    int* label;          // and their labels
+    float2* stats;       // [token of the piece][tile]: maximum, sum of exponentials without the label's
+    float* at_label;     // logit of the label, by token of the piece
+    void* e;             // exponentials, [token of the piece][ldv]
+    bf16_t* D;           // planes of D, [token of the piece][ldv]; in place of e where that is fp16
+    int64_t ldv, d_plane;
+    int tiles, n_planes, keep;
+};
+
+// ---- tokens that count ----------------------------------------------------------------------------------------------
+
+constexpr int kGatherThreads = 256;
+
+__device__ inline bool counts(int64_t label, int vocab) { return label >= 0 && label < vocab; }
+
+// Block b has tokens [b * per, ...): where its first token goes is the number of counted ones before it, which every block finds for
+// itself (8 bytes per label, from L2).  x to its planes in `xc` (row length ldc, zeros beyond d); a token that does not count gets loss 0
+// and a zero row of dX.
+template <class T>
+__global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, int per, const T* x, int64_t ldx, bf16_t* xc, int64_t ldc, int planes,
+                                                                     T* dx, int64_t lddx) {
+    __shared__ int sum[kGatherThreads / 64];
+    __shared__ int place[kGatherThreads];
+    const int first = blockIdx.x * per, last = min(h.tokens, first + per);
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int mine = 0;
+    for (int i = threadIdx.x; i < first; i += kGatherThreads) mine += counts(h.labels[i], h.vocab) ? 1 : 0;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) mine += __shfl_xor(mine, s);
+    if (lane == 0) sum[wv] = mine;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < kGatherThreads / 64; ++w) before += sum[w];
+    for (int t0 = first; t0 < last; t0 += kGatherThreads) {
+        const int t = t0 + threadIdx.x;
+        const int64_t y = t < last ? h.labels[t] : -1;
+        const bool in = counts(y, h.vocab);
+        const unsigned long long mask = __ballot(in);
+        __syncthreads();
+        if (lane == 0) sum[wv] = __popcll(mask);
+        __syncthreads();
+        int at = before + __popcll(mask & ((1ull << lane) - 1));
+        for (int w = 0; w < wv; ++w) at += sum[w];
+        place[threadIdx.x] = in ? at : -1;
+        if (in) { h.rows[at] = t; h.label[at] = (int)y; }
+        else if (t < last) h.loss[t] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kGatherThreads / 64; ++w) before += sum[w];
+        __syncthreads();
+        // a wave per row
+        const int pieces = (h.d + 7) / 8;
+        for (int r = wv; r < kGatherThreads && t0 + r < last; r += kGatherThreads / 64) {
+            const int to = place[r];
+            const PSGD_GLOBAL T* src = as_global(x) + (int64_t)(t0 + r) * ldx;
+            if (to < 0) {
+                if (dx)
+                    for (int c = lane; c < h.d; c += 64) as_global(dx)[(int64_t)(t0 + r) * lddx + c] = (T)0.f;
+                continue;
+            }
+            for (int p = lane; p < pieces; p += 64) {
+                bf16x8 out[kMaxPlanes];
+                float v[8];
+                if constexpr (sizeof(T) == 2) {
+                    const bf16x8 b = *reinterpret_cast<const PSGD_GLOBAL bf16x8*>(src + 8 * p);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) out[0][u] = 8 * p + u < h.d ? b[u] : (bf16_t)0.f;
+                } else {
+                    const floatx4 a = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(src + 8 * p), b = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(src + 8 * p + 4);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) { v[u] = a[u]; v[u + 4] = b[u]; }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        bf16_t q[kMaxPlanes];
+                        split_planes<kMaxPlanes>(8 * p + u < h.d ? v[u] : 0.f, q);
+#pragma unroll
+                        for (int k = 0; k < kMaxPlanes; ++k) out[k][u] = q[k];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < (sizeof(T) == 2 ? 1 : kMaxPlanes); ++k)
+                    *reinterpret_cast<PSGD_GLOBAL bf16x8*>(as_global(xc) + ((int64_t)k * h.tokens + to) * ldc + 8 * p) = out[k];
+            }
+        }
+    }
+    if (last == h.tokens && threadIdx.x == 0) *h.count = before;
+}
+
+// ---- logits of a piece: statistics per tile, exponentials --------------------------------------------------------------
+
+template <int BL, int KEEP>
+__global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t, HeadDev h, int n_p, int n_l) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    using T = Tile<true, true, BL>;
+    const TilePlace at = tile_place(blockIdx.x, n_p, n_l, 1);
+    const int p0 = at.p * kTileP, l0 = at.l * BL;
+    const int nl = counted(t, t.L.extent);
+    if (l0 >= nl) return;
+    T tile;
+    tile.run(t, p0, l0, nl, t.K, 0, (PSGD_TLDS unsigned char*)smem);
+    const int valid = h.vocab - p0;         // columns of this tile
+    constexpr float kLog2e = 1.4426950408889634f;
+    // the wave's maximum per row, over its columns; a tile has at least one column
+    float* red = reinterpret_cast<float*>(smem);        // [WP][BL]
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j) {
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int c = tile.col(i, v >> 2) + (v & 3);
+                if (c >= valid) tile.acc[i][j][v] = -__builtin_inff();
+                m = fmaxf(m, tile.acc[i][j][v]);
+            }
+        m = fmaxf(m, __shfl_xor(m, 32));
+        if ((threadIdx.x & 63) < 32) red[tile.wp * BL + tile.row(j)] = m;
+    }
+    __syncthreads();
+    float most[T::FL], sum[T::FL];
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j) {
+        const int row = tile.row(j), l = l0 + row;
+        float m = red[row];
+#pragma unroll
+        for (int w = 1; w < T::WP; ++w) m = fmaxf(m, red[w * BL + row]);
+        most[j] = m;
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        const int y = l < nl ? h.label[t.first + l] - p0 : -1;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = tile.col(i, q);
+                float e[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float x = tile.acc[i][j][4 * q + u];
+                    e[u] = __builtin_amdgcn_exp2f((x - base) * kLog2e);
+                    if (c + u == y) h.at_label[l] = x;
+                    else s += e[u];
+                }
+                if (KEEP != KEEP_NONE && l < nl && p0 + c < h.ldv) {
+                    if constexpr (KEEP == KEEP_F16) {
+                        halfx4 o;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) o[u] = (_Float16)(e[u] * kHalfScale);
+                        *reinterpret_cast<PSGD_GLOBAL halfx4*>(as_global((_Float16*)h.e) + l * h.ldv + p0 + c) = o;
+                    } else {
+                        const floatx4 o = {e[0], e[1], e[2], e[3]};
+                        *reinterpret_cast<PSGD_GLOBAL floatx4*>(as_global((float*)h.e) + l * h.ldv + p0 + c) = o;
+                    }
+                }
+            }
+        sum[j] = s + __shfl_xor(s, 32);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j)
+        if ((threadIdx.x & 63) < 32) red[tile.wp * BL + tile.row(j)] = sum[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j) {
+        const int row = tile.row(j), l = l0 + row;
+        if (tile.wp == 0 && (threadIdx.x & 63) < 32 && l < nl) {
+            float s = red[row];
+#pragma unroll
+            for (int w = 1; w < T::WP; ++w) s += red[w * BL + row];
+            h.stats[(int64_t)l * h.tiles + at.p] = make_float2(most[j], s);
+        }
+    }
+}
+
+// ---- the row's sum, the loss, and D ------------------------------------------------------------------------------------
+
+// Largest logit of row l and the sum of exp(logit - it) over all columns but the label's, by all threads of the block
+struct RowSum { float most, others; };
+__device__ __forceinline__ RowSum row_sum(const HeadDev& h, int l, float* shared) {
+    const float2* st = h.stats + (int64_t)l * h.tiles;
+    float m = -__builtin_inff(), s = 0.f;
+    auto join = [&](float mo, float so) {
+        const float n = fmaxf(m, mo);
+        if (n != -__builtin_inff()) s = s * expf(m - n) + so * expf(mo - n);
+        else s += so;
+        m = n;
+    };
+    for (int i = threadIdx.x; i < h.tiles; i += kThreads) join(st[i].x, st[i].y);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const float mo = __shfl_xor(m, d), so = __shfl_xor(s, d);
+        join(mo, so);
+    }
+    if ((threadIdx.x & 63) == 0) { shared[threadIdx.x >> 6] = m; shared[4 + (threadIdx.x >> 6)] = s; }
+    __syncthreads();
+    m = shared[0], s = shared[4];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) join(shared[w], shared[4 + w]);
+    return {m, s};
+}
+
+// block: one token's row, blockIdx.y its part of the vocabulary; without gradients one part and no D
+template <int KEEP, int PL>
+__global__ __launch_bounds__(kThreads) void head_rows_kernel(HeadDev h, int first, int most_rows, int span) {
+    __shared__ float shared[8];
+    const int l = blockIdx.x;
+    if (l >= min(most_rows, *h.count - first)) return;
+    const int token = h.rows[first + l];
+    const RowSum r = row_sum(h, l, shared);
+    const float at_label = h.at_label[l], e_label = expf(at_label - r.most), total = r.others + e_label;
+    // log(1 + others / label's) keeps the loss of a token that is all but certain, which the difference of two logits does not
+    if (blockIdx.y == 0 && threadIdx.x == 0)
+        h.loss[token] = r.others < e_label ? log1pf(r.others / e_label) : r.most - at_label + logf(total);
+    if constexpr (KEEP == KEEP_NONE) return;
+    const float c = (h.weight ? h.weight[token] : 1.f / (float)*h.count) / total;
+    const int y = h.label[first + l];
+    const float d_label = -r.others * c;        // (p - 1 as the sum of the other probabilities)
+    const int end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
+    for (int v = blockIdx.y * span + 8 * threadIdx.x; v < end; v += 8 * kThreads) {
+        const float most = h.stats[(int64_t)l * h.tiles + v / kTileP].x;
+        const float f = expf(most - r.most) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
+        float x[8];
+        if constexpr (KEEP == KEEP_F16) {
+            const halfx8 e = *reinterpret_cast<const PSGD_GLOBAL halfx8*>(as_global((_Float16*)h.e) + l * h.ldv + v);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = (float)e[u] * f;
+        } else {
+            const PSGD_GLOBAL floatx4* e = reinterpret_cast<const PSGD_GLOBAL floatx4*>(as_global((float*)h.e) + l * h.ldv + v);
+            const floatx4 a = e[0], b = e[1];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { x[u] = a[u] * f; x[u + 4] = b[u] * f; }
+        }
+        bf16x8 out[PL];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            bf16_t q[PL];
+            split_planes<PL>(v + u == y ? d_label : x[u], q);
+#pragma unroll
+            for (int k = 0; k < PL; ++k) out[k][u] = q[k];
+        }
+#pragma unroll
+        for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL bf16x8*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = out[k];
+    }
+}
+
+// fp32 sums of all pieces to bf16
+__global__ __launch_bounds__(kThreads) void head_round_kernel(const float* sum, int64_t rows, int cols, int64_t lds, bf16_t* out, int64_t ld, int accumulate) {
+    const int quads = (cols + 3) / 4;
+    const int64_t all = rows * quads;
+    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < all; e += (int64_t)gridDim.x * kThreads) {
+        const int64_t r = e / quads;
+        const int c = 4 * (int)(e - r * quads);
+        const floatx4 s = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(as_global(sum) + r * lds + c);
+        PSGD_GLOBAL bf16_t* p = as_global(out) + r * ld + c;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (c + u < cols) p[u] = (bf16_t)(accumulate ? s[u] + (float)p[u] : s[u]);
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+
+constexpr size_t kPieceBytes = (size_t)1 << 30;     // what is kept of one piece of the tokens: exponentials and D, or statistics alone
+
+struct HeadPlan {
+    size_t bytes = 0;
+    size_t count, rows, label, xc, wc, stats, at_label, e, D, part, sum;
+    int64_t ldc, ldv;
+    int piece, pieces, tiles, x_planes, w_planes, d_planes, keep, bl, dx_split, dw_split;
+    unsigned pairs, dx_pairs, dw_pairs;
+    int n_pairs, n_dx_pairs, n_dw_pairs;
+    bool copy_w;
+};
+
+static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
+    HeadPlan p = {};
+    const bool f32 = s.dtype == PSGD_F32;
+    p.ldc = up8(s.d);
+    p.ldv = up8(s.vocab);
+    p.tiles = (int)((s.vocab + kTileP - 1) / kTileP);
+    p.x_planes = p.w_planes = f32 ? 3 : 1;
+    p.copy_w = f32 || s.d % 8 != 0;
+    p.pairs = f32 ? kPairs33 : kPairs1;
+    p.n_pairs = f32 ? 6 : 1;
+    p.keep = !gradients ? KEEP_NONE : f32 || s.grad_dtype == PSGD_F32 ? KEEP_F32 : KEEP_F16;
+    p.d_planes = f32 ? 3 : s.grad_dtype == PSGD_F32 ? 2 : 1;
+    p.dx_pairs = p.pairs, p.n_dx_pairs = p.n_pairs;
+    if (f32) { p.dw_pairs = s.grad_dtype == PSGD_F32 ? kPairs33 : kPairs22; p.n_dw_pairs = s.grad_dtype == PSGD_F32 ? 6 : 3; }
+    else { p.dw_pairs = s.grad_dtype == PSGD_F32 ? kPairsL2 : kPairs1; p.n_dw_pairs = s.grad_dtype == PSGD_F32 ? 2 : 1; }
+    // tokens per piece
+    const int64_t tokens = std::max<int64_t>(1, s.tokens);
+    const size_t row = !gradients ? p.tiles * sizeof(float2) : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
+    const int64_t most = s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256);
+    p.pieces = (int)((tokens + most - 1) / most);
+    p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
+    if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
+    p.pieces = (int)((tokens + p.piece - 1) / p.piece);
+    p.bl = tile_rows(p.piece);
+    auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
+    p.count = take(4);
+    p.rows = take((size_t)tokens * 4);
+    p.label = take((size_t)tokens * 4);
+    p.xc = take((size_t)tokens * p.ldc * 2 * p.x_planes);
+    p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2 * p.w_planes) : 0;
+    p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
+    p.at_label = take((size_t)p.piece * 4);
+    if (gradients) {
+        const size_t elems = (size_t)p.piece * p.ldv;
+        p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
+        p.D = p.keep == KEEP_F16 ? p.e : take(elems * 2 * p.d_planes);
+        const int64_t n_d = (s.d + kTileP - 1) / kTileP;
+        p.dx_split = tile_splits(n_d, (p.piece + p.bl - 1) / p.bl, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, p.piece * s.d);
+        p.dw_split = tile_splits(n_d, p.tiles, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, s.vocab * s.d);
+        p.part = take(std::max(tile_part_bytes((int)s.d, p.piece, p.dx_split), tile_part_bytes((int)s.d, (int)s.vocab, p.dw_split)));
+        p.sum = p.pieces > 1 && s.grad_dtype == PSGD_BF16 ? take((size_t)s.vocab * p.ldc * 4) : 0;
+    }
+    return p;
+}
+
+static int head_shape(const psgd_head_desc* s) {
+    if (!s || bad_dtype(s->dtype) || bad_dtype(s->grad_dtype) || s->piece_tokens < 0) return PSGD_E_INVALID_ARG;
+    if (s->tokens < 0 || s->d < 1 || s->vocab < 1 || s->tokens > kMaxExtent || s->vocab > kMaxExtent || up8(s->d) > kMaxLd || up8(s->vocab) > kMaxLd) return PSGD_E_SHAPE;
+    return PSGD_OK;
+}
+
+static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, int bl, hipStream_t st) {
+    const int n_p = h.tiles, n_l = (t.L.extent + bl - 1) / bl;
+    hipError_t e = hipErrorInvalidValue;
+#define PSGD_LOGITS(BL, KEEP)                                                                                             \
+    do {                                                                                                                  \
+        auto kfn = head_logits_kernel<BL, KEEP>;                                                                          \
+        constexpr int lds = Tile<true, true, BL>::LDS_BYTES;                                                              \
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);     \
+        if (e != hipSuccess) return e;                                                                                    \
+        hipLaunchKernelGGL(kfn, dim3(n_p * n_l), dim3(kTileThreads), lds, st, t, h, n_p, n_l);                            \
+        e = hipGetLastError();                                                                                            \
+    } while (0)
+#define PSGD_LOGITS_KEEP(BL)                                       \
+    do {                                                           \
+        if (h.keep == KEEP_NONE) PSGD_LOGITS(BL, KEEP_NONE);       \
+        else if (h.keep == KEEP_F16) PSGD_LOGITS(BL, KEEP_F16);    \
+        else PSGD_LOGITS(BL, KEEP_F32);                            \
+    } while (0)
+    if (bl == 256) PSGD_LOGITS_KEEP(256);
+    else if (bl == 128) PSGD_LOGITS_KEEP(128);
+    else if (bl == 64) PSGD_LOGITS_KEEP(64);
+#undef PSGD_LOGITS
+#undef PSGD_LOGITS_KEEP
+    return e;
+}
+
+static hipError_t launch_rows(const HeadDev& h, int first, int rows, hipStream_t st) {
+    if (h.keep == KEEP_NONE) {
+        hipLaunchKernelGGL((head_rows_kernel<KEEP_NONE, 1>), dim3(rows), dim3(kThreads), 0, st, h, first, rows, 0);
+        return hipGetLastError();
+    }
+    // parts of the vocabulary, so that a few rows fill the card as well
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>((h.ldv + 8 * kThreads - 1) / (8 * kThreads), 2048 / std::max(1, rows)));
+    const int span = (int)(((h.ldv + parts - 1) / parts + 7) / 8 * 8);
+    parts = (h.ldv + span - 1) / span;
+    const dim3 grid(rows, (unsigned)parts);
+    if (h.keep == KEEP_F16) hipLaunchKernelGGL((head_rows_kernel<KEEP_F16, 1>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    else if (h.n_planes == 2) hipLaunchKernelGGL((head_rows_kernel<KEEP_F32, 2>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    else hipLaunchKernelGGL((head_rows_kernel<KEEP_F32, 3>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    return hipGetLastError();
+}
+
+static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
+                    const float* weight, float* loss, void* dx, void* dw, int accumulate) {
+    if (int rc = head_shape(s)) return rc;
+    if (!workspace || !w || (gradients && !dw) || (s->tokens != 0 && (!x || !labels || !loss || (gradients && !dx)))) return PSGD_E_INVALID_ARG;
+    const int64_t ldx = s->ldx ? s->ldx : s->d, ldw = s->ldw ? s->ldw : s->d, lddx = s->lddx ? s->lddx : s->d, lddw = s->lddw ? s->lddw : s->d;
+    if (ldx > kMaxLd || ldw > kMaxLd || lddx > kMaxLd || lddw > kMaxLd) return PSGD_E_SHAPE;
+    if (bad_ld(ldx, s->d) || bad_ld(ldw, s->d) || misaligned(x) || misaligned(w) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
+    if (gradients && (bad_ld(lddx, s->d) || bad_ld(lddw, s->d) || misaligned(dx) || misaligned(dw))) return PSGD_E_ALIGN;
+    const HeadPlan p = head_plan(*s, gradients);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    const bool f32 = s->dtype == PSGD_F32;
+
+    HeadDev h = {};
+    h.labels = labels, h.weight = weight, h.loss = loss;
+    h.tokens = (int)s->tokens, h.d = (int)s->d, h.vocab = (int)s->vocab;
+    h.count = reinterpret_cast<int*>(ws + p.count);
+    h.rows = reinterpret_cast<int*>(ws + p.rows);
+    h.label = reinterpret_cast<int*>(ws + p.label);
+    h.stats = reinterpret_cast<float2*>(ws + p.stats);
+    h.at_label = reinterpret_cast<float*>(ws + p.at_label);
+    h.e = ws + p.e;
+    h.D = reinterpret_cast<bf16_t*>(ws + p.D);
+    h.ldv = p.ldv, h.d_plane = (int64_t)p.piece * p.ldv;
+    h.tiles = p.tiles, h.n_planes = p.d_planes, h.keep = p.keep;
+    bf16_t* xc = reinterpret_cast<bf16_t*>(ws + p.xc);
+    const bf16_t* wc = static_cast<const bf16_t*>(w);
+    int64_t ldwc = ldw, w_plane = 0;
+
+    // at most 1024 blocks, each of which reads the labels before its own
+    const int per = std::max(16, (int)((s->tokens + 1023) / 1024));
+    const dim3 blocks((unsigned)std::max<int64_t>(1, (s->tokens + per - 1) / per));
+    if (f32) hipLaunchKernelGGL(head_gather_kernel<float>, blocks, dim3(kGatherThreads), 0, st, h, per, (const float*)x, ldx, xc, p.ldc, p.x_planes, (float*)dx, lddx);
+    else hipLaunchKernelGGL(head_gather_kernel<bf16_t>, blocks, dim3(kGatherThreads), 0, st, h, per, (const bf16_t*)x, ldx, xc, p.ldc, p.x_planes, (bf16_t*)dx, lddx);
+    if (hipGetLastError() != hipSuccess) return PSGD_E_HIP;
+    if (p.copy_w) {
+        bf16_t* to = reinterpret_cast<bf16_t*>(ws + p.wc);
+        if (launch_planes(w, s->dtype, s->vocab, s->d, ldw, to, p.w_planes, st) != hipSuccess) return PSGD_E_HIP;
+        wc = to, ldwc = p.ldc, w_plane = s->vocab * p.ldc;
+    }
+    for (int piece = 0; piece < p.pieces; ++piece) {
+        const int first = piece * p.piece, rows = (int)std::min<int64_t>(p.piece, s->tokens - first);
+        const bf16_t* xp = xc + (int64_t)first * p.ldc;
+        const int64_t x_plane = s->tokens * p.ldc;
+        TileArgs t = {};
+        t.count = h.count, t.first = first, t.n_split = 1;
+        if (rows > 0) {
+            t.P = {wc, ldwc, w_plane, (int)s->vocab};
+            t.L = {xp, p.ldc, x_plane, rows};
+            t.K = (int)p.ldc;
+            t.pairs = p.pairs, t.n_pairs = p.n_pairs;
+            if (launch_logits(t, h, p.bl, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
+        }
+        if (!gradients) continue;
+        TileOut o = {};
+        o.part = reinterpret_cast<float*>(ws + p.part);
+        if (rows > 0) {
+            t.P = {wc, ldwc, w_plane, (int)s->d};
+            t.L = {h.D, p.ldv, h.d_plane, rows};
+            t.K = (int)s->vocab;
+            t.pairs = p.dx_pairs, t.n_pairs = p.n_dx_pairs, t.n_split = p.dx_split;
+            o.ptr = dx, o.ld = lddx, o.dtype = s->dtype, o.rows = h.rows;
+            if (launch_product(false, true, p.bl, t, o, st) != hipSuccess) return PSGD_E_HIP;
+        }
+        t.P = {xp, p.ldc, x_plane, (int)s->d};
+        t.L = {h.D, p.ldv, h.d_plane, (int)s->vocab};
+        t.K = rows, t.count_is_k = 1;
+        t.pairs = p.dw_pairs, t.n_pairs = p.n_dw_pairs, t.n_split = p.dw_split;
+        o.rows = nullptr;
+        if (p.sum) { o.ptr = ws + p.sum; o.ld = p.ldc; o.dtype = PSGD_F32; o.accumulate = piece > 0; }
+        else { o.ptr = dw; o.ld = lddw; o.dtype = s->grad_dtype; o.accumulate = piece > 0 || accumulate; }
+        o.skip_empty = o.accumulate;
+        if (launch_product(false, false, 256, t, o, st) != hipSuccess) return PSGD_E_HIP;
+    }
+    if (gradients && p.sum) {
+        hipLaunchKernelGGL(head_round_kernel, dim3(2048), dim3(kThreads), 0, st, (const float*)(ws + p.sum), s->vocab, (int)s->d, p.ldc, (bf16_t*)dw, lddw, accumulate);
+        if (hipGetLastError() != hipSuccess) return PSGD_E_HIP;
+    }
+    return PSGD_OK;
+}
+
+}  // namespace psgd
+
+using namespace psgd;
+
+extern "C" {
+
+size_t psgd_head_workspace_bytes(const psgd_head_desc* desc, int gradients) {
+    return head_shape(desc) ? 0 : head_plan(*desc, gradients != 0).bytes;
+}
+
+int psgd_head_loss(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels, float* loss) {
+    return head_run(desc, false, workspace, stream, x, w, labels, nullptr, loss, nullptr, nullptr, 0);
+}
+
+int psgd_head_loss_grad(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
+                        const float* weight, float* loss, void* dx, void* dw, int accumulate) {
+    return head_run(desc, true, workspace, stream, x, w, labels, weight, loss, dx, dw, accumulate);
+}
+
+}  // extern "C"

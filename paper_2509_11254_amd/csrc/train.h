@@ -1,0 +1,60 @@
+// Host side of the training operators: the matrix products on tiles (tile.hip), 8-bit checkpoints (act.hip), the output
+// head's loss (head.hip).
+#pragma once
+#include "psgd_dev.h"
+#include "../../include/psgd.h"
+
+namespace psgd {
+
+struct TileOperand {
+    const bf16_t* ptr;
+    int64_t ld;         // elements, multiple of 8
+    int64_t plane;      // elements between planes
+    int extent;         // rows or columns of C that it covers
+};
+
+// What every kernel on tiles gets.  An operand may have several bf16 planes whose sum it is; `pairs` lists the products of planes to
+// add up, smallest first, four bits each: P's plane in the lower two, L's in the upper two.
+struct TileArgs {
+    TileOperand P, L;
+    int K;
+    const int* count;   // nullable: device word, tokens that count; of them this call takes those from `first` on, at most K or L.extent ...
+    int first;
+    int count_is_k;     // ... as contraction steps (1) or as rows of C (0)
+    unsigned pairs;
+    int n_pairs;
+    int n_split;        // parts of the contraction, each a workgroup of its own
+};
+constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048, kPairs22 = 0x014;
+// three planes each, six products: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+constexpr unsigned kPairs33 = 0x014852;
+
+// Where a product goes: C row l to row `rows[first + l]` (or l), columns as they are
+struct TileOut {
+    void* ptr;
+    int64_t ld;
+    int dtype;          // PSGD_F32 or PSGD_BF16
+    int accumulate;     // add to what is there
+    int skip_empty;     // write nothing where no token counts (a later piece of an accumulated product)
+    const int* rows;    // nullable
+    float* part;        // n_split > 1: partial sums [split][rows of C][part_ld]
+    int64_t part_ld;
+};
+
+int tile_splits(int64_t n_p, int64_t n_l, int64_t chunks, int64_t elems);
+size_t tile_part_bytes(int extent_p, int extent_l, int n_split);
+int tile_rows(int64_t extent_l);
+// C = L P^T over the operands' orientations: K-contiguous or K-strided
+hipError_t launch_product(bool p_contiguous, bool l_contiguous, int bl, const TileArgs& t, const TileOut& o, hipStream_t st);
+// rows x cols (ld) of fp32 or bf16 to `planes` bf16 planes [rows][round_up(cols, 8)], zeros beyond cols
+hipError_t launch_planes(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bf16_t* dst, int planes, hipStream_t st);
+
+inline int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline bool bad_dtype(int t) { return t != PSGD_F32 && t != PSGD_BF16; }
+inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+inline bool bad_ld(int64_t ld, int64_t cols) { return ld < cols || (ld & 7) != 0; }
+constexpr int64_t kMaxLd = 1 << 22;     // 255 rows * ld * 2 bytes stay within a buffer descriptor's range
+constexpr int64_t kMaxExtent = 1 << 30;
+
+}  // namespace psgd

@@ -24,7 +24,11 @@ EXPORTS = [
     "psgd_decompress", "psgd_decompress_msgd", "psgd_decompress_adam", "psgd_compress_project", "psgd_compress_finish", "psgd_status", "psgd_algorithmic_bytes", "psgd_kernel_bytes", "psgd_copy_bytes",
     "psgd_last_hip_error",
     "psgd_strerror", "psgd_destroy", "psgd_profile_enable", "psgd_profile_select", "psgd_profile_read",
+    "psgd_head_workspace_bytes", "psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore",
+    "psgd_act_glu", "psgd_act_glu_backward", "psgd_act_wgrad_workspace_bytes", "psgd_act_wgrad",
 ]
+PSGD_SILU, PSGD_GELU = 0, 1
+ACT_GROUP = 32      # columns of an activation that share a scale
 PROF_TAGS = ("sweep1", "sweep2", "residual")
 
 
@@ -43,6 +47,12 @@ class Options(C.Structure):
 class LayerStatus(C.Structure):
     _fields_ = [("rank_deficient", C.c_int32), ("refresh_iters_next", C.c_int32), ("sigma_max", C.c_float),
                 ("sigma_r", C.c_float), ("refresh_iters_no_gap", C.c_int32)]
+
+
+class HeadDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("d", C.c_int64), ("vocab", C.c_int64), ("ldx", C.c_int64), ("ldw", C.c_int64),
+                ("lddx", C.c_int64), ("lddw", C.c_int64), ("dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("piece_tokens", C.c_int64)]
 
 
 class PsgdError(RuntimeError):
@@ -112,6 +122,21 @@ def load_library() -> C.CDLL:
     lib.psgd_profile_select.restype = C.c_int
     lib.psgd_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int), C.c_int]
     lib.psgd_profile_read.restype = C.c_int
+    i, l, hd = C.c_int, C.c_int64, C.POINTER(HeadDesc)
+    lib.psgd_head_workspace_bytes.argtypes = [hd, i]
+    lib.psgd_head_workspace_bytes.restype = C.c_size_t
+    lib.psgd_head_loss.argtypes = [hd, vp, vp, vp, vp, vp, vp]
+    lib.psgd_head_loss_grad.argtypes = [hd, vp, vp, vp, vp, vp, vp, vp, vp, vp, i]
+    lib.psgd_act_store.argtypes = [vp, l, l, vp, i, l, vp, l, vp]
+    lib.psgd_act_restore.argtypes = [vp, l, l, vp, l, vp, vp, i, l]
+    lib.psgd_act_glu.argtypes = [vp, l, l, i, i, vp, vp, l, vp, l, vp, vp, vp, vp, l]
+    lib.psgd_act_glu_backward.argtypes = [vp, l, l, i, i, vp, vp, vp, vp, l, vp, l, vp, vp, l]
+    lib.psgd_act_wgrad_workspace_bytes.argtypes = [l, l, l, i]
+    lib.psgd_act_wgrad_workspace_bytes.restype = C.c_size_t
+    lib.psgd_act_wgrad.argtypes = [vp, vp, l, l, l, vp, i, l, vp, l, vp, vp, i, l, i]
+    for name in ("psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore", "psgd_act_glu",
+                 "psgd_act_glu_backward", "psgd_act_wgrad"):
+        getattr(lib, name).restype = C.c_int
     lib.psgd_destroy.argtypes = [vp]
     lib.psgd_destroy.restype = None
     _lib = lib
@@ -295,3 +320,184 @@ def copy_bytes(dst, src, n_bytes: int, stream=None) -> None:
     lib = load_library()
     rc = lib.psgd_copy_bytes(_stream_handle(stream), dst.data_ptr(), src.data_ptr(), int(n_bytes))
     _check(lib, None, rc)
+
+
+# ---- the training step around the compressor ---------------------------------------------------------------------------
+
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return PSGD_F32
+    if t.dtype == torch.bfloat16:
+        return PSGD_BF16
+    raise ValueError("float32 or bfloat16 expected, got %s" % t.dtype)
+
+
+def _matrix(name: str, t, rows: int, cols: int, dtype: Optional[int] = None) -> int:
+    """Checks a rows x cols matrix on the GPU with adjacent columns; its leading dimension."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols) or not t.is_cuda or (cols > 1 and t.stride(1) != 1):
+        raise ValueError("%s: a %d x %d matrix on the GPU with adjacent columns expected, got %s with strides %s on %s"
+                         % (name, rows, cols, tuple(t.shape), t.stride(), t.device))
+    if dtype is not None and _dtype_code(t) != dtype:
+        raise ValueError("%s: wrong element type %s" % (name, t.dtype))
+    # (with one row the stride says nothing)
+    ld = int(t.stride(0)) if rows > 1 else (cols + 7) // 8 * 8
+    if rows and t.storage_offset() + (rows - 1) * ld + (cols + 7) // 8 * 8 > t.untyped_storage().nbytes() // t.element_size():
+        raise ValueError("%s: the last row ends before the next multiple of 8 columns, up to which rows may be read" % name)
+    return ld
+
+
+def _vector(name: str, t, n: int, dtype):
+    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous elements of %s on the GPU expected" % (name, n, dtype))
+    return t
+
+
+def _work_area(n_bytes: int, device):
+    import torch
+    buf = torch.empty(n_bytes + 256, dtype=torch.uint8, device=device)
+    return buf, (buf.data_ptr() + 255) // 256 * 256
+
+
+class HeadLoss:
+    """Softmax cross entropy of X W^T against labels without logits in memory, and its gradients: psgd_head_loss and
+    psgd_head_loss_grad with a torch-allocated workspace, for one set of sizes and types.
+
+    A token whose label lies outside [0, vocab) does not count.  grad=False: losses alone (a smaller workspace).
+    """
+
+    def __init__(self, tokens: int, d: int, vocab: int, dtype: int = PSGD_BF16, grad_dtype: Optional[int] = None, *,
+                 grad: bool = True, piece_tokens: int = 0, device: str = "cuda"):
+        self.lib = load_library()
+        self.desc = HeadDesc(int(tokens), int(d), int(vocab), 0, 0, 0, 0, int(dtype),
+                             int(dtype if grad_dtype is None else grad_dtype), int(piece_tokens))
+        self.grad = bool(grad)
+        sizes = [int(self.lib.psgd_head_workspace_bytes(C.byref(self.desc), g)) for g in ([0, 1] if grad else [0])]
+        if min(sizes) == 0:
+            raise PsgdError(PSGD_E_INVALID_ARG, "sizes or types of the head")
+        self.workspace_bytes = max(sizes)
+        self.workspace, self._ws_ptr = _work_area(self.workspace_bytes, device)
+
+    def _inputs(self, X, W, labels, loss):
+        import torch
+        d = self.desc
+        d.ldx, d.ldw = _matrix("X", X, d.tokens, d.d, d.dtype), _matrix("W", W, d.vocab, d.d, d.dtype)
+        _vector("labels", labels, d.tokens, torch.int64)
+        _vector("loss", loss, d.tokens, torch.float32)
+
+    def loss(self, X, W, labels, loss, stream=None) -> None:
+        """loss[t] <- lse_t - logit of the label, 0 for tokens that do not count."""
+        self._inputs(X, W, labels, loss)
+        _check(self.lib, None, self.lib.psgd_head_loss(C.byref(self.desc), self._ws_ptr, _stream_handle(stream), X.data_ptr(),
+                                                       W.data_ptr(), labels.data_ptr(), loss.data_ptr()))
+
+    def loss_grad(self, X, W, labels, loss, dX, dW, weight=None, accumulate: bool = False, stream=None) -> None:
+        """loss as above; dX <- gradient of sum_t weight[t] loss[t] (weight None: the mean over the tokens that count), and
+        dW <- (accumulate: +=) its gradient."""
+        import torch
+        if not self.grad:
+            raise ValueError("this HeadLoss has no workspace for gradients (grad=False)")
+        self._inputs(X, W, labels, loss)
+        d = self.desc
+        d.lddx, d.lddw = _matrix("dX", dX, d.tokens, d.d, d.dtype), _matrix("dW", dW, d.vocab, d.d, d.grad_dtype)
+        if weight is not None:
+            _vector("weight", weight, d.tokens, torch.float32)
+        _check(self.lib, None, self.lib.psgd_head_loss_grad(
+            C.byref(self.desc), self._ws_ptr, _stream_handle(stream), X.data_ptr(), W.data_ptr(), labels.data_ptr(),
+            weight.data_ptr() if weight is not None else None, loss.data_ptr(), dX.data_ptr(), dW.data_ptr(), 1 if accumulate else 0))
+
+
+class Act8:
+    """An 8-bit checkpoint of an activation: codes (rows x ldc int8, ldc a multiple of 16, the first `cols` count) and
+    scales (rows x ceil(cols / 32) uint8, contiguous)."""
+
+    def __init__(self, codes, scales, cols: int):
+        import torch
+        rows, cols = int(codes.shape[0]), int(cols)
+        if codes.dtype != torch.int8 or codes.dim() != 2 or codes.shape[1] < (cols + 15) // 16 * 16 or codes.stride(1) != 1 or not codes.is_cuda:
+            raise ValueError("codes: an int8 matrix on the GPU with whole 16-byte pieces of adjacent columns expected")
+        if scales.dtype != torch.uint8 or tuple(scales.shape) != (rows, -(-cols // ACT_GROUP)) or not scales.is_contiguous() or not scales.is_cuda:
+            raise ValueError("scales: a contiguous %d x %d uint8 matrix on the GPU expected" % (rows, -(-cols // ACT_GROUP)))
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self.ldc = int(codes.stride(0)) if rows > 1 else (cols + 15) // 16 * 16
+
+
+def act_empty(rows: int, cols: int, device: str = "cuda") -> Act8:
+    """Buffers for the checkpoint of a rows x cols activation."""
+    import torch
+    return Act8(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device),
+                torch.empty((rows, -(-cols // ACT_GROUP)), dtype=torch.uint8, device=device), cols)
+
+
+def act_store(X, kept: Act8, stream=None) -> None:
+    """psgd_act_store: kept <- X in 8 bits."""
+    lib = load_library()
+    ld = _matrix("X", X, kept.rows, kept.cols)
+    _check(lib, None, lib.psgd_act_store(_stream_handle(stream), kept.rows, kept.cols, X.data_ptr(), _dtype_code(X), ld,
+                                         kept.codes.data_ptr(), kept.ldc, kept.scales.data_ptr()))
+
+
+def act_restore(kept: Act8, X, stream=None) -> None:
+    """psgd_act_restore: X <- the values that kept stands for."""
+    lib = load_library()
+    ld = _matrix("X", X, kept.rows, kept.cols)
+    _check(lib, None, lib.psgd_act_restore(_stream_handle(stream), kept.rows, kept.cols, kept.codes.data_ptr(), kept.ldc,
+                                           kept.scales.data_ptr(), X.data_ptr(), _dtype_code(X), ld))
+
+
+def _same(name: str, a, b) -> None:
+    if a != b:
+        raise ValueError("%s: %s and %s differ" % (name, a, b))
+
+
+def act_glu(gate, up, h, kept_gate: Act8, kept_up: Optional[Act8], act: int = PSGD_SILU, stream=None) -> None:
+    """psgd_act_glu: h <- act(gate) * up (up None: act(gate)), and the checkpoints of gate and up."""
+    lib = load_library()
+    rows, cols, dt = kept_gate.rows, kept_gate.cols, _dtype_code(gate)
+    ld_in, ld_h = _matrix("gate", gate, rows, cols), _matrix("h", h, rows, cols, dt)
+    if up is not None:
+        _same("leading dimensions of gate and up", ld_in, _matrix("up", up, rows, cols, dt))
+        _same("checkpoints of gate and up", (rows, cols, kept_gate.ldc), (kept_up.rows, kept_up.cols, kept_up.ldc))
+    _check(lib, None, lib.psgd_act_glu(
+        _stream_handle(stream), rows, cols, int(act), dt, gate.data_ptr(), up.data_ptr() if up is not None else None, ld_in,
+        h.data_ptr(), ld_h, kept_gate.codes.data_ptr(), kept_gate.scales.data_ptr(),
+        kept_up.codes.data_ptr() if up is not None else None, kept_up.scales.data_ptr() if up is not None else None, kept_gate.ldc))
+
+
+def act_glu_backward(kept_gate: Act8, kept_up: Optional[Act8], dh, dgate, dup, act: int = PSGD_SILU, stream=None) -> None:
+    """psgd_act_glu_backward: dgate <- dh * up * act'(gate), dup <- dh * act(gate) (kept_up, dup None: dgate <- dh * act'(gate))."""
+    lib = load_library()
+    rows, cols, dt = kept_gate.rows, kept_gate.cols, _dtype_code(dh)
+    ld_h, ld_out = _matrix("dh", dh, rows, cols), _matrix("dgate", dgate, rows, cols, dt)
+    _same("presence of the checkpoint of up and of dup", kept_up is None, dup is None)
+    if dup is not None:
+        _same("leading dimensions of dgate and dup", ld_out, _matrix("dup", dup, rows, cols, dt))
+        _same("checkpoints of gate and up", (rows, cols, kept_gate.ldc), (kept_up.rows, kept_up.cols, kept_up.ldc))
+    _check(lib, None, lib.psgd_act_glu_backward(
+        _stream_handle(stream), rows, cols, int(act), dt, kept_gate.codes.data_ptr(), kept_gate.scales.data_ptr(),
+        kept_up.codes.data_ptr() if dup is not None else None, kept_up.scales.data_ptr() if dup is not None else None,
+        kept_gate.ldc, dh.data_ptr(), ld_h, dgate.data_ptr(), dup.data_ptr() if dup is not None else None, ld_out))
+
+
+class WeightGrad:
+    """psgd_act_wgrad with a torch-allocated workspace, for one set of sizes and types: G = dY^T X from dY and the 8-bit
+    checkpoint of X."""
+
+    def __init__(self, tokens: int, out_features: int, in_features: int, dtype: int = PSGD_BF16,
+                 grad_dtype: Optional[int] = None, *, device: str = "cuda"):
+        self.lib = load_library()
+        self.shape = (int(tokens), int(out_features), int(in_features))
+        self.dtype, self.grad_dtype = int(dtype), int(dtype if grad_dtype is None else grad_dtype)
+        self.workspace_bytes = int(self.lib.psgd_act_wgrad_workspace_bytes(*self.shape, self.dtype))
+        if self.workspace_bytes == 0 or self.grad_dtype not in (PSGD_F32, PSGD_BF16):
+            raise PsgdError(PSGD_E_INVALID_ARG, "sizes or types of the weight gradient")
+        self.workspace, self._ws_ptr = _work_area(self.workspace_bytes, device)
+
+    def run(self, dY, kept: Act8, G, accumulate: bool = False, stream=None) -> None:
+        tokens, out_features, in_features = self.shape
+        ldy = _matrix("dY", dY, tokens, out_features, self.dtype)
+        ldg = _matrix("G", G, out_features, in_features, self.grad_dtype)
+        _same("sizes of the checkpoint", (kept.rows, kept.cols), (tokens, in_features))
+        _check(self.lib, None, self.lib.psgd_act_wgrad(
+            self._ws_ptr, _stream_handle(stream), tokens, out_features, in_features, dY.data_ptr(), self.dtype, ldy,
+            kept.codes.data_ptr(), kept.ldc, kept.scales.data_ptr(), G.data_ptr(), self.grad_dtype, ldg, 1 if accumulate else 0))
