@@ -14,7 +14,6 @@
 
 namespace psgd {
 
-typedef _Float16 halfx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
 // what is kept of exp(l - tile's maximum): nothing, fp16 of 2^15 times it (the range of fp16 starts 2^29 below the maximum;
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
 // ---- logits of a piece: statistics per tile, exponentials --------------------------------------------------------------
 
 template <int BL, int KEEP>
-__global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t, HeadDev h, int n_p, int n_l) {
+__global__ __launch_bounds__(tile_threads<BL>(), BL == 256 ? 1 : 2) void head_logits_kernel(TileArgs t, HeadDev h, int n_p, int n_l) {
     extern __shared__ __align__(16) unsigned char smem[];
     using T = Tile<true, true, BL>;
     const TilePlace at = tile_place(blockIdx.x, n_p, n_l, 1);
@@ -129,8 +128,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t
     const int nl = counted(t, t.L.extent);
     if (l0 >= nl) return;
     T tile;
-    tile.run(t, p0, l0, nl, t.K, 0, (PSGD_TLDS unsigned char*)smem);
-    const int valid = h.vocab - p0;         // columns of this tile
+    tile.template run<true>(t, p0, l0, nl, t.K, 0, (PSGD_TLDS unsigned char*)smem);
     constexpr float kLog2e = 1.4426950408889634f;
     // the wave's maximum per row, over its columns; a tile has at least one column
     float* red = reinterpret_cast<float*>(smem);        // [WP][BL]
@@ -141,11 +139,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t
 #pragma unroll
         for (int i = 0; i < T::FP; ++i)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int c = tile.col(i, v >> 2) + (v & 3);
-                if (c >= valid) tile.acc[i][j][v] = -__builtin_inff();
-                m = fmaxf(m, tile.acc[i][j][v]);
-            }
+            for (int v = 0; v < 16; ++v) m = fmaxf(m, tile.acc[i][j][v]);
         m = fmaxf(m, __shfl_xor(m, 32));
         if ((threadIdx.x & 63) < 32) red[tile.wp * BL + tile.row(j)] = m;
     }
@@ -159,33 +153,33 @@ __global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t
         for (int w = 1; w < T::WP; ++w) m = fmaxf(m, red[w * BL + row]);
         most[j] = m;
         const float base = m == -__builtin_inff() ? 0.f : m;
-        const int y = l < nl ? h.label[t.first + l] - p0 : -1;
-        float s = 0.f;
+        // The label's element, if it is this lane's (of eight columns next to each other a lane has the first or the last four), is left out of
+        // the sum.  Few tiles have it: the search for it stands apart, and only reads.
+        const int y = l < nl ? h.label[t.first + l] - p0 - tile.col(0, 0) : -1;
+        const bool found = y >= 0 && y < 32 * T::FP && (y & 4) == 0, any = __any(found);
+        float at_label = 0.f, s = 0.f;
+        if (any) {
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) at_label = y == 32 * i + 8 * (v >> 2) + (v & 3) ? tile.acc[i][j][v] : at_label;
+            if (found) h.at_label[l] = at_label;
+        }
 #pragma unroll
         for (int i = 0; i < T::FP; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = tile.col(i, q);
-                float e[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float x = tile.acc[i][j][4 * q + u];
-                    e[u] = __builtin_amdgcn_exp2f((x - base) * kLog2e);
-                    if (c + u == y) h.at_label[l] = x;
-                    else s += e[u];
-                }
-                if (KEEP != KEEP_NONE && l < nl && p0 + c < h.ldv) {
-                    if constexpr (KEEP == KEEP_F16) {
-                        halfx4 o;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) o[u] = (_Float16)(e[u] * kHalfScale);
-                        *reinterpret_cast<PSGD_GLOBAL halfx4*>(as_global((_Float16*)h.e) + l * h.ldv + p0 + c) = o;
-                    } else {
-                        const floatx4 o = {e[0], e[1], e[2], e[3]};
-                        *reinterpret_cast<PSGD_GLOBAL floatx4*>(as_global((float*)h.e) + l * h.ldv + p0 + c) = o;
-                    }
-                }
+            for (int v = 0; v < 16; ++v) {
+                const float e = __builtin_amdgcn_exp2f((tile.acc[i][j][v] - base) * kLog2e);
+                s += e;
+                tile.acc[i][j][v] = e;
             }
+        if (any) {
+            s = 0.f;
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s += y == 32 * i + 8 * (v >> 2) + (v & 3) ? 0.f : tile.acc[i][j][v];
+        }
         sum[j] = s + __shfl_xor(s, 32);
     }
     __syncthreads();
@@ -202,6 +196,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void head_logits_kernel(TileArgs t
             for (int w = 1; w < T::WP; ++w) s += red[w * BL + row];
             h.stats[(int64_t)l * h.tiles + at.p] = make_float2(most[j], s);
         }
+    }
+    if constexpr (KEEP == KEEP_F16) {
+        tile.template for_rows<8>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, const float (&v)[8]) {
+            halfx8 o;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = (_Float16)(v[u] * kHalfScale);
+            if (l0 + row < nl && p0 + col < h.ldv) *reinterpret_cast<PSGD_GLOBAL halfx8*>(as_global((_Float16*)h.e) + (l0 + row) * h.ldv + p0 + col) = o;
+        });
+    } else if constexpr (KEEP == KEEP_F32) {
+        tile.template for_rows<4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, const float (&v)[4]) {
+            if (l0 + row < nl && p0 + col < h.ldv)
+                *reinterpret_cast<PSGD_GLOBAL floatx4*>(as_global((float*)h.e) + (l0 + row) * h.ldv + p0 + col) = floatx4{v[0], v[1], v[2], v[3]};
+        });
     }
 }
 
@@ -365,7 +372,7 @@ static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, int bl, hip
         constexpr int lds = Tile<true, true, BL>::LDS_BYTES;                                                              \
         e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);     \
         if (e != hipSuccess) return e;                                                                                    \
-        hipLaunchKernelGGL(kfn, dim3(n_p * n_l), dim3(kTileThreads), lds, st, t, h, n_p, n_l);                            \
+        hipLaunchKernelGGL(kfn, dim3(n_p * n_l), dim3(tile_threads<BL>()), lds, st, t, h, n_p, n_l);                            \
         e = hipGetLastError();                                                                                            \
     } while (0)
 #define PSGD_LOGITS_KEEP(BL)                                       \

@@ -4,36 +4,45 @@
 
 namespace psgd {
 
-__device__ __forceinline__ void store4(PSGD_GLOBAL float* p, const float (&v)[4], int n, bool add) {
-    if (n >= 4) {
-        floatx4 o = {v[0], v[1], v[2], v[3]};
-        PSGD_GLOBAL floatx4* q = reinterpret_cast<PSGD_GLOBAL floatx4*>(p);
-        if (add) o += *q;
-        *q = o;
-    } else {
-        for (int u = 0; u < n; ++u) p[u] = add ? p[u] + v[u] : v[u];
-    }
-}
-__device__ __forceinline__ void store4(PSGD_GLOBAL bf16_t* p, const float (&v)[4], int n, bool add) {
-    if (n >= 4) {
-        PSGD_GLOBAL bf16x4* q = reinterpret_cast<PSGD_GLOBAL bf16x4*>(p);
-        bf16x4 o;
-        if (add) {
-            const bf16x4 b = *q;
+// N consecutive elements of a row of C, of which the first n are inside
+template <int N>
+__device__ __forceinline__ void store_row(PSGD_GLOBAL float* p, const float (&v)[N], int n, bool add) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) o[u] = (bf16_t)(v[u] + (float)b[u]);
+    for (int h = 0; h < N; h += 4) {
+        if (n >= h + 4) {
+            floatx4 o = {v[h], v[h + 1], v[h + 2], v[h + 3]};
+            PSGD_GLOBAL floatx4* q = reinterpret_cast<PSGD_GLOBAL floatx4*>(p + h);
+            if (add) o += *q;
+            *q = o;
         } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) o[u] = (bf16_t)v[u];
+            for (int u = 0; u < 4; ++u)
+                if (h + u < n) p[h + u] = add ? p[h + u] + v[h + u] : v[h + u];
         }
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_row(PSGD_GLOBAL bf16_t* p, const float (&v)[N], int n, bool add) {
+    static_assert(N == 8, "pieces");
+    if (n >= 8) {
+        PSGD_GLOBAL bf16x8* q = reinterpret_cast<PSGD_GLOBAL bf16x8*>(p);
+        bf16x8 o, b;
+        if (add) b = *q;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[u] = (bf16_t)(add ? v[u] + (float)b[u] : v[u]);
         *q = o;
     } else {
-        for (int u = 0; u < n; ++u) p[u] = (bf16_t)(add ? (float)p[u] + v[u] : v[u]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (u < n) p[u] = (bf16_t)(add ? (float)p[u] + v[u] : v[u]);
     }
 }
 
-template <bool PKC, bool LKC, int BL>
-__global__ __launch_bounds__(kTileThreads, 2) void product_kernel(TileArgs t, TileOut o, int n_p, int n_l) {
+// what a product kernel writes
+enum TileKind { TILE_PART = 0, TILE_F32 = 1, TILE_BF16 = 2 };
+
+template <bool PKC, bool LKC, int BL, int KIND>
+__global__ __launch_bounds__(tile_threads<BL>(), BL == 256 ? 1 : 2) void product_kernel(TileArgs t, TileOut o, int n_p, int n_l) {
     extern __shared__ __align__(16) unsigned char smem[];
     using T = Tile<PKC, LKC, BL>;
     const TilePlace at = tile_place(blockIdx.x, n_p, n_l, t.n_split);
@@ -42,40 +51,38 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(TileArgs t, Ti
     if (l0 >= nl || (K == 0 && o.skip_empty)) return;
     T tile;
     tile.run(t, p0, l0, nl, K, at.split, (PSGD_TLDS unsigned char*)smem);
-#pragma unroll
-    for (int j = 0; j < T::FL; ++j) {
-        const int l = l0 + tile.row(j);
-        if (l >= nl) continue;
-        const int64_t row = o.rows && !o.part ? o.rows[t.first + l] : l;
-#pragma unroll
-        for (int i = 0; i < T::FP; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = p0 + tile.col(i, q), n = t.P.extent - c;
-                if (n <= 0) continue;
-                const float v[4] = {tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1], tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3]};
-                if (o.part) store4(as_global(o.part) + ((int64_t)at.split * t.L.extent + l) * o.part_ld + c, v, 4, false);
-                else if (o.dtype == PSGD_F32) store4(as_global((float*)o.ptr) + row * o.ld + c, v, n, o.accumulate);
-                else store4(as_global((bf16_t*)o.ptr) + row * o.ld + c, v, n, o.accumulate);
-            }
-    }
+    tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, const auto& v) {
+        const int l = l0 + row, c = p0 + col, n = t.P.extent - c;
+        if (l >= nl || n <= 0) return;
+        if constexpr (KIND == TILE_PART) {
+            PSGD_GLOBAL float* p = as_global(o.part) + ((int64_t)at.split * t.L.extent + l) * o.part_ld + c;
+            *reinterpret_cast<PSGD_GLOBAL floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+        } else {
+            const int64_t to = (o.rows ? o.rows[t.first + l] : l) * o.ld + c;
+            if constexpr (KIND == TILE_F32) store_row(as_global((float*)o.ptr) + to, v, n, o.accumulate);
+            else store_row(as_global((bf16_t*)o.ptr) + to, v, n, o.accumulate);
+        }
+    });
 }
 
-// sum over the splits, in their order, of four elements per thread
+// sum over the splits, in their order, of eight elements per thread
 __global__ __launch_bounds__(kThreads) void split_sum_kernel(TileArgs t, TileOut o) {
     const int K = t.count_is_k ? counted(t, t.K) : t.K, nl = t.count_is_k ? t.L.extent : counted(t, t.L.extent);
     if (K == 0 && o.skip_empty) return;
-    const int quads = (t.P.extent + 3) / 4;
-    const int64_t all = (int64_t)nl * quads, layer = (int64_t)t.L.extent * o.part_ld;
+    const int pieces = (t.P.extent + 7) / 8;
+    const int64_t all = (int64_t)nl * pieces, layer = (int64_t)t.L.extent * o.part_ld;
     for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < all; e += (int64_t)gridDim.x * kThreads) {
-        const int l = (int)(e / quads), c = 4 * (int)(e - (int64_t)l * quads);
+        const int l = (int)(e / pieces), c = 8 * (int)(e - (int64_t)l * pieces);
         const PSGD_GLOBAL float* p = as_global(o.part) + l * o.part_ld + c;
-        floatx4 s = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < t.n_split; ++k) s += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer);
-        const float v[4] = {s[0], s[1], s[2], s[3]};
+        floatx4 s = {0.f, 0.f, 0.f, 0.f}, r = s;
+        for (int k = 0; k < t.n_split; ++k) {
+            s += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer);
+            r += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer + 4);
+        }
+        const float v[8] = {s[0], s[1], s[2], s[3], r[0], r[1], r[2], r[3]};
         const int64_t row = o.rows ? o.rows[t.first + l] : l;
-        if (o.dtype == PSGD_F32) store4(as_global((float*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
-        else store4(as_global((bf16_t*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
+        if (o.dtype == PSGD_F32) store_row(as_global((float*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
+        else store_row(as_global((bf16_t*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
     }
 }
 
@@ -114,23 +121,29 @@ int tile_splits(int64_t n_p, int64_t n_l, int64_t chunks, int64_t elems) {
 }
 
 size_t tile_part_bytes(int extent_p, int extent_l, int n_split) {
-    return n_split > 1 ? up256((size_t)n_split * extent_l * ((extent_p + 3) / 4 * 4) * sizeof(float)) : 0;
+    return n_split > 1 ? up256((size_t)n_split * extent_l * ((extent_p + 7) / 8 * 8) * sizeof(float)) : 0;
 }
 
-template <bool PKC, bool LKC, int BL>
-static hipError_t launch_tiles(const TileArgs& t, const TileOut& o, int n_p, int n_l, hipStream_t st) {
-    auto kfn = product_kernel<PKC, LKC, BL>;
+template <bool PKC, bool LKC, int BL, int KIND>
+static hipError_t launch_kind(const TileArgs& t, const TileOut& o, int n_p, int n_l, hipStream_t st) {
+    auto kfn = product_kernel<PKC, LKC, BL, KIND>;
     constexpr int lds = Tile<PKC, LKC, BL>::LDS_BYTES;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kfn, dim3(n_p * n_l * t.n_split), dim3(kTileThreads), lds, st, t, o, n_p, n_l);
+    hipLaunchKernelGGL(kfn, dim3(n_p * n_l * t.n_split), dim3(tile_threads<BL>()), lds, st, t, o, n_p, n_l);
     return hipGetLastError();
+}
+template <bool PKC, bool LKC, int BL>
+static hipError_t launch_tiles(const TileArgs& t, const TileOut& o, int n_p, int n_l, hipStream_t st) {
+    if (o.part) return launch_kind<PKC, LKC, BL, TILE_PART>(t, o, n_p, n_l, st);
+    if (o.dtype == PSGD_F32) return launch_kind<PKC, LKC, BL, TILE_F32>(t, o, n_p, n_l, st);
+    return launch_kind<PKC, LKC, BL, TILE_BF16>(t, o, n_p, n_l, st);
 }
 
 hipError_t launch_product(bool p_contiguous, bool l_contiguous, int bl, const TileArgs& t, const TileOut& out, hipStream_t st) {
     TileOut o = out;
     if (t.n_split == 1) o.part = nullptr;
-    o.part_ld = (t.P.extent + 3) / 4 * 4;
+    o.part_ld = (t.P.extent + 7) / 8 * 8;
     const int n_p = (t.P.extent + kTileP - 1) / kTileP, n_l = (t.L.extent + bl - 1) / bl;
     if (n_p * (int64_t)n_l * t.n_split > INT32_MAX) return hipErrorInvalidValue;
     hipError_t e = hipErrorInvalidValue;
@@ -142,8 +155,8 @@ hipError_t launch_product(bool p_contiguous, bool l_contiguous, int bl, const Ti
         e = launch_tiles<false, false, 256>(t, o, n_p, n_l, st);
     }
     if (e != hipSuccess || t.n_split == 1) return e;
-    const int64_t quads = (int64_t)t.L.extent * ((t.P.extent + 3) / 4);
-    hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)std::min<int64_t>((quads + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
+    const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 7) / 8);
+    hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
     return hipGetLastError();
 }
 

@@ -6,6 +6,9 @@
 
 namespace psgd {
 
+constexpr int kTileP = 256;     // elements of a tile of C along P
+constexpr int kTileK = 64;      // contraction steps per chunk
+
 struct TileOperand {
     const bf16_t* ptr;
     int64_t ld;         // elements, multiple of 8
