@@ -223,7 +223,8 @@ static bool bad_ldc(int64_t ldc, int64_t cols) { return ldc < cols || (ldc & 15)
 
 struct WgradPlan {
     size_t bytes = 0, x = 0, planes = 0, part = 0;
-    int n_planes = 1, n_split = 1;
+    int n_planes = 1;
+    TilePlan tile = {};
     int64_t ldx = 0;
 };
 static WgradPlan wgrad_plan(int64_t tokens, int64_t out, int64_t in, int dtype) {
@@ -235,8 +236,8 @@ static WgradPlan wgrad_plan(int64_t tokens, int64_t out, int64_t in, int dtype) 
         w.n_planes = 3;
         w.planes = take((size_t)tokens * up8(out) * 2 * 3);
     }
-    w.n_split = tile_splits((in + 255) / 256, (out + 255) / 256, (tokens + 63) / 64 * w.n_planes, out * in);
-    w.part = take(tile_part_bytes((int)in, (int)out, w.n_split));
+    w.tile = tile_plan(in, out, (tokens + kTileK - 1) / kTileK * w.n_planes, true);
+    w.part = take(tile_part_bytes(in, out, w.tile));
     return w;
 }
 static int wgrad_shape(int64_t tokens, int64_t out, int64_t in) {
@@ -351,14 +352,14 @@ int psgd_act_wgrad(void* workspace, void* stream, int64_t tokens, int64_t out_fe
     t.K = (int)tokens;
     t.pairs = w.n_planes == 3 ? kPairsL3 : kPairs1;
     t.n_pairs = w.n_planes;
-    t.n_split = w.n_split;
+    t.n_split = w.tile.n_split;
     TileOut o = {};
     o.ptr = g;
     o.ld = ldg;
     o.dtype = g_dtype;
     o.accumulate = accumulate != 0;
     o.part = reinterpret_cast<float*>(ws + w.part);
-    return launch_product(false, false, 256, t, o, st) == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+    return launch_product(false, w.tile.shape, t, o, st) == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
 
 }  // extern "C"

@@ -2,6 +2,7 @@
 //
 //   l_tv = x_t . w_v,  lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,y(t)
 //   D_tv = c_t (exp(l_tv - lse_t) - [v = y(t)]),  dX = D W,  dW = D^T X,   c_t: the token's weight, or 1 / (tokens that count)
+//   (D is kept relative to the largest c_t, which the products are multiplied by at their end)
 //
 // Tokens whose label lies outside [0, V) do not count: their rows are left out from the start (the others are copied together,
 // in order), so that what they hold, NaN or not, reaches neither sum nor product.
@@ -28,6 +29,7 @@ struct HeadDev {
     int tokens, d, vocab;
     // in the workspace
     int* count;          // tokens that count
+    float* scale;        // the largest c_t: D is kept relative to it and its products are multiplied by it
     int* rows;           // which they are
     int* label;          // and their labels
     float2* stats;       // [token of the piece][tile]: maximum, sum of exponentials without the label's
@@ -35,7 +37,7 @@ struct HeadDev {
     void* e;             // exponentials, [token of the piece][ldv]
     bf16_t* D;           // planes of D, [token of the piece][ldv]; in place of e where that is fp16
     int64_t ldv, d_plane;
-    int tiles, n_planes, keep;
+    int tiles, tile_width, n_planes, keep;
 };
 
 // ---- tokens that count ----------------------------------------------------------------------------------------------
@@ -114,21 +116,40 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
             }
         }
     }
-    if (last == h.tokens && threadIdx.x == 0) *h.count = before;
+    if (last == h.tokens) {
+        // (1 / count is not a bf16 number, and the same error in all of D would come out in the results; relative to the largest weight, D of
+        // a token that its model gives no probability is -1)
+        float most = 0.f;
+        if (h.weight)
+            for (int i = threadIdx.x; i < h.tokens; i += kGatherThreads) most = fmaxf(most, counts(h.labels[i], h.vocab) ? fabsf(h.weight[i]) : 0.f);
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+        __syncthreads();
+        float* all = reinterpret_cast<float*>(sum);
+        if (lane == 0) all[wv] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int w = 0; w < kGatherThreads / 64; ++w) most = fmaxf(most, all[w]);
+            *h.count = before;
+            *h.scale = !h.weight ? 1.f / (float)max(before, 1) : most > 0.f && most < __builtin_inff() ? most : 1.f;
+        }
+    }
 }
 
 // ---- logits of a piece: statistics per tile, exponentials --------------------------------------------------------------
 
-template <int BL, int KEEP>
-__global__ __launch_bounds__(tile_threads<BL>(), BL == 256 ? 1 : 2) void head_logits_kernel(TileArgs t, HeadDev h, int n_p, int n_l) {
+template <TileShape SHAPE, int KEEP>
+__global__ __launch_bounds__(kTileThreads, 1) void head_logits_kernel(TileArgs t, HeadDev h) {
     extern __shared__ __align__(16) unsigned char smem[];
-    using T = Tile<true, true, BL>;
-    const TilePlace at = tile_place(blockIdx.x, n_p, n_l, 1);
-    const int p0 = at.p * kTileP, l0 = at.l * BL;
+    using T = Tile<true, true, SHAPE>;
+    constexpr int BL = T::BL;
     const int nl = counted(t, t.L.extent);
-    if (l0 >= nl) return;
+    const TilePlace at = tile_place(blockIdx.x, tile_grid<SHAPE>(t, nl, 0));
+    if (at.split < 0) return;
+    const int p0 = at.p * T::BP, l0 = at.l * BL;
     T tile;
-    tile.template run<true>(t, p0, l0, nl, t.K, 0, (PSGD_TLDS unsigned char*)smem);
+    tile.template run<true>(t, p0, l0, nl, t.K, 0, 1, (PSGD_TLDS unsigned char*)smem);
     constexpr float kLog2e = 1.4426950408889634f;
     // the wave's maximum per row, over its columns; a tile has at least one column
     float* red = reinterpret_cast<float*>(smem);        // [WP][BL]
@@ -252,12 +273,12 @@ __global__ __launch_bounds__(kThreads) void head_rows_kernel(HeadDev h, int firs
     if (blockIdx.y == 0 && threadIdx.x == 0)
         h.loss[token] = r.others < e_label ? log1pf(r.others / e_label) : r.most - at_label + logf(total);
     if constexpr (KEEP == KEEP_NONE) return;
-    const float c = (h.weight ? h.weight[token] : 1.f / (float)*h.count) / total;
+    const float c = (h.weight ? h.weight[token] / *h.scale : 1.f) / total;
     const int y = h.label[first + l];
     const float d_label = -r.others * c;        // (p - 1 as the sum of the other probabilities)
     const int end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
     for (int v = blockIdx.y * span + 8 * threadIdx.x; v < end; v += 8 * kThreads) {
-        const float most = h.stats[(int64_t)l * h.tiles + v / kTileP].x;
+        const float most = h.stats[(int64_t)l * h.tiles + v / h.tile_width].x;
         const float f = expf(most - r.most) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
         float x[8];
         if constexpr (KEEP == KEEP_F16) {
@@ -304,9 +325,10 @@ constexpr size_t kPieceBytes = (size_t)1 << 30;     // what is kept of one piece
 
 struct HeadPlan {
     size_t bytes = 0;
-    size_t count, rows, label, xc, wc, stats, at_label, e, D, part, sum;
+    size_t count, scale, rows, label, xc, wc, stats, at_label, e, D, part, sum;
     int64_t ldc, ldv;
-    int piece, pieces, tiles, x_planes, w_planes, d_planes, keep, bl, dx_split, dw_split;
+    int piece, pieces, tiles, x_planes, w_planes, d_planes, keep;
+    TilePlan logits, dx, dw;
     unsigned pairs, dx_pairs, dw_pairs;
     int n_pairs, n_dx_pairs, n_dw_pairs;
     bool copy_w;
@@ -317,7 +339,6 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     const bool f32 = s.dtype == PSGD_F32;
     p.ldc = up8(s.d);
     p.ldv = up8(s.vocab);
-    p.tiles = (int)((s.vocab + kTileP - 1) / kTileP);
     p.x_planes = p.w_planes = f32 ? 3 : 1;
     p.copy_w = f32 || s.d % 8 != 0;
     p.pairs = f32 ? kPairs33 : kPairs1;
@@ -329,15 +350,17 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     else { p.dw_pairs = s.grad_dtype == PSGD_F32 ? kPairsL2 : kPairs1; p.n_dw_pairs = s.grad_dtype == PSGD_F32 ? 2 : 1; }
     // tokens per piece
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
-    const size_t row = !gradients ? p.tiles * sizeof(float2) : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
+    const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
     const int64_t most = s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256);
     p.pieces = (int)((tokens + most - 1) / most);
     p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
     if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
     p.pieces = (int)((tokens + p.piece - 1) / p.piece);
-    p.bl = tile_rows(p.piece);
+    p.logits = tile_plan(s.vocab, p.piece, (p.ldc + kTileK - 1) / kTileK * p.n_pairs, false);
+    p.tiles = (int)((s.vocab + tile_p(p.logits.shape) - 1) / tile_p(p.logits.shape));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
     p.count = take(4);
+    p.scale = take(4);
     p.rows = take((size_t)tokens * 4);
     p.label = take((size_t)tokens * 4);
     p.xc = take((size_t)tokens * p.ldc * 2 * p.x_planes);
@@ -348,10 +371,9 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
         const size_t elems = (size_t)p.piece * p.ldv;
         p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
         p.D = p.keep == KEEP_F16 ? p.e : take(elems * 2 * p.d_planes);
-        const int64_t n_d = (s.d + kTileP - 1) / kTileP;
-        p.dx_split = tile_splits(n_d, (p.piece + p.bl - 1) / p.bl, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, p.piece * s.d);
-        p.dw_split = tile_splits(n_d, p.tiles, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, s.vocab * s.d);
-        p.part = take(std::max(tile_part_bytes((int)s.d, p.piece, p.dx_split), tile_part_bytes((int)s.d, (int)s.vocab, p.dw_split)));
+        p.dx = tile_plan(s.d, p.piece, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, true);
+        p.dw = tile_plan(s.d, s.vocab, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, true);
+        p.part = take(std::max(tile_part_bytes(s.d, p.piece, p.dx), tile_part_bytes(s.d, s.vocab, p.dw)));
         p.sum = p.pieces > 1 && s.grad_dtype == PSGD_BF16 ? take((size_t)s.vocab * p.ldc * 4) : 0;
     }
     return p;
@@ -363,30 +385,27 @@ static int head_shape(const psgd_head_desc* s) {
     return PSGD_OK;
 }
 
-static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, int bl, hipStream_t st) {
-    const int n_p = h.tiles, n_l = (t.L.extent + bl - 1) / bl;
-    hipError_t e = hipErrorInvalidValue;
-#define PSGD_LOGITS(BL, KEEP)                                                                                             \
-    do {                                                                                                                  \
-        auto kfn = head_logits_kernel<BL, KEEP>;                                                                          \
-        constexpr int lds = Tile<true, true, BL>::LDS_BYTES;                                                              \
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);     \
-        if (e != hipSuccess) return e;                                                                                    \
-        hipLaunchKernelGGL(kfn, dim3(n_p * n_l), dim3(tile_threads<BL>()), lds, st, t, h, n_p, n_l);                            \
-        e = hipGetLastError();                                                                                            \
-    } while (0)
-#define PSGD_LOGITS_KEEP(BL)                                       \
-    do {                                                           \
-        if (h.keep == KEEP_NONE) PSGD_LOGITS(BL, KEEP_NONE);       \
-        else if (h.keep == KEEP_F16) PSGD_LOGITS(BL, KEEP_F16);    \
-        else PSGD_LOGITS(BL, KEEP_F32);                            \
-    } while (0)
-    if (bl == 256) PSGD_LOGITS_KEEP(256);
-    else if (bl == 128) PSGD_LOGITS_KEEP(128);
-    else if (bl == 64) PSGD_LOGITS_KEEP(64);
-#undef PSGD_LOGITS
-#undef PSGD_LOGITS_KEEP
-    return e;
+template <TileShape SHAPE, int KEEP>
+static hipError_t launch_logits_as(const TileArgs& t, const HeadDev& h, hipStream_t st) {
+    const int64_t blocks = h.tiles * (int64_t)((t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE));
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    auto kfn = head_logits_kernel<SHAPE, KEEP>;
+    constexpr int lds = Tile<true, true, SHAPE>::LDS_BYTES;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(kTileThreads), lds, st, t, h);
+    return hipGetLastError();
+}
+template <TileShape SHAPE>
+static hipError_t launch_logits_shape(const TileArgs& t, const HeadDev& h, hipStream_t st) {
+    if (h.keep == KEEP_NONE) return launch_logits_as<SHAPE, KEEP_NONE>(t, h, st);
+    if (h.keep == KEEP_F16) return launch_logits_as<SHAPE, KEEP_F16>(t, h, st);
+    return launch_logits_as<SHAPE, KEEP_F32>(t, h, st);
+}
+static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, TileShape shape, hipStream_t st) {
+    if (shape == TILE_256) return launch_logits_shape<TILE_256>(t, h, st);
+    if (shape == TILE_128) return launch_logits_shape<TILE_128>(t, h, st);
+    return launch_logits_shape<TILE_THIN>(t, h, st);
 }
 
 static hipError_t launch_rows(const HeadDev& h, int first, int rows, hipStream_t st) {
@@ -422,6 +441,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     h.labels = labels, h.weight = weight, h.loss = loss;
     h.tokens = (int)s->tokens, h.d = (int)s->d, h.vocab = (int)s->vocab;
     h.count = reinterpret_cast<int*>(ws + p.count);
+    h.scale = reinterpret_cast<float*>(ws + p.scale);
     h.rows = reinterpret_cast<int*>(ws + p.rows);
     h.label = reinterpret_cast<int*>(ws + p.label);
     h.stats = reinterpret_cast<float2*>(ws + p.stats);
@@ -429,7 +449,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     h.e = ws + p.e;
     h.D = reinterpret_cast<bf16_t*>(ws + p.D);
     h.ldv = p.ldv, h.d_plane = (int64_t)p.piece * p.ldv;
-    h.tiles = p.tiles, h.n_planes = p.d_planes, h.keep = p.keep;
+    h.tiles = p.tiles, h.tile_width = tile_p(p.logits.shape), h.n_planes = p.d_planes, h.keep = p.keep;
     bf16_t* xc = reinterpret_cast<bf16_t*>(ws + p.xc);
     const bf16_t* wc = static_cast<const bf16_t*>(w);
     int64_t ldwc = ldw, w_plane = 0;
@@ -456,28 +476,29 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
             t.L = {xp, p.ldc, x_plane, rows};
             t.K = (int)p.ldc;
             t.pairs = p.pairs, t.n_pairs = p.n_pairs;
-            if (launch_logits(t, h, p.bl, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
+            if (launch_logits(t, h, p.logits.shape, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
         }
         if (!gradients) continue;
         TileOut o = {};
         o.part = reinterpret_cast<float*>(ws + p.part);
+        o.scale = h.scale;
         if (rows > 0) {
             t.P = {wc, ldwc, w_plane, (int)s->d};
             t.L = {h.D, p.ldv, h.d_plane, rows};
             t.K = (int)s->vocab;
-            t.pairs = p.dx_pairs, t.n_pairs = p.n_dx_pairs, t.n_split = p.dx_split;
+            t.pairs = p.dx_pairs, t.n_pairs = p.n_dx_pairs, t.n_split = p.dx.n_split;
             o.ptr = dx, o.ld = lddx, o.dtype = s->dtype, o.rows = h.rows;
-            if (launch_product(false, true, p.bl, t, o, st) != hipSuccess) return PSGD_E_HIP;
+            if (launch_product(true, p.dx.shape, t, o, st) != hipSuccess) return PSGD_E_HIP;
         }
         t.P = {xp, p.ldc, x_plane, (int)s->d};
         t.L = {h.D, p.ldv, h.d_plane, (int)s->vocab};
         t.K = rows, t.count_is_k = 1;
-        t.pairs = p.dw_pairs, t.n_pairs = p.n_dw_pairs, t.n_split = p.dw_split;
+        t.pairs = p.dw_pairs, t.n_pairs = p.n_dw_pairs, t.n_split = p.dw.n_split;
         o.rows = nullptr;
         if (p.sum) { o.ptr = ws + p.sum; o.ld = p.ldc; o.dtype = PSGD_F32; o.accumulate = piece > 0; }
         else { o.ptr = dw; o.ld = lddw; o.dtype = s->grad_dtype; o.accumulate = piece > 0 || accumulate; }
         o.skip_empty = o.accumulate;
-        if (launch_product(false, false, 256, t, o, st) != hipSuccess) return PSGD_E_HIP;
+        if (launch_product(false, p.dw.shape, t, o, st) != hipSuccess) return PSGD_E_HIP;
     }
     if (gradients && p.sum) {
         hipLaunchKernelGGL(head_round_kernel, dim3(2048), dim3(kThreads), 0, st, (const float*)(ws + p.sum), s->vocab, (int)s->d, p.ldc, (bf16_t*)dw, lddw, accumulate);

@@ -23,17 +23,17 @@ __device__ __forceinline__ void store_row(PSGD_GLOBAL float* p, const float (&v)
 }
 template <int N>
 __device__ __forceinline__ void store_row(PSGD_GLOBAL bf16_t* p, const float (&v)[N], int n, bool add) {
-    static_assert(N == 8, "pieces");
-    if (n >= 8) {
-        PSGD_GLOBAL bf16x8* q = reinterpret_cast<PSGD_GLOBAL bf16x8*>(p);
-        bf16x8 o, b;
+    typedef __attribute__((__vector_size__(N * sizeof(__bf16)))) __bf16 piece;
+    if (n >= N) {
+        PSGD_GLOBAL piece* q = reinterpret_cast<PSGD_GLOBAL piece*>(p);
+        piece o, b;
         if (add) b = *q;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) o[u] = (bf16_t)(add ? v[u] + (float)b[u] : v[u]);
+        for (int u = 0; u < N; ++u) o[u] = (bf16_t)(add ? v[u] + (float)b[u] : v[u]);
         *q = o;
     } else {
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < N; ++u)
             if (u < n) p[u] = (bf16_t)(add ? (float)p[u] + v[u] : v[u]);
     }
 }
@@ -41,23 +41,37 @@ __device__ __forceinline__ void store_row(PSGD_GLOBAL bf16_t* p, const float (&v
 // what a product kernel writes
 enum TileKind { TILE_PART = 0, TILE_F32 = 1, TILE_BF16 = 2 };
 
-template <bool PKC, bool LKC, int BL, int KIND>
-__global__ __launch_bounds__(tile_threads<BL>(), BL == 256 ? 1 : 2) void product_kernel(TileArgs t, TileOut o, int n_p, int n_l) {
+// contraction steps and rows of C that count
+struct TileSize { int K, nl, chunks; };
+__device__ inline TileSize tile_size(const TileArgs& t) {
+    TileSize s;
+    s.K = t.count_is_k ? counted(t, t.K) : t.K;
+    s.nl = t.count_is_k ? t.L.extent : counted(t, t.L.extent);
+    s.chunks = (s.K + kTileK - 1) / kTileK * t.n_pairs;
+    return s;
+}
+
+template <bool LKC, TileShape SHAPE, int KIND>
+__global__ __launch_bounds__(kTileThreads, 1) void product_kernel(TileArgs t, TileOut o) {
     extern __shared__ __align__(16) unsigned char smem[];
-    using T = Tile<PKC, LKC, BL>;
-    const TilePlace at = tile_place(blockIdx.x, n_p, n_l, t.n_split);
-    const int p0 = at.p * kTileP, l0 = at.l * BL;
-    const int K = t.count_is_k ? counted(t, t.K) : t.K, nl = t.count_is_k ? t.L.extent : counted(t, t.L.extent);
-    if (l0 >= nl || (K == 0 && o.skip_empty)) return;
+    using T = Tile<false, LKC, SHAPE>;
+    const TileSize size = tile_size(t);
+    const TileGrid grid = tile_grid<SHAPE>(t, size.nl, size.chunks);
+    const TilePlace at = tile_place(blockIdx.x, grid);
+    if (at.split < 0 || (size.K == 0 && o.skip_empty)) return;
+    const int p0 = at.p * T::BP, l0 = at.l * T::BL, nl = size.nl;
     T tile;
-    tile.run(t, p0, l0, nl, K, at.split, (PSGD_TLDS unsigned char*)smem);
-    tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, const auto& v) {
+    tile.run(t, p0, l0, nl, size.K, at.split, grid.n_split, (PSGD_TLDS unsigned char*)smem);
+    const float scale = KIND != TILE_PART && o.scale ? *o.scale : 1.f;
+    tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, auto& v) {
         const int l = l0 + row, c = p0 + col, n = t.P.extent - c;
         if (l >= nl || n <= 0) return;
         if constexpr (KIND == TILE_PART) {
-            PSGD_GLOBAL float* p = as_global(o.part) + ((int64_t)at.split * t.L.extent + l) * o.part_ld + c;
+            PSGD_GLOBAL float* p = as_global(o.part) + ((int64_t)at.split * nl + l) * o.part_ld + c;
             *reinterpret_cast<PSGD_GLOBAL floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
         } else {
+#pragma unroll
+            for (int u = 0; u < (KIND == TILE_BF16 ? 8 : 4); ++u) v[u] *= scale;
             const int64_t to = (o.rows ? o.rows[t.first + l] : l) * o.ld + c;
             if constexpr (KIND == TILE_F32) store_row(as_global((float*)o.ptr) + to, v, n, o.accumulate);
             else store_row(as_global((bf16_t*)o.ptr) + to, v, n, o.accumulate);
@@ -65,21 +79,29 @@ __global__ __launch_bounds__(tile_threads<BL>(), BL == 256 ? 1 : 2) void product
     });
 }
 
-// sum over the splits, in their order, of eight elements per thread
+// sum over the splits, in their order, of four elements per thread
+template <TileShape SHAPE>
 __global__ __launch_bounds__(kThreads) void split_sum_kernel(TileArgs t, TileOut o) {
-    const int K = t.count_is_k ? counted(t, t.K) : t.K, nl = t.count_is_k ? t.L.extent : counted(t, t.L.extent);
-    if (K == 0 && o.skip_empty) return;
-    const int pieces = (t.P.extent + 7) / 8;
-    const int64_t all = (int64_t)nl * pieces, layer = (int64_t)t.L.extent * o.part_ld;
+    const TileSize size = tile_size(t);
+    if (size.K == 0 && o.skip_empty) return;
+    const int nl = size.nl, n_split = tile_grid<SHAPE>(t, nl, size.chunks).n_split;
+    const float scale = o.scale ? *o.scale : 1.f;
+    const int pieces = (t.P.extent + 3) / 4;
+    const int64_t all = (int64_t)nl * pieces, layer = (int64_t)nl * o.part_ld;
     for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < all; e += (int64_t)gridDim.x * kThreads) {
-        const int l = (int)(e / pieces), c = 8 * (int)(e - (int64_t)l * pieces);
+        const int l = (int)(e / pieces), c = 4 * (int)(e - (int64_t)l * pieces);
         const PSGD_GLOBAL float* p = as_global(o.part) + l * o.part_ld + c;
-        floatx4 s = {0.f, 0.f, 0.f, 0.f}, r = s;
-        for (int k = 0; k < t.n_split; ++k) {
-            s += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer);
-            r += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer + 4);
+        floatx4 s = {0.f, 0.f, 0.f, 0.f};
+        int k = 0;
+        for (; k + 8 <= n_split; k += 8) {        // eight loads in flight
+            floatx4 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + (k + u) * layer);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += x[u];
         }
-        const float v[8] = {s[0], s[1], s[2], s[3], r[0], r[1], r[2], r[3]};
+        for (; k < n_split; ++k) s += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer);
+        const float v[4] = {s[0] * scale, s[1] * scale, s[2] * scale, s[3] * scale};
         const int64_t row = o.rows ? o.rows[t.first + l] : l;
         if (o.dtype == PSGD_F32) store_row(as_global((float*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
         else store_row(as_global((bf16_t*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
@@ -109,55 +131,72 @@ __global__ __launch_bounds__(kThreads) void planes_kernel(const T* src, int64_t 
     }
 }
 
-constexpr int kUnits = 256;     // compute units; one workgroup of a 256-row tile fills one
+constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel fills one
 
-int tile_rows(int64_t extent_l) { return extent_l <= 64 ? 64 : extent_l <= 128 ? 128 : 256; }
-
-int tile_splits(int64_t n_p, int64_t n_l, int64_t chunks, int64_t elems) {
-    (void)elems;
-    const int64_t tiles = n_p * n_l;
-    if (tiles >= kUnits || tiles == 0) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({kUnits / tiles, chunks / 4, 64}));
+// Shape and splits by an estimate in microseconds.  A workgroup takes A before and after its chunks and C per chunk (256 x 256: 11 and 1.65, which
+// is the matrix cores' rate; 128 x 128: 5 and 0.57; 128 x 64: 4.5 and 0.45, the smaller ones' latency), workgroups run 256 at a time; a split
+// contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for each that a thread adds up.  Weight
+// gradients tokens x out x in, measured with 256 x 256 / 128 x 128 / 128 x 64, each with its best number of splits, in us:
+// 128 x 800 x 800 18.5 / 13.9 / 14.4;  1000 x 2048 x 2048 34.7 / 22.7 / 29.5;  9001 x 256 x 1032 32.8 / 27.7 / 32.4;  4096 x 512 x 512
+// 29.5 / 20.8 / 19.7;  8192 x 2048 x 2048 87.3 / 89.9 / 134.7;  2000 x 4096 x 4096 73.3 / 96.7 / 147.8;  64 x 4096 x 4096 19.8 / 26.2 / 35.4.
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split) {
+    static const double A[3] = {11, 5, 4.5}, C[3] = {1.65, 0.57, 0.45};
+    TilePlan best = {TILE_256, 1};
+    double least = 1e300;
+    for (TileShape shape : {TILE_256, TILE_128, TILE_THIN}) {
+        const int64_t tiles = (extent_p + tile_p(shape) - 1) / tile_p(shape) * ((extent_l + tile_l(shape) - 1) / tile_l(shape));
+        const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
+        for (int64_t want : {(int64_t)1, fill / 4, fill / 2, fill, 2 * fill}) {
+            if (want < 1 || (want > 1 && (!may_split || want > 64 || want > chunks))) continue;
+            const int64_t share = (chunks + want - 1) / want, split = share > 0 ? (chunks + share - 1) / share : 1;
+            double us = (double)((tiles * split + kUnits - 1) / kUnits) * (A[shape] + share * C[shape]);
+            if (split > 1) us += 4 + 0.08 * split + split * (double)extent_p * (double)extent_l * 8e-6 / 8;
+            if (us < least) least = us, best = {shape, (int)split};
+        }
+    }
+    return best;
 }
 
-size_t tile_part_bytes(int extent_p, int extent_l, int n_split) {
-    return n_split > 1 ? up256((size_t)n_split * extent_l * ((extent_p + 7) / 8 * 8) * sizeof(float)) : 0;
+size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan) {
+    // (whole tiles: where fewer rows count there are more parts of as many tiles in all)
+    const int64_t rows = (extent_l + tile_l(plan.shape) - 1) / tile_l(plan.shape) * tile_l(plan.shape);
+    return plan.n_split > 1 ? up256((size_t)plan.n_split * rows * up8(extent_p) * sizeof(float)) : 0;
 }
 
-template <bool PKC, bool LKC, int BL, int KIND>
-static hipError_t launch_kind(const TileArgs& t, const TileOut& o, int n_p, int n_l, hipStream_t st) {
-    auto kfn = product_kernel<PKC, LKC, BL, KIND>;
-    constexpr int lds = Tile<PKC, LKC, BL>::LDS_BYTES;
+template <bool LKC, TileShape SHAPE, int KIND>
+static hipError_t launch_kind(const TileArgs& t, const TileOut& o, hipStream_t st) {
+    auto kfn = product_kernel<LKC, SHAPE, KIND>;
+    constexpr int lds = Tile<false, LKC, SHAPE>::LDS_BYTES;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kfn, dim3(n_p * n_l * t.n_split), dim3(tile_threads<BL>()), lds, st, t, o, n_p, n_l);
+    hipLaunchKernelGGL(kfn, dim3(t.blocks), dim3(kTileThreads), lds, st, t, o);
     return hipGetLastError();
 }
-template <bool PKC, bool LKC, int BL>
-static hipError_t launch_tiles(const TileArgs& t, const TileOut& o, int n_p, int n_l, hipStream_t st) {
-    if (o.part) return launch_kind<PKC, LKC, BL, TILE_PART>(t, o, n_p, n_l, st);
-    if (o.dtype == PSGD_F32) return launch_kind<PKC, LKC, BL, TILE_F32>(t, o, n_p, n_l, st);
-    return launch_kind<PKC, LKC, BL, TILE_BF16>(t, o, n_p, n_l, st);
+template <bool LKC, TileShape SHAPE>
+static hipError_t launch_shape(TileArgs t, const TileOut& o, hipStream_t st) {
+    const int64_t n_p = (t.P.extent + tile_p(SHAPE) - 1) / tile_p(SHAPE), n_l = (t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE);
+    if (n_p * n_l * t.n_split > INT32_MAX) return hipErrorInvalidValue;
+    t.blocks = (int)(n_p * n_l * t.n_split);
+    if (!o.part) return o.dtype == PSGD_F32 ? launch_kind<LKC, SHAPE, TILE_F32>(t, o, st) : launch_kind<LKC, SHAPE, TILE_BF16>(t, o, st);
+    hipError_t e = launch_kind<LKC, SHAPE, TILE_PART>(t, o, st);
+    if (e != hipSuccess) return e;
+    const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 3) / 4);
+    hipLaunchKernelGGL(split_sum_kernel<SHAPE>, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
+    return hipGetLastError();
 }
 
-hipError_t launch_product(bool p_contiguous, bool l_contiguous, int bl, const TileArgs& t, const TileOut& out, hipStream_t st) {
+hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& out, hipStream_t st) {
     TileOut o = out;
     if (t.n_split == 1) o.part = nullptr;
-    o.part_ld = (t.P.extent + 7) / 8 * 8;
-    const int n_p = (t.P.extent + kTileP - 1) / kTileP, n_l = (t.L.extent + bl - 1) / bl;
-    if (n_p * (int64_t)n_l * t.n_split > INT32_MAX) return hipErrorInvalidValue;
-    hipError_t e = hipErrorInvalidValue;
-    if (!p_contiguous && l_contiguous) {
-        if (bl == 256) e = launch_tiles<false, true, 256>(t, o, n_p, n_l, st);
-        else if (bl == 128) e = launch_tiles<false, true, 128>(t, o, n_p, n_l, st);
-        else if (bl == 64) e = launch_tiles<false, true, 64>(t, o, n_p, n_l, st);
-    } else if (!p_contiguous && !l_contiguous && bl == 256) {
-        e = launch_tiles<false, false, 256>(t, o, n_p, n_l, st);
+    o.part_ld = up8(t.P.extent);
+    if (l_contiguous) {
+        if (shape == TILE_256) return launch_shape<true, TILE_256>(t, o, st);
+        if (shape == TILE_128) return launch_shape<true, TILE_128>(t, o, st);
+        return launch_shape<true, TILE_THIN>(t, o, st);
     }
-    if (e != hipSuccess || t.n_split == 1) return e;
-    const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 7) / 8);
-    hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
-    return hipGetLastError();
+    if (shape == TILE_256) return launch_shape<false, TILE_256>(t, o, st);
+    if (shape == TILE_128) return launch_shape<false, TILE_128>(t, o, st);
+    return launch_shape<false, TILE_THIN>(t, o, st);
 }
 
 hipError_t launch_planes(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bf16_t* dst, int planes, hipStream_t st) {

@@ -18,7 +18,6 @@ namespace psgd {
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short shortx4;
 typedef __attribute__((__vector_size__(8 * sizeof(short)))) short shortx8;
 
-template <int BL> constexpr int tile_threads() { return BL == 256 ? 256 : 512; }
 constexpr unsigned kOutside = 0x80000000u;      // byte offset beyond every descriptor's range
 
 __device__ inline int counted(const TileArgs& a, int upper) {
@@ -26,11 +25,24 @@ __device__ inline int counted(const TileArgs& a, int upper) {
     return __builtin_amdgcn_readfirstlane(max(0, min(upper, *a.count - a.first)));
 }
 
-// Which tile a workgroup takes.  Consecutive workgroups go to consecutive XCDs; each XCD gets a run of consecutive tiles (its L2 then
-// holds operands that its workgroups share), and a run goes through 8 tiles along L before the next along P.
+// Tiles and parts of the contraction of a product of nl rows that count: where that is fewer than the launch was planned for, its workgroups
+// go to more parts.  chunks: of the whole contraction.
+struct TileGrid { int n_p, n_l, n_split; };
+template <TileShape SHAPE>
+__device__ inline TileGrid tile_grid(const TileArgs& t, int nl, int chunks) {
+    TileGrid g;
+    g.n_p = (t.P.extent + tile_p(SHAPE) - 1) / tile_p(SHAPE);
+    g.n_l = (nl + tile_l(SHAPE) - 1) / tile_l(SHAPE);
+    g.n_split = t.n_split == 1 || nl == 0 ? 1 : max(1, min(chunks, t.blocks / (g.n_p * g.n_l)));
+    return g;
+}
+
+// Which tile a workgroup takes (split < 0: none).  Consecutive workgroups go to consecutive XCDs; each XCD gets a run of consecutive tiles
+// (its L2 then holds operands that its workgroups share), and a run goes through 8 tiles along L before the next along P.
 struct TilePlace { int p, l, split; };
-__device__ inline TilePlace tile_place(int id, int n_p, int n_l, int n_split) {
-    const int n = n_p * n_l * n_split, q = n >> 3, r = n & 7, x = id & 7;
+__device__ inline TilePlace tile_place(int id, const TileGrid& g) {
+    const int n_p = g.n_p, n_l = g.n_l, n = n_p * n_l * g.n_split, q = n >> 3, r = n & 7, x = id & 7;
+    if (id >= n) return {0, 0, -1};
     int t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (id >> 3);
     TilePlace at;
     at.split = t / (n_p * n_l);
@@ -53,9 +65,10 @@ struct TileSide {
     static_assert(LOADS >= 1 && LOADS * NW * 1024 == BYTES, "chunk");
 
     // K-contiguous: rows of 2 BK bytes, piece c of row r at place c ^ swizzle(r): sixteen rows' reads of one piece cover all 64
-    // banks.  K-strided: rows of 2 E bytes, 64-byte piece c of row k at place c ^ (k & 3): the four rows that a transposing read
+    // banks.  K-strided: rows of 2 E bytes, 64-byte piece c of row k at place c ^ turn(k): the four rows that a transposing read
     // takes lie in different banks.
     static constexpr int PIECES = BK / 8;       // of 16 bytes in a K-contiguous row
+    __device__ static int turn(int k) { return E == 64 ? (k >> 1) & 1 : k & 3; }
     __device__ static int swizzle(int r) { return BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; }
     unsigned off[LOADS];
     int kpiece;          // K-contiguous: first step of this lane's pieces, K-strided: unused
@@ -70,7 +83,7 @@ struct TileSide {
                 off[i] = start + row < extent ? (unsigned)(((int64_t)row * o.ld + 8 * piece) * 2) : kOutside;
             } else {
                 constexpr int LANES = E / 8, ROWS = 64 / LANES;     // lanes per row, rows per load
-                const int k = block * ROWS + lane / LANES, place = lane % LANES, col = 8 * (place ^ ((k & 3) << 2));
+                const int k = block * ROWS + lane / LANES, place = lane % LANES, col = 8 * (place ^ (turn(k) << 2));
                 off[i] = start + col < extent ? (unsigned)(((int64_t)k * o.ld + col) * 2) : kOutside;
             }
         }
@@ -113,12 +126,12 @@ struct TileFragment {
         if constexpr (KC) {
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk)
-                base[kk] = (unsigned)((e0 + li) * 2 * BK + (((2 * kk + lg) ^ TileSide<KC, E, BK, 8>::swizzle(li)) << 4));
+                base[kk] = (unsigned)((e0 + li) * 2 * BK + (((2 * kk + lg) ^ TileSide<KC, E, BK, 4>::swizzle(li)) << 4));
         } else {
             const int row = 8 * lg + ((lane & 15) >> 2);
 #pragma unroll
             for (int f = 0; f < 4; ++f)
-                base[f] = (unsigned)(row * 2 * E + (((2 * (e0 + 32 * f)) ^ ((row & 3) << 6)) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3)));
+                base[f] = (unsigned)(row * 2 * E + (((2 * (e0 + 32 * f)) ^ (TileSide<KC, E, BK, 4>::turn(row) << 6)) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3)));
         }
     }
     template <int KK, int F>
@@ -135,31 +148,31 @@ struct TileFragment {
     }
 };
 
-// shapes: waves along P and L, contraction steps per chunk, chunks in LDS
-template <int BL> struct TileShape;
-template <> struct TileShape<256> { static constexpr int WP = 2, WL = 2, BK = kTileK, STAGES = 2; };
-template <> struct TileShape<128> { static constexpr int WP = 4, WL = 2, BK = kTileK, STAGES = 3; };
-template <> struct TileShape<64> { static constexpr int WP = 4, WL = 2, BK = kTileK, STAGES = 3; };
+// Waves along P and L, chunks in LDS.  All have four waves, one per SIMD, and LDS for one workgroup per compute unit.
+template <TileShape SHAPE> struct TileWaves;
+template <> struct TileWaves<TILE_256> { static constexpr int WP = 2, WL = 2, STAGES = 0; };
+template <> struct TileWaves<TILE_128> { static constexpr int WP = 2, WL = 2, STAGES = 5; };
+template <> struct TileWaves<TILE_THIN> { static constexpr int WP = 2, WL = 2, STAGES = 6; };
 
-template <bool PKC, bool LKC, int BL>
+template <bool PKC, bool LKC, TileShape SHAPE>
 struct Tile {
-    using S = TileShape<BL>;
-    static constexpr int WP = S::WP, WL = S::WL, NW = WP * WL, BK = S::BK, STAGES = S::STAGES;
-    static constexpr bool FULL = BL == 256;      // the large tile: one wave per SIMD
-    static constexpr int FP = kTileP / WP / 32, FL = BL / WL / 32;      // fragments per wave
-    using SideP = TileSide<PKC, kTileP, BK, NW>;
+    using S = TileWaves<SHAPE>;
+    static constexpr int BP = tile_p(SHAPE), BL = tile_l(SHAPE), WP = S::WP, WL = S::WL, NW = WP * WL, BK = kTileK, STAGES = S::STAGES;
+    static constexpr bool FULL = SHAPE == TILE_256;
+    static constexpr int FP = BP / WP / 32, FL = BL / WL / 32;      // fragments per wave
+    using SideP = TileSide<PKC, BP, BK, NW>;
     using SideL = TileSide<LKC, BL, BK, NW>;
     static constexpr int STAGE_BYTES = SideP::BYTES + SideL::BYTES;
     static constexpr int LDS_BYTES = FULL ? 5 * SideP::BYTES : STAGES * STAGE_BYTES;
     static constexpr int LOADS = SideP::LOADS + SideL::LOADS;
-    static constexpr int THREADS = NW * 64;
-    static_assert(FP >= 1 && FL >= 1 && FP <= 4 && FL <= 4 && BK == 64 && THREADS == tile_threads<BL>(), "waves");
+    static_assert(FP >= 1 && FL >= 1 && FP <= 4 && FL <= 4 && BK == 64 && NW * 64 == kTileThreads && LDS_BYTES <= 160 * 1024, "waves");
+    static_assert((STAGES - 2) * LOADS <= 63, "the wait counter's range");
 
     floatx16 acc[FP][FL];
     int wp, wl, lane;
 
     template <int KK>
-    __device__ __forceinline__ void read(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, kTileP, BK>& fp,
+    __device__ __forceinline__ void read(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, BP, BK>& fp,
                                          const TileFragment<LKC, BL, BK>& fl, bf16x8 (&a)[FP], bf16x8 (&b)[FL]) {
         a[0] = fp.template read<KK, 0>(chunk);
         if constexpr (FP > 1) a[1] = fp.template read<KK, 1>(chunk);
@@ -171,7 +184,7 @@ struct Tile {
         if constexpr (FL > 3) b[3] = fl.template read<KK, 3>(chunk + SideP::BYTES);
     }
     template <int KK>
-    __device__ __forceinline__ void read_ab(const PSGD_TLDS unsigned char* cp, const PSGD_TLDS unsigned char* cl, const TileFragment<PKC, kTileP, BK>& fp,
+    __device__ __forceinline__ void read_ab(const PSGD_TLDS unsigned char* cp, const PSGD_TLDS unsigned char* cl, const TileFragment<PKC, BP, BK>& fp,
                                             const TileFragment<LKC, BL, BK>& fl, bf16x8 (&a)[FP], bf16x8 (&b)[FL]) {
         a[0] = fp.template read<KK, 0>(cp);
         if constexpr (FP > 1) a[1] = fp.template read<KK, 1>(cp);
@@ -189,7 +202,7 @@ struct Tile {
             for (int j = 0; j < FL; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
     }
     template <int KK>
-    __device__ __forceinline__ void step(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, kTileP, BK>& fp, const TileFragment<LKC, BL, BK>& fl) {
+    __device__ __forceinline__ void step(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl) {
         bf16x8 a[FP], b[FL];
         read<KK>(chunk, fp, fl, a, b);
         multiply(a, b);
@@ -199,7 +212,7 @@ struct Tile {
     // of a side's chunk.  Loads and reads go between the products, two products apart.
     template <int KK, int H, class Side>
     __device__ __forceinline__ void round(const bf16x8 (&a)[FP], const bf16x8 (&b)[FL], bf16x8 (&an)[FP], bf16x8 (&bn)[FL],
-                                          const PSGD_TLDS unsigned char* cp, const PSGD_TLDS unsigned char* cl, const TileFragment<PKC, kTileP, BK>& fp,
+                                          const PSGD_TLDS unsigned char* cp, const PSGD_TLDS unsigned char* cl, const TileFragment<PKC, BP, BK>& fp,
                                           const TileFragment<LKC, BL, BK>& fl, const Side& side, const typename Side::Source& src,
                                           PSGD_TLDS unsigned char* dst, int wv) {
         an[0] = fp.template read<KK, 0>(cp);
@@ -237,7 +250,7 @@ struct Tile {
     // with both places of the chunk, and its loads of the next chunk have arrived.  After it L's part of the chunk after the next goes to
     // one of the places, and then P's of the chunk after that.  Past the end the loads bring zeros, so that no wait depends on where one is.
     __device__ __forceinline__ void run_full(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
-                                             const SideL& sl, const TileFragment<PKC, kTileP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
+                                             const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
                                              PSGD_TLDS unsigned char* lds) {
         constexpr int PLACE = SideP::BYTES;
         static_assert(SideP::BYTES == SideL::BYTES && SideP::LOADS == 8 && SideL::LOADS == 8, "places");
@@ -293,10 +306,10 @@ struct Tile {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     }
 
-    // acc = the tile at (p0, l0), part `split` of the contraction over K steps; nl: rows of C there are.  MINUS_INF: what lies beyond P's
+    // acc = the tile at (p0, l0), part `split` of n_split of the contraction over K steps; nl: rows of C there are.  MINUS_INF: what lies beyond P's
     // extent comes out as -inf, where sums begin that only get zeros added
     template <bool MINUS_INF = false>
-    __device__ void run(const TileArgs& t, int p0, int l0, int nl, int K, int split, PSGD_TLDS unsigned char* lds) {
+    __device__ void run(const TileArgs& t, int p0, int l0, int nl, int K, int split, int n_split, PSGD_TLDS unsigned char* lds) {
         lane = threadIdx.x & 63;
         const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wp = wv % WP;
@@ -314,37 +327,37 @@ struct Tile {
         SideL sl;
         sp.init(t.P, p0, t.P.extent, wv, lane);
         sl.init(t.L, l0, nl, wv, lane);
-        TileFragment<PKC, kTileP, BK> fp;
+        TileFragment<PKC, BP, BK> fp;
         TileFragment<LKC, BL, BK> fl;
         fp.init(wp * FP * 32, lane);
         fl.init(wl * FL * 32, lane);
 
-        const int per = (K + BK - 1) / BK, all = per * t.n_pairs, share = (all + t.n_split - 1) / t.n_split;
+        const int per = (K + BK - 1) / BK, all = per * t.n_pairs, share = (all + n_split - 1) / n_split;
         const int n0 = min(all, split * share), n = min(all, n0 + share) - n0;
         if (n <= 0) return;
         if constexpr (FULL) {
             run_full(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         } else {
-            int pair = n0 / per, kc = n0 - pair * per;      // of the next chunk to load
-            int into = 0;
+            // A ring of chunks; past the end the loads bring zeros, so that no wait depends on where one is.
+            int left = n, pair = n0 / per, kc = n0 - pair * per, into = 0, from = 0;     // of the next chunk to load
             auto issue = [&]() {
                 const unsigned which = t.pairs >> (4 * pair);
                 PSGD_TLDS unsigned char* dst = lds + into * STAGE_BYTES;
-                sp.load_all(SideP::source(t.P, which & 3, p0, kc * BK, K, true), dst, wv);
-                sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, true), dst + SideP::BYTES, wv);
-                asm volatile("" ::: "memory");
-                if (++kc == per) { kc = 0; ++pair; }
+                sp.load_all(SideP::source(t.P, which & 3, p0, kc * BK, K, left > 0), dst, wv);
+                sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, left > 0), dst + SideP::BYTES, wv);
+                --left;
+                const bool wrap = ++kc == per;
+                kc = wrap ? 0 : kc;
+                pair = min(pair + (wrap ? 1 : 0), 7);
                 into = into + 1 == STAGES ? 0 : into + 1;
             };
-            int issued = 0, from = 0;
-            for (; issued < STAGES - 1 && issued < n; ++issued) issue();
+            for (int i = 0; i < STAGES - 1; ++i) issue();
             for (int it = 0; it < n; ++it) {
                 // this chunk has arrived, for every wave, and nobody reads the buffer of the one before any more
-                if (it + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * LOADS) : "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
-                if (issued < n) { issue(); ++issued; }
+                issue();
                 const PSGD_TLDS unsigned char* chunk = lds + from * STAGE_BYTES;
                 step<0>(chunk, fp, fl);
                 step<1>(chunk, fp, fl);
@@ -352,6 +365,7 @@ struct Tile {
                 step<3>(chunk, fp, fl);
                 from = from + 1 == STAGES ? 0 : from + 1;
             }
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         }
     }
 

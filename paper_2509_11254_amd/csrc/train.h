@@ -6,8 +6,14 @@
 
 namespace psgd {
 
-constexpr int kTileP = 256;     // elements of a tile of C along P
 constexpr int kTileK = 64;      // contraction steps per chunk
+constexpr int kTileThreads = 256;
+
+// Elements of a tile of C along P and L: 256 x 256 where there are enough of them; 128 x 128 where smaller tiles fill the card better;
+// 128 x 64 for few rows
+enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2 };
+constexpr int tile_p(TileShape s) { return s == TILE_256 ? 256 : 128; }
+constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_128 ? 128 : 64; }
 
 struct TileOperand {
     const bf16_t* ptr;
@@ -26,7 +32,8 @@ struct TileArgs {
     int count_is_k;     // ... as contraction steps (1) or as rows of C (0)
     unsigned pairs;
     int n_pairs;
-    int n_split;        // parts of the contraction, each a workgroup of its own
+    int n_split;        // parts of the contraction, each a workgroup of its own; more where fewer rows count (tile_grid)
+    int blocks;         // workgroups of the launch (set by it)
 };
 constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048, kPairs22 = 0x014;
 // three planes each, six products: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
@@ -40,15 +47,17 @@ struct TileOut {
     int accumulate;     // add to what is there
     int skip_empty;     // write nothing where no token counts (a later piece of an accumulated product)
     const int* rows;    // nullable
-    float* part;        // n_split > 1: partial sums [split][rows of C][part_ld]
+    const float* scale; // nullable: device word that C is multiplied by
+    float* part;        // n_split > 1: partial sums [split][rows of C that count][part_ld]
     int64_t part_ld;
 };
 
-int tile_splits(int64_t n_p, int64_t n_l, int64_t chunks, int64_t elems);
-size_t tile_part_bytes(int extent_p, int extent_l, int n_split);
-int tile_rows(int64_t extent_l);
-// C = L P^T over the operands' orientations: K-contiguous or K-strided
-hipError_t launch_product(bool p_contiguous, bool l_contiguous, int bl, const TileArgs& t, const TileOut& o, hipStream_t st);
+// shape and number of parts of the contraction of a product: extents of C, chunks of the contraction (of all pairs of planes)
+struct TilePlan { TileShape shape; int n_split; };
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split);
+size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan);
+// C = L P^T over the operands' orientations: P K-strided, L K-contiguous or K-strided
+hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& o, hipStream_t st);
 // rows x cols (ld) of fp32 or bf16 to `planes` bf16 planes [rows][round_up(cols, 8)], zeros beyond cols
 hipError_t launch_planes(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bf16_t* dst, int planes, hipStream_t st);
 
