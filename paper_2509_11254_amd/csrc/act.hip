@@ -5,221 +5,384 @@
 // is not finite and comes back as NaN.  With a power of two neither the division nor the way back rounds, and a value has at most
 // seven significant bits: it is a bf16 number, so that matrix products take it as it is.
 //
-// A thread has 16 columns, two threads a group: one to four 16-byte loads, a 16-byte store of codes, one exchange for the
-// maximum.  All kernels here read and write each byte once and are bound by HBM.
+// A thread has 16 bytes of an activation at a time, 8 columns in bf16 and 4 in fp32, so that every load and store of a wavefront is one
+// run of 1 KB (with two stores of 16 bytes side by side, each leaves half of every line to the other, and the non-temporal hint costs 40 %); four or eight threads next to each other have a group.  Each byte is read and written once, and HBM would bound all of it, were
+// it not for the arithmetic: at 5 TB/s there are 24 vector instructions per element.  So the common case has few: rounding to a
+// whole number is the addition of 1.5 * 2^23 (whose last bit is 1), the codes are the sums' low bytes; a code becomes a value by the
+// conversion of an unsigned byte and one multiply-add; what is not finite or beyond the largest scale is sought once per group, and sends the
+// wavefront the slow way.  16384 x 11008 in bf16, stored and restored: 201 -> 171 us, 6.4 TB/s; gated unit of 8192 x 11008, both ways: 293 -> 229, 6.4 TB/s.
 #include "tile_dev.h"
 
 namespace psgd {
 
 constexpr int kGroup = 32;
-typedef signed char codex16 __attribute__((ext_vector_type(16)));
+constexpr int kActItems = 2;        // pieces per thread, all of whose loads are sent off first (1: 225 us, 4: 202, where 2 take 200)
+// From this many bytes of activations in a call on they are loaded and stored with the non-temporal hint (16384 x 11008 in bf16 and back 200 -> 180 us,
+// gated unit of 8192 x 11008 forward and backward 260 -> 228); what is smaller, the next kernel may find in the caches.  Codes never have it (188, 240).
+constexpr int64_t kActStream = 96 << 20;
+template <bool STREAM, class V> __device__ __forceinline__ V ld_act(const PSGD_GLOBAL V* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p); else return *p;
+}
+template <bool STREAM, class V> __device__ __forceinline__ void st_act(PSGD_GLOBAL V* p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p); else *p = v;
+}
 
-// item of 16 columns: row and first column.  `per` items per row.
+template <class T> constexpr int kPiece = 16 / (int)sizeof(T);      // columns of a piece
+constexpr unsigned kInfBits = 0x7f800000u;
+constexpr unsigned kTopBits = 0x7f7e0000u;      // 127 * 2^121, the largest number that the largest scale holds
+constexpr float kWhole = 12582912.f;            // 1.5 * 2^23
+
+// piece i of this thread: row and first column.  `per`: pieces of a row, of whole groups; inv_per its reciprocal.
+struct ActRows { int64_t rows; int cols, per; double inv_per; };
 struct ActPlace { int64_t row; int col; bool in; };
-__device__ __forceinline__ ActPlace act_place(int64_t rows, int per) {
-    const int64_t first = (int64_t)blockIdx.x * kThreads;
-    const int64_t row0 = first / per;
-    const unsigned at = (unsigned)(first - row0 * per) + threadIdx.x, down = at / (unsigned)per;
+template <int N>
+__device__ __forceinline__ ActPlace act_place(const ActRows& r, int i) {
+    const int64_t first = ((int64_t)blockIdx.x * kActItems + i) * kThreads;
+    int64_t row0 = (int64_t)((double)first * r.inv_per);        // off by one at most
+    int64_t rest = first - row0 * r.per;
+    if (rest < 0) { --row0; rest += r.per; }
+    if (rest >= r.per) { ++row0; rest -= r.per; }
+    unsigned at = (unsigned)rest + threadIdx.x, down = 0;
+    if (r.per >= kThreads) {
+        if (at >= (unsigned)r.per) { at -= r.per; down = 1; }
+    } else {
+        down = at / (unsigned)r.per;
+        at -= down * r.per;
+    }
     ActPlace p;
     p.row = row0 + down;
-    p.col = 16 * (int)(at - down * per);
-    p.in = p.row < rows;
+    p.col = N * (int)at;
+    p.in = p.row < r.rows && p.col < r.cols;
     return p;
 }
 
-// 16 elements from column c on of a row; zeros beyond cols.  Whole 16-byte pieces that begin inside the row are read.
-__device__ __forceinline__ void load16(const PSGD_GLOBAL bf16_t* p, int c, int cols, float (&x)[16]) {
+// A piece as it is stored; zeros beyond cols.  A piece that begins inside the row is read as a whole.
+template <bool STREAM, class T>
+__device__ __forceinline__ uintx4 load_raw(const T* x, int64_t ld, const ActPlace& p) {
+    uintx4 w = {0u, 0u, 0u, 0u};
+    if (p.in) w = ld_act<STREAM>(reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global(x) + p.row * ld + p.col));
+    return w;
+}
+template <class T>
+__device__ __forceinline__ void clear_beyond(uintx4& w, const ActPlace& p, int cols) {
+    if (p.col + kPiece<T> > cols) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        bf16x8 v;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = (bf16_t)0.f;
-        if (c + 8 * h < cols) v = *reinterpret_cast<const PSGD_GLOBAL bf16x8*>(p + c + 8 * h);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[8 * h + u] = c + 8 * h + u < cols ? (float)v[u] : 0.f;
+        for (int u = 0; u < 4; ++u) {
+            if constexpr (sizeof(T) == 4) w[u] = p.col + u < cols ? w[u] : 0u;
+            else w[u] &= (p.col + 2 * u < cols ? 0xffffu : 0u) | (p.col + 2 * u + 1 < cols ? 0xffff0000u : 0u);
+        }
     }
 }
-__device__ __forceinline__ void load16(const PSGD_GLOBAL float* p, int c, int cols, float (&x)[16]) {
+template <class T, int N = kPiece<T>>
+__device__ __forceinline__ void widen(const uintx4& w, float (&v)[N]) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        floatx4 v = {0.f, 0.f, 0.f, 0.f};
-        if (c + 4 * h < cols) v = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + c + 4 * h);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x[4 * h + u] = c + 4 * h + u < cols ? v[u] : 0.f;
+    for (int u = 0; u < 4; ++u) {
+        if constexpr (N == 4) v[u] = __uint_as_float(w[u]);
+        else { v[2 * u] = __uint_as_float(w[u] << 16); v[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
     }
 }
 // nothing beyond cols is written
-__device__ __forceinline__ void store16(PSGD_GLOBAL bf16_t* p, int c, int cols, const float (&x)[16]) {
+template <bool STREAM, class T, int N = kPiece<T>>
+__device__ __forceinline__ void store_piece(T* x, int64_t ld, const ActPlace& p, int cols, const float (&v)[N]) {
+    if (!p.in) return;
+    PSGD_GLOBAL T* at = as_global(x) + p.row * ld + p.col;
+    if (p.col + N <= cols) {
+        typedef __attribute__((__vector_size__(16))) T piece;
+        piece q;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (c + 8 * h + 8 <= cols) {
-            bf16x8 v;
+        for (int u = 0; u < N; ++u) q[u] = (T)v[u];
+        st_act<STREAM>(reinterpret_cast<PSGD_GLOBAL uintx4*>(at), __builtin_bit_cast(uintx4, q));
+    } else {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = (bf16_t)x[8 * h + u];
-            *reinterpret_cast<PSGD_GLOBAL bf16x8*>(p + c + 8 * h) = v;
-        } else {
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (c + 8 * h + u < cols) p[c + 8 * h + u] = (bf16_t)x[8 * h + u];
-        }
-    }
-}
-__device__ __forceinline__ void store16(PSGD_GLOBAL float* p, int c, int cols, const float (&x)[16]) {
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        if (c + 4 * h + 4 <= cols) {
-            const floatx4 v = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-            *reinterpret_cast<PSGD_GLOBAL floatx4*>(p + c + 4 * h) = v;
-        } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (c + 4 * h + u < cols) p[c + 4 * h + u] = x[4 * h + u];
-        }
+        for (int u = 0; u < N; ++u)
+            if (p.col + u < cols) at[u] = (T)v[u];
     }
 }
 
-// codes of this thread's half of a group, and the group's scale byte (the other half is lane ^ 1's: all lanes come here)
-__device__ __forceinline__ int quantise16(const float (&x)[16], codex16& code) {
-    unsigned most = 0;
+// the largest magnitude of a group as fp32 bits, what is not finite included (all lanes of the group come here)
+template <class T>
+__device__ __forceinline__ unsigned group_most(const uintx4& w) {
+    typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+    unsigned most;
+    if constexpr (sizeof(T) == 4) {
+        most = max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
+    } else {
+        ushortx2 m = __builtin_bit_cast(ushortx2, w[0] & 0x7fff7fffu);
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        const unsigned a = __float_as_uint(x[u]) & 0x7fffffffu;
-        most = max(most, a < 0x7f800000u ? a : 0u);
+        for (int u = 1; u < 4; ++u) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushortx2, w[u] & 0x7fff7fffu));
+        most = (unsigned)max(m[0], m[1]) << 16;
     }
-    most = max(most, (unsigned)__shfl_xor((int)most, 1));
-    // 127 * 2^e reaches 1.f * 2^E for e = E - 6 where 1.f <= 127 / 64, else for E - 5
-    const int e = (int)(most >> 23) - 6 + ((most & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-    const int scale = most == 0 ? 0 : min(max(e, 1), 248);
+    // lanes ^ 1, ^ 2 and, for eight lanes to a group, the other four
+    most = max(most, (unsigned)__builtin_amdgcn_mov_dpp((int)most, 0xB1, 0xf, 0xf, true));
+    most = max(most, (unsigned)__builtin_amdgcn_mov_dpp((int)most, 0x4E, 0xf, 0xf, true));
+    if constexpr (sizeof(T) == 4) most = max(most, (unsigned)__builtin_amdgcn_mov_dpp((int)most, 0x141, 0xf, 0xf, true));
+    return most;
+}
+// the scale byte for a largest magnitude that is finite: 127 * 2^e reaches 1.f * 2^E for e = E - 6 where 1.f <= 127 / 64, else for E - 5
+__device__ __forceinline__ int scale_byte(unsigned most) {
+    const int e = (int)((most + 0x1ffffu) >> 23) - 6;          // (a fraction above 0x7e0000 carries)
+    return most == 0 ? 0 : min(max(e, 1), 248);
+}
+
+// four codes: the low bytes of four sums
+__device__ __forceinline__ unsigned low_bytes(float a, float b, float c, float d) {
+    const unsigned ab = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0c0c0400u);
+    const unsigned cd = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x0c0c0400u);
+    return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+}
+
+// codes of this thread's part of a group (kPiece / 4 words) and the group's scale byte; all lanes come here
+template <class T, int N = kPiece<T>>
+__device__ __forceinline__ int quantise(const uintx4& w, const float (&x)[N], unsigned (&code)[N / 4]) {
+    unsigned most = group_most<T>(w);
+    int scale = scale_byte(most);
     const float inverse = __uint_as_float((unsigned)(254 - scale) << 23);
+    if (!__any(most > kTopBits)) {
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
-        const bool finite = (__float_as_uint(x[u]) & 0x7f800000u) != 0x7f800000u;
-        const int q = (int)rintf(fminf(fmaxf(x[u] * inverse, -127.f), 127.f));
-        code[u] = (signed char)(finite ? (scale ? q : 0) : -128);
+        for (int u = 0; u < N; u += 4)
+            code[u / 4] = low_bytes(fmaf(x[u], inverse, kWhole), fmaf(x[u + 1], inverse, kWhole), fmaf(x[u + 2], inverse, kWhole), fmaf(x[u + 3], inverse, kWhole));
+        return scale;
+    }
+    most = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const unsigned a = __float_as_uint(x[u]) & 0x7fffffffu;
+        most = max(most, a < kInfBits ? a : 0u);
+    }
+#pragma unroll
+    for (int d = 1; d < kGroup / N; d <<= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
+    scale = scale_byte(most);
+    const float inv = __uint_as_float((unsigned)(254 - scale) << 23);
+#pragma unroll
+    for (int u = 0; u < N; u += 4) {
+        code[u / 4] = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool finite = (__float_as_uint(x[u + k]) & 0x7fffffffu) < kInfBits;
+            const int q = finite ? (int)rintf(fminf(fmaxf(x[u + k] * inv, -127.f), 127.f)) : -128;
+            code[u / 4] |= ((unsigned)q & 0xffu) << (8 * k);
+        }
     }
     return scale;
-}
-__device__ __forceinline__ float act_scale(unsigned byte) { return __uint_as_float(byte << 23); }
-__device__ __forceinline__ float act_value(signed char code, float scale) {
-    return code == -128 ? __builtin_nanf("") : (float)code * scale;
 }
 
 struct ActOut { signed char* codes; unsigned char* scales; };
 
-__device__ __forceinline__ void store_codes(const ActOut& k, const ActPlace& p, int64_t ldc, int groups, const codex16& code, int scale) {
-    if (!p.in) return;
-    *reinterpret_cast<PSGD_GLOBAL codex16*>(as_global(k.codes) + p.row * ldc + p.col) = code;
-    if ((p.col & (kGroup - 1)) == 0) as_global(k.scales)[p.row * groups + p.col / kGroup] = (unsigned char)scale;
+// (a row's codes reach to the next multiple of 16 columns)
+template <int W>
+__device__ __forceinline__ void store_codes(const ActOut& k, const ActPlace& p, const ActRows& r, int64_t ldc, const unsigned (&code)[W], int scale) {
+    if (p.row < r.rows && p.col < (r.cols + 15) / 16 * 16) {
+        PSGD_GLOBAL signed char* at = as_global(k.codes) + p.row * ldc + p.col;
+        if constexpr (W == 2) *reinterpret_cast<PSGD_GLOBAL uintx2*>(at) = uintx2{code[0], code[1]};
+        else *reinterpret_cast<PSGD_GLOBAL unsigned*>(at) = code[0];
+    }
+    if (p.in && (p.col & (kGroup - 1)) == 0) as_global(k.scales)[p.row * ((r.cols + kGroup - 1) / kGroup) + p.col / kGroup] = (unsigned char)scale;
 }
-__device__ __forceinline__ void load_values(const signed char* codes, const unsigned char* scales, const ActPlace& p, int64_t ldc, int groups,
-                                            float (&x)[16]) {
-    const codex16 code = *reinterpret_cast<const PSGD_GLOBAL codex16*>(as_global(codes) + p.row * ldc + p.col);
-    const float scale = act_scale(as_global(scales)[p.row * groups + p.col / kGroup]);
+
+// a piece's codes (kPiece / 4 words) and its group's scale
+template <int W> struct ActCodes { unsigned w[W]; float scale; };
+template <int W>
+__device__ __forceinline__ ActCodes<W> load_codes(const signed char* codes, const unsigned char* scales, const ActPlace& p, const ActRows& r, int64_t ldc) {
+    ActCodes<W> c = {};
+    if (p.in) {
+        const PSGD_GLOBAL signed char* at = as_global(codes) + p.row * ldc + p.col;
+        if constexpr (W == 2) {
+            const uintx2 w = *reinterpret_cast<const PSGD_GLOBAL uintx2*>(at);
+            c.w[0] = w[0], c.w[1] = w[1];
+        } else {
+            c.w[0] = *reinterpret_cast<const PSGD_GLOBAL unsigned*>(at);
+        }
+        c.scale = __uint_as_float((unsigned)as_global(scales)[p.row * ((r.cols + kGroup - 1) / kGroup) + p.col / kGroup] << 23);
+    }
+    return c;
+}
+template <int W>
+__device__ __forceinline__ void values(const ActCodes<W>& c, float (&x)[4 * W]) {
+    bool any = c.scale > 0x1p120f;       // (128 times the largest scale is infinite)
 #pragma unroll
-    for (int u = 0; u < 16; ++u) x[u] = act_value(code[u], scale);
+    for (int i = 0; i < W; ++i) {
+        const unsigned w = c.w[i] ^ 0x80808080u;        // code + 128
+        any |= ((w - 0x01010101u) & ~w & 0x80808080u) != 0;         // a byte that is zero
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[4 * i + k] = fmaf((float)((w >> (8 * k)) & 0xffu), c.scale, -128.f * c.scale);
+    }
+    if (__any(any)) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const signed char code = (signed char)(c.w[i] >> (8 * k));
+                x[4 * i + k] = code == -128 ? __builtin_nanf("") : (float)code * c.scale;
+            }
+    }
 }
 
-// The two threads of a group are neighbours: `per` counts whole groups' halves (an even number of items per row).
-template <class T>
-__global__ __launch_bounds__(kThreads) void act_store_kernel(int64_t rows, int cols, int per, const T* x, int64_t ld, ActOut out, int64_t ldc, int groups) {
-    const ActPlace p = act_place(rows, per);
-    float v[16];
-    load16(as_global(x) + (p.in ? p.row : 0) * ld, p.in ? p.col : cols, cols, v);
-    codex16 code;
-    const int scale = quantise16(v, code);
-    if (p.col < (cols + 15) / 16 * 16) store_codes(out, p, ldc, groups, code, scale);
+template <class T, bool STREAM>
+__global__ __launch_bounds__(kThreads) void act_store_kernel(ActRows r, const T* x, int64_t ld, ActOut out, int64_t ldc) {
+    constexpr int N = kPiece<T>;
+    ActPlace p[kActItems];
+    uintx4 w[kActItems];
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        p[i] = act_place<N>(r, i);
+        w[i] = load_raw<STREAM>(x, ld, p[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        clear_beyond<T>(w[i], p[i], r.cols);
+        float v[N];
+        unsigned code[N / 4];
+        widen<T>(w[i], v);
+        const int scale = quantise<T>(w[i], v, code);
+        store_codes(out, p[i], r, ldc, code, scale);
+    }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void act_restore_kernel(int64_t rows, int cols, int per, const signed char* codes, const unsigned char* scales,
-                                                               int64_t ldc, int groups, T* x, int64_t ld) {
-    const ActPlace p = act_place(rows, per);
-    if (!p.in || p.col >= cols) return;
-    float v[16];
-    load_values(codes, scales, p, ldc, groups, v);
-    store16(as_global(x) + p.row * ld, p.col, cols, v);
+template <class T, bool STREAM>
+__global__ __launch_bounds__(kThreads) void act_restore_kernel(ActRows r, const signed char* codes, const unsigned char* scales, int64_t ldc, T* x, int64_t ld) {
+    constexpr int N = kPiece<T>;
+    ActPlace p[kActItems];
+    ActCodes<N / 4> c[kActItems];
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        p[i] = act_place<N>(r, i);
+        c[i] = load_codes<N / 4>(codes, scales, p[i], r, ldc);
+    }
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        float v[N];
+        values(c[i], v);
+        store_piece<STREAM>(x, ld, p[i], r.cols, v);
+    }
 }
 
 // act(x) and its derivative.  SiLU: x s, s (1 + x (1 - s)) with s = 1 / (1 + e^-x).  GELU: x F, F + x f with the normal
-// distribution's F and f.  bf16 results take the hardware's exponential (1e-6 relative), fp32 ones the library's.
+// distribution's F and f.  For bf16 results (FAST) the hardware's exponential and reciprocal, good to 1e-6, and F from f by formula
+// 7.1.26 of Abramowitz and Stegun, good to 1e-7: one exponential serves both; for fp32 the library's functions.
 template <int ACT, bool FAST>
 __device__ __forceinline__ float act_fn(float x, float& slope) {
     if constexpr (ACT == PSGD_SILU) {
-        const float s = 1.f / (1.f + (FAST ? __expf(-x) : expf(-x)));
-        slope = s * (1.f + x * (1.f - s));
+        const float s = FAST ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x)) : 1.f / (1.f + expf(-x));
+        slope = s * fmaf(x, 1.f - s, 1.f);
         return x * s;
+    } else if constexpr (FAST) {
+        const float z = fabsf(x) * 0.70710678118654752f, k = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+        const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * x * x);
+        const float poly = k * fmaf(k, fmaf(k, fmaf(k, fmaf(k, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        const float tail = 0.5f * poly * e, cdf = x < 0.f ? tail : 1.f - tail;
+        slope = fmaf(x * 0.39894228040143268f, e, cdf);
+        return x * cdf;
     } else {
         const float cdf = 0.5f * (1.f + erff(x * 0.70710678118654752f));
-        slope = cdf + x * 0.39894228040143268f * (FAST ? __expf(-0.5f * x * x) : expf(-0.5f * x * x));
+        slope = cdf + x * 0.39894228040143268f * expf(-0.5f * x * x);
         return x * cdf;
     }
 }
 
-template <class T, int ACT, bool GATED>
-__global__ __launch_bounds__(kThreads) void act_glu_kernel(int64_t rows, int cols, int per, const T* gate, const T* up, int64_t ld_in, T* h,
-                                                           int64_t ld_h, ActOut kg, ActOut ku, int64_t ldc, int groups) {
-    const ActPlace p = act_place(rows, per);
-    const int64_t row = p.in ? p.row : 0;
-    const int col = p.in ? p.col : cols;
-    const bool kept = p.col < (cols + 15) / 16 * 16;
-    float g[16], u[16], y[16];
-    load16(as_global(gate) + row * ld_in, col, cols, g);
-    if constexpr (GATED) load16(as_global(up) + row * ld_in, col, cols, u);
-    codex16 code;
-    int scale = quantise16(g, code);
-    if (kept) store_codes(kg, p, ldc, groups, code, scale);
-    if constexpr (GATED) {
-        scale = quantise16(u, code);
-        if (kept) store_codes(ku, p, ldc, groups, code, scale);
+template <class T, int ACT, bool GATED, bool STREAM>
+__global__ __launch_bounds__(kThreads) void act_glu_kernel(ActRows r, const T* gate, const T* up, int64_t ld_in, T* h, int64_t ld_h, ActOut kg, ActOut ku,
+                                                           int64_t ldc) {
+    constexpr int N = kPiece<T>;
+    ActPlace p[kActItems];
+    uintx4 wg[kActItems], wu[kActItems];
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        p[i] = act_place<N>(r, i);
+        wg[i] = load_raw<STREAM>(gate, ld_in, p[i]);
+        if constexpr (GATED) wu[i] = load_raw<STREAM>(up, ld_in, p[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float slope;
-        y[i] = act_fn<ACT, sizeof(T) == 2>(g[i], slope);
-        if constexpr (GATED) y[i] *= u[i];
+    for (int i = 0; i < kActItems; ++i) {
+        float g[N], u[N], y[N];
+        unsigned code[N / 4];
+        clear_beyond<T>(wg[i], p[i], r.cols);
+        widen<T>(wg[i], g);
+        int scale = quantise<T>(wg[i], g, code);
+        store_codes(kg, p[i], r, ldc, code, scale);
+        if constexpr (GATED) {
+            clear_beyond<T>(wu[i], p[i], r.cols);
+            widen<T>(wu[i], u);
+            scale = quantise<T>(wu[i], u, code);
+            store_codes(ku, p[i], r, ldc, code, scale);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float slope;
+            y[k] = act_fn<ACT, sizeof(T) == 2>(g[k], slope);
+            if constexpr (GATED) y[k] *= u[k];
+        }
+        store_piece<STREAM>(h, ld_h, p[i], r.cols, y);
     }
-    if (p.in) store16(as_global(h) + p.row * ld_h, p.col, cols, y);
 }
 
-template <class T, int ACT, bool GATED>
-__global__ __launch_bounds__(kThreads) void act_glu_backward_kernel(int64_t rows, int cols, int per, const signed char* cg, const unsigned char* sg,
-                                                                    const signed char* cu, const unsigned char* su, int64_t ldc, int groups,
-                                                                    const T* dh, int64_t ld_h, T* dgate, T* dup, int64_t ld_out) {
-    const ActPlace p = act_place(rows, per);
-    if (!p.in || p.col >= cols) return;
-    float g[16], u[16], d[16], y[16];
-    load_values(cg, sg, p, ldc, groups, g);
-    if constexpr (GATED) load_values(cu, su, p, ldc, groups, u);
-    load16(as_global(dh) + p.row * ld_h, p.col, cols, d);
+template <class T, int ACT, bool GATED, bool STREAM>
+__global__ __launch_bounds__(kThreads) void act_glu_backward_kernel(ActRows r, const signed char* cg, const unsigned char* sg, const signed char* cu,
+                                                                    const unsigned char* su, int64_t ldc, const T* dh, int64_t ld_h, T* dgate, T* dup,
+                                                                    int64_t ld_out) {
+    constexpr int N = kPiece<T>;
+    ActPlace p[kActItems];
+    ActCodes<N / 4> kg[kActItems], ku[kActItems];
+    uintx4 wd[kActItems];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float slope;
-        const float a = act_fn<ACT, sizeof(T) == 2>(g[i], slope);
-        y[i] = d[i] * a;
-        g[i] = (GATED ? d[i] * u[i] : d[i]) * slope;
+    for (int i = 0; i < kActItems; ++i) {
+        p[i] = act_place<N>(r, i);
+        kg[i] = load_codes<N / 4>(cg, sg, p[i], r, ldc);
+        if constexpr (GATED) ku[i] = load_codes<N / 4>(cu, su, p[i], r, ldc);
+        wd[i] = load_raw<STREAM>(dh, ld_h, p[i]);
     }
-    store16(as_global(dgate) + p.row * ld_out, p.col, cols, g);
-    if constexpr (GATED) store16(as_global(dup) + p.row * ld_out, p.col, cols, y);
+#pragma unroll
+    for (int i = 0; i < kActItems; ++i) {
+        float g[N], u[N], d[N], y[N];
+        values(kg[i], g);
+        if constexpr (GATED) values(ku[i], u);
+        widen<T>(wd[i], d);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float slope;
+            const float a = act_fn<ACT, sizeof(T) == 2>(g[k], slope);
+            y[k] = d[k] * a;
+            g[k] = (GATED ? d[k] * u[k] : d[k]) * slope;
+        }
+        store_piece<STREAM>(dgate, ld_out, p[i], r.cols, g);
+        if constexpr (GATED) store_piece<STREAM>(dup, ld_out, p[i], r.cols, y);
+    }
 }
 
 struct ActGrid {
+    ActRows rows;
     dim3 grid;
-    int per, groups;
 };
-static ActGrid act_grid(int64_t rows, int64_t cols) {
+static ActGrid act_grid(int64_t rows, int64_t cols, int dtype) {
     ActGrid g;
-    g.groups = (int)((cols + kGroup - 1) / kGroup);
-    g.per = 2 * g.groups;
-    g.grid = dim3((unsigned)((rows * g.per + kThreads - 1) / kThreads));
+    const int n = dtype == PSGD_F32 ? kPiece<float> : kPiece<bf16_t>;
+    g.rows.rows = rows, g.rows.cols = (int)cols;
+    g.rows.per = (int)((cols + kGroup - 1) / kGroup * (kGroup / n));
+    g.rows.inv_per = 1.0 / g.rows.per;
+    g.grid = dim3((unsigned)((rows * g.rows.per + kThreads * kActItems - 1) / (kThreads * kActItems)));
     return g;
 }
 static int act_shape(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || rows > kMaxExtent || cols > kMaxExtent) return PSGD_E_SHAPE;
-    if (rows * (2 * ((cols + kGroup - 1) / kGroup)) > (int64_t)INT32_MAX * kThreads) return PSGD_E_SHAPE;
+    if (rows * (8 * ((cols + kGroup - 1) / kGroup)) > (int64_t)INT32_MAX * kThreads) return PSGD_E_SHAPE;
     return PSGD_OK;
 }
 static bool bad_codes(const void* codes, const void* scales) { return !codes || !scales; }
 static bool bad_ldc(int64_t ldc, int64_t cols) { return ldc < cols || (ldc & 15) != 0; }
+
+static bool act_stream(int64_t rows, int64_t cols, int dtype, int matrices) {
+    return rows * cols * (dtype == PSGD_F32 ? 4 : 2) * matrices >= kActStream;
+}
+static int act_restore(void* stream, int64_t rows, int64_t cols, const int8_t* codes, int64_t ldc, const uint8_t* scales, void* x, int dtype, int64_t ld,
+                       bool stream_it) {
+    if (rows == 0) return PSGD_OK;
+    const ActGrid g = act_grid(rows, cols, dtype);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+#define PSGD_RESTORE(T, STREAM) hipLaunchKernelGGL((act_restore_kernel<T, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, codes, scales, ldc, (T*)x, ld)
+    if (dtype == PSGD_F32) { if (stream_it) PSGD_RESTORE(float, true); else PSGD_RESTORE(float, false); }
+    else                   { if (stream_it) PSGD_RESTORE(bf16_t, true); else PSGD_RESTORE(bf16_t, false); }
+#undef PSGD_RESTORE
+    return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+}
 
 struct WgradPlan {
     size_t bytes = 0, x = 0, planes = 0, part = 0;
@@ -257,11 +420,14 @@ int psgd_act_store(void* stream, int64_t rows, int64_t cols, const void* x, int 
     if (int rc = act_shape(rows, cols)) return rc;
     if (bad_ld(ld, cols) || bad_ldc(ldc, cols) || misaligned(x) || misaligned(codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;
-    const ActGrid g = act_grid(rows, cols);
+    const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const ActOut out = {codes, scales};
-    if (dtype == PSGD_F32) hipLaunchKernelGGL(act_store_kernel<float>, g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, (const float*)x, ld, out, ldc, g.groups);
-    else hipLaunchKernelGGL(act_store_kernel<bf16_t>, g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, (const bf16_t*)x, ld, out, ldc, g.groups);
+#define PSGD_STORE(T, STREAM) hipLaunchKernelGGL((act_store_kernel<T, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, (const T*)x, ld, out, ldc)
+    const bool stream_it = act_stream(rows, cols, dtype, 1);
+    if (dtype == PSGD_F32) { if (stream_it) PSGD_STORE(float, true); else PSGD_STORE(float, false); }
+    else                   { if (stream_it) PSGD_STORE(bf16_t, true); else PSGD_STORE(bf16_t, false); }
+#undef PSGD_STORE
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
 
@@ -269,12 +435,7 @@ int psgd_act_restore(void* stream, int64_t rows, int64_t cols, const int8_t* cod
     if ((rows != 0 && (!x || bad_codes(codes, scales))) || bad_dtype(dtype)) return PSGD_E_INVALID_ARG;
     if (int rc = act_shape(rows, cols)) return rc;
     if (bad_ld(ld, cols) || bad_ldc(ldc, cols) || misaligned(x) || misaligned(codes)) return PSGD_E_ALIGN;
-    if (rows == 0) return PSGD_OK;
-    const ActGrid g = act_grid(rows, cols);
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == PSGD_F32) hipLaunchKernelGGL(act_restore_kernel<float>, g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, codes, scales, ldc, g.groups, (float*)x, ld);
-    else hipLaunchKernelGGL(act_restore_kernel<bf16_t>, g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, codes, scales, ldc, g.groups, (bf16_t*)x, ld);
-    return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+    return act_restore(stream, rows, cols, codes, ldc, scales, x, dtype, ld, act_stream(rows, cols, dtype, 1));
 }
 
 int psgd_act_glu(void* stream, int64_t rows, int64_t cols, int act, int dtype, const void* gate, const void* up, int64_t ld_in, void* h, int64_t ld_h,
@@ -286,16 +447,19 @@ int psgd_act_glu(void* stream, int64_t rows, int64_t cols, int act, int dtype, c
     if (bad_ld(ld_in, cols) || bad_ld(ld_h, cols) || bad_ldc(ldc, cols) || misaligned(gate) || misaligned(up) || misaligned(h) ||
         misaligned(gate_codes) || misaligned(up_codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;
-    const ActGrid g = act_grid(rows, cols);
+    const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const ActOut kg = {gate_codes, gate_scales}, ku = {up_codes, up_scales};
-#define PSGD_GLU(T, ACT, GATED)                                                                                                       \
-    hipLaunchKernelGGL((act_glu_kernel<T, ACT, GATED>), g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, (const T*)gate, (const T*)up, \
-                       ld_in, (T*)h, ld_h, kg, ku, ldc, g.groups)
-#define PSGD_GLU_ACT(T, GATED) do { if (act == PSGD_SILU) PSGD_GLU(T, PSGD_SILU, GATED); else PSGD_GLU(T, PSGD_GELU, GATED); } while (0)
+    const bool stream_it = act_stream(rows, cols, dtype, up ? 3 : 2);
+#define PSGD_GLU(T, ACT, GATED, STREAM)                                                                                                       \
+    hipLaunchKernelGGL((act_glu_kernel<T, ACT, GATED, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, (const T*)gate, (const T*)up, \
+                       ld_in, (T*)h, ld_h, kg, ku, ldc)
+#define PSGD_GLU_STREAM(T, ACT, GATED) do { if (stream_it) PSGD_GLU(T, ACT, GATED, true); else PSGD_GLU(T, ACT, GATED, false); } while (0)
+#define PSGD_GLU_ACT(T, GATED) do { if (act == PSGD_SILU) PSGD_GLU_STREAM(T, PSGD_SILU, GATED); else PSGD_GLU_STREAM(T, PSGD_GELU, GATED); } while (0)
     if (dtype == PSGD_F32) { if (up) PSGD_GLU_ACT(float, true); else PSGD_GLU_ACT(float, false); }
     else                   { if (up) PSGD_GLU_ACT(bf16_t, true); else PSGD_GLU_ACT(bf16_t, false); }
 #undef PSGD_GLU
+#undef PSGD_GLU_STREAM
 #undef PSGD_GLU_ACT
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
@@ -311,15 +475,18 @@ int psgd_act_glu_backward(void* stream, int64_t rows, int64_t cols, int act, int
     if (bad_ld(ld_h, cols) || bad_ld(ld_out, cols) || bad_ldc(ldc, cols) || misaligned(dh) || misaligned(dgate) || misaligned(dup) ||
         misaligned(gate_codes) || misaligned(up_codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;
-    const ActGrid g = act_grid(rows, cols);
+    const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-#define PSGD_GLU(T, ACT, GATED)                                                                                                       \
-    hipLaunchKernelGGL((act_glu_backward_kernel<T, ACT, GATED>), g.grid, dim3(kThreads), 0, st, rows, (int)cols, g.per, gate_codes,    \
-                       gate_scales, up_codes, up_scales, ldc, g.groups, (const T*)dh, ld_h, (T*)dgate, (T*)dup, ld_out)
-#define PSGD_GLU_ACT(T, GATED) do { if (act == PSGD_SILU) PSGD_GLU(T, PSGD_SILU, GATED); else PSGD_GLU(T, PSGD_GELU, GATED); } while (0)
+    const bool stream_it = act_stream(rows, cols, dtype, gated ? 3 : 2);
+#define PSGD_GLU(T, ACT, GATED, STREAM)                                                                                                       \
+    hipLaunchKernelGGL((act_glu_backward_kernel<T, ACT, GATED, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, gate_codes,    \
+                       gate_scales, up_codes, up_scales, ldc, (const T*)dh, ld_h, (T*)dgate, (T*)dup, ld_out)
+#define PSGD_GLU_STREAM(T, ACT, GATED) do { if (stream_it) PSGD_GLU(T, ACT, GATED, true); else PSGD_GLU(T, ACT, GATED, false); } while (0)
+#define PSGD_GLU_ACT(T, GATED) do { if (act == PSGD_SILU) PSGD_GLU_STREAM(T, PSGD_SILU, GATED); else PSGD_GLU_STREAM(T, PSGD_GELU, GATED); } while (0)
     if (dtype == PSGD_F32) { if (gated) PSGD_GLU_ACT(float, true); else PSGD_GLU_ACT(float, false); }
     else                   { if (gated) PSGD_GLU_ACT(bf16_t, true); else PSGD_GLU_ACT(bf16_t, false); }
 #undef PSGD_GLU
+#undef PSGD_GLU_STREAM
 #undef PSGD_GLU_ACT
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
@@ -342,7 +509,7 @@ int psgd_act_wgrad(void* workspace, void* stream, int64_t tokens, int64_t out_fe
     bf16_t* x = reinterpret_cast<bf16_t*>(ws + w.x);
     bf16_t* planes = reinterpret_cast<bf16_t*>(ws + w.planes);
     if (tokens > 0) {
-        if (int rc = psgd_act_restore(stream, tokens, in_features, codes, ldc, scales, x, PSGD_BF16, w.ldx)) return rc;
+        if (int rc = act_restore(stream, tokens, in_features, codes, ldc, scales, x, PSGD_BF16, w.ldx, false)) return rc;
         if (dtype == PSGD_F32 && launch_planes(dy, dtype, tokens, out_features, ldy, planes, 3, st) != hipSuccess) return PSGD_E_HIP;
     }
     TileArgs t = {};
