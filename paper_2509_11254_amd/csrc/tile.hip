@@ -52,7 +52,7 @@ __device__ inline TileSize tile_size(const TileArgs& t) {
 }
 
 template <bool LKC, TileShape SHAPE, int KIND>
-__global__ __launch_bounds__(kTileThreads, 1) void product_kernel(TileArgs t, TileOut o) {
+__global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kernel(TileArgs t, TileOut o) {
     extern __shared__ __align__(16) unsigned char smem[];
     using T = Tile<false, LKC, SHAPE>;
     const TileSize size = tile_size(t);
@@ -133,23 +133,39 @@ __global__ __launch_bounds__(kThreads) void planes_kernel(const T* src, int64_t 
 
 constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel fills one
 
-// Shape and splits by an estimate in microseconds.  A workgroup takes A before and after its chunks and C per chunk (256 x 256: 11 and 1.65, which
-// is the matrix cores' rate; 128 x 128: 5 and 0.57; 128 x 64: 4.5 and 0.45, the smaller ones' latency), workgroups run 256 at a time; a split
-// contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for each that a thread adds up.  Weight
-// gradients tokens x out x in, measured with 256 x 256 / 128 x 128 / 128 x 64, each with its best number of splits, in us:
-// 128 x 800 x 800 18.5 / 13.9 / 14.4;  1000 x 2048 x 2048 34.7 / 22.7 / 29.5;  9001 x 256 x 1032 32.8 / 27.7 / 32.4;  4096 x 512 x 512
-// 29.5 / 20.8 / 19.7;  8192 x 2048 x 2048 87.3 / 89.9 / 134.7;  2000 x 4096 x 4096 73.3 / 96.7 / 147.8;  64 x 4096 x 4096 19.8 / 26.2 / 35.4.
+// Shape and splits by an estimate in microseconds.  A workgroup takes A before and after its chunks and C per chunk: 256 x 256 11 and 1.65 (the matrix
+// cores' rate), 128 x 128 5 and 0.57, 128 x 64 4.5 and 0.45, one to a compute unit; TILE_MANY 5 and 1 with up to two to a compute unit, 0.52 for each
+// of three and four.  A split contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for
+// each that a thread adds up.  Weight gradients tokens x out x in, each shape with its best number of splits, in us:
+//                    256 x 256   128 x 128   128 x 64   TILE_MANY
+//   1 x 4096 x 4096       20.9        29.8       39.5        15.7
+//   64 x 11008 x 11008     113         170        244          56
+//   300 x 11008 x 11008    161         242        340         112
+//   800 x 4096 x 4096     42.8        62.3         82        43.3
+//   2000 x 4096 x 4096    74.1       108.3      148.8        80.0
+//   8192 x 2048 x 2048    87.4        99.6      131.6        96.6
+//   1000 x 2048 x 2048    34.6        23.4       29.9        29.2
+//   9001 x 256 x 1032     33.3        28.9       31.7        29.7
+//   4096 x 512 x 512      29.8        21.4       19.7
 TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split) {
-    static const double A[3] = {11, 5, 4.5}, C[3] = {1.65, 0.57, 0.45};
+    static const double A[TILE_SHAPES] = {11, 5, 4.5, 5}, C[TILE_SHAPES] = {1.65, 0.57, 0.45, 0.52};
     TilePlan best = {TILE_256, 1};
     double least = 1e300;
-    for (TileShape shape : {TILE_256, TILE_128, TILE_THIN}) {
+    for (TileShape shape : {TILE_256, TILE_128, TILE_THIN, TILE_MANY}) {
         const int64_t tiles = (extent_p + tile_p(shape) - 1) / tile_p(shape) * ((extent_l + tile_l(shape) - 1) / tile_l(shape));
         const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
         for (int64_t want : {(int64_t)1, fill / 4, fill / 2, fill, 2 * fill}) {
             if (want < 1 || (want > 1 && (!may_split || want > 64 || want > chunks))) continue;
             const int64_t share = (chunks + want - 1) / want, split = share > 0 ? (chunks + share - 1) / share : 1;
-            double us = (double)((tiles * split + kUnits - 1) / kUnits) * (A[shape] + share * C[shape]);
+            const int64_t blocks = tiles * split;
+            double us;
+            if (shape == TILE_MANY) {
+                const int64_t last = (blocks % (4 * kUnits) + kUnits - 1) / kUnits;        // workgroups to a compute unit in the last round
+                us = (double)(blocks / (4 * kUnits)) * (A[shape] + share * 4 * C[shape]);
+                if (last > 0) us += A[shape] + share * std::max(1.0, last * C[shape]);
+            } else {
+                us = (double)((blocks + kUnits - 1) / kUnits) * (A[shape] + share * C[shape]);
+            }
             if (split > 1) us += 4 + 0.08 * split + split * (double)extent_p * (double)extent_l * 8e-6 / 8;
             if (us < least) least = us, best = {shape, (int)split};
         }
@@ -192,10 +208,12 @@ hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t,
     if (l_contiguous) {
         if (shape == TILE_256) return launch_shape<true, TILE_256>(t, o, st);
         if (shape == TILE_128) return launch_shape<true, TILE_128>(t, o, st);
+        if (shape == TILE_MANY) return launch_shape<true, TILE_MANY>(t, o, st);
         return launch_shape<true, TILE_THIN>(t, o, st);
     }
     if (shape == TILE_256) return launch_shape<false, TILE_256>(t, o, st);
     if (shape == TILE_128) return launch_shape<false, TILE_128>(t, o, st);
+    if (shape == TILE_MANY) return launch_shape<false, TILE_MANY>(t, o, st);
     return launch_shape<false, TILE_THIN>(t, o, st);
 }
 

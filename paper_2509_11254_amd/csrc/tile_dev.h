@@ -103,9 +103,10 @@ struct TileSide {
     __device__ __forceinline__ void load(const Source& s, PSGD_TLDS unsigned char* dst, int wv) const {
         const unsigned v = KC && kpiece >= s.left ? kOutside : off[I];
         // (Written out so that the compiler, which cannot tell the places in LDS apart, does not wait for all loads before each
-        // transposing read.  No result: what is in flight holds no register.  run() does the waiting.)
+        // transposing read.  No result: what is in flight holds no register.  run() does the waiting.  m0 is a register the compiler reserves, and sets
+        // before each instruction of its own that takes it, of which these kernels have none.)
         const unsigned to = scalar((unsigned)(uintptr_t)(dst + (I * NW + wv) * 1024));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(s.rsrc) : "m0");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(s.rsrc));
     }
     __device__ __forceinline__ void load_all(const Source& s, PSGD_TLDS unsigned char* dst, int wv) const {
         load<0>(s, dst, wv);
@@ -148,10 +149,13 @@ struct TileFragment {
     }
 };
 
-// Waves along P and L, chunks in LDS.  All have four waves, one per SIMD, and LDS for one workgroup per compute unit.
+// Waves along P and L, chunks in LDS.  All have four waves, one per SIMD.
+// workgroups to a compute unit
+constexpr int tile_share(TileShape s) { return s == TILE_MANY ? 4 : 1; }
 template <TileShape SHAPE> struct TileWaves;
 template <> struct TileWaves<TILE_256> { static constexpr int WP = 2, WL = 2, STAGES = 0; };
 template <> struct TileWaves<TILE_128> { static constexpr int WP = 2, WL = 2, STAGES = 5; };
+template <> struct TileWaves<TILE_MANY> { static constexpr int WP = 2, WL = 2, STAGES = 1; };
 template <> struct TileWaves<TILE_THIN> { static constexpr int WP = 2, WL = 2, STAGES = 6; };
 
 template <bool PKC, bool LKC, TileShape SHAPE>
@@ -163,26 +167,17 @@ struct Tile {
     using SideP = TileSide<PKC, BP, BK, NW>;
     using SideL = TileSide<LKC, BL, BK, NW>;
     static constexpr int STAGE_BYTES = SideP::BYTES + SideL::BYTES;
-    static constexpr int LDS_BYTES = FULL ? 5 * SideP::BYTES : STAGES * STAGE_BYTES;
+    static constexpr int ROWS_BYTES = NW * 32 * (32 * FP + 4) * 4;         // for_rows()
+    static constexpr int CHUNK_BYTES = FULL ? 5 * SideP::BYTES : STAGES * STAGE_BYTES;
+    static constexpr int LDS_BYTES = CHUNK_BYTES > ROWS_BYTES ? CHUNK_BYTES : ROWS_BYTES;
     static constexpr int LOADS = SideP::LOADS + SideL::LOADS;
     static_assert(FP >= 1 && FL >= 1 && FP <= 4 && FL <= 4 && BK == 64 && NW * 64 == kTileThreads && LDS_BYTES <= 160 * 1024, "waves");
-    static_assert((STAGES - 2) * LOADS <= 63, "the wait counter's range");
+    static_assert((STAGES - 1) * LOADS <= 63 && (FULL || LOADS >= 3), "the wait counter's range, thirds");
+    static_assert(SHAPE != TILE_MANY || 4 * LDS_BYTES <= 160 * 1024, "four to a compute unit");
 
     floatx16 acc[FP][FL];
     int wp, wl, lane;
 
-    template <int KK>
-    __device__ __forceinline__ void read(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, BP, BK>& fp,
-                                         const TileFragment<LKC, BL, BK>& fl, bf16x8 (&a)[FP], bf16x8 (&b)[FL]) {
-        a[0] = fp.template read<KK, 0>(chunk);
-        if constexpr (FP > 1) a[1] = fp.template read<KK, 1>(chunk);
-        if constexpr (FP > 2) a[2] = fp.template read<KK, 2>(chunk);
-        if constexpr (FP > 3) a[3] = fp.template read<KK, 3>(chunk);
-        b[0] = fl.template read<KK, 0>(chunk + SideP::BYTES);
-        if constexpr (FL > 1) b[1] = fl.template read<KK, 1>(chunk + SideP::BYTES);
-        if constexpr (FL > 2) b[2] = fl.template read<KK, 2>(chunk + SideP::BYTES);
-        if constexpr (FL > 3) b[3] = fl.template read<KK, 3>(chunk + SideP::BYTES);
-    }
     template <int KK>
     __device__ __forceinline__ void read_ab(const PSGD_TLDS unsigned char* cp, const PSGD_TLDS unsigned char* cl, const TileFragment<PKC, BP, BK>& fp,
                                             const TileFragment<LKC, BL, BK>& fl, bf16x8 (&a)[FP], bf16x8 (&b)[FL]) {
@@ -201,13 +196,6 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < FL; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
     }
-    template <int KK>
-    __device__ __forceinline__ void step(const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl) {
-        bf16x8 a[FP], b[FL];
-        read<KK>(chunk, fp, fl, a, b);
-        multiply(a, b);
-    }
-
     // 16 steps: multiply a, b; on the way read the fragments of steps 16 KK .. of (cp, cl) into an, bn and send off loads H, H + 1, .. + 3
     // of a side's chunk.  Loads and reads go between the products, two products apart.
     template <int KK, int H, class Side>
@@ -338,34 +326,107 @@ struct Tile {
         if constexpr (FULL) {
             run_full(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         } else {
-            // A ring of chunks; past the end the loads bring zeros, so that no wait depends on where one is.
-            int left = n, pair = n0 / per, kc = n0 - pair * per, into = 0, from = 0;     // of the next chunk to load
-            auto issue = [&]() {
-                const unsigned which = t.pairs >> (4 * pair);
-                PSGD_TLDS unsigned char* dst = lds + into * STAGE_BYTES;
-                sp.load_all(SideP::source(t.P, which & 3, p0, kc * BK, K, left > 0), dst, wv);
-                sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, left > 0), dst + SideP::BYTES, wv);
-                --left;
-                const bool wrap = ++kc == per;
-                kc = wrap ? 0 : kc;
-                pair = min(pair + (wrap ? 1 : 0), 7);
-                into = into + 1 == STAGES ? 0 : into + 1;
-            };
-            for (int i = 0; i < STAGES - 1; ++i) issue();
-            for (int it = 0; it < n; ++it) {
-                // this chunk has arrived, for every wave, and nobody reads the buffer of the one before any more
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * LOADS) : "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                issue();
-                const PSGD_TLDS unsigned char* chunk = lds + from * STAGE_BYTES;
-                step<0>(chunk, fp, fl);
-                step<1>(chunk, fp, fl);
-                step<2>(chunk, fp, fl);
-                step<3>(chunk, fp, fl);
-                from = from + 1 == STAGES ? 0 : from + 1;
-            }
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if constexpr (STAGES == 1) run_single(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
+            else run_ring(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
+        }
+    }
+
+    // 16 steps of the smaller tiles: as round(), with loads H .. H + COUNT - 1 of a chunk (P's first, then L's)
+    template <int KK, int H, int COUNT>
+    __device__ __forceinline__ void ring_round(const bf16x8 (&a)[FP], const bf16x8 (&b)[FL], bf16x8 (&an)[FP], bf16x8 (&bn)[FL],
+                                               const PSGD_TLDS unsigned char* chunk, const TileFragment<PKC, BP, BK>& fp,
+                                               const TileFragment<LKC, BL, BK>& fl, const SideP& sp, const SideL& sl, const typename SideP::Source& from_p,
+                                               const typename SideL::Source& from_l, PSGD_TLDS unsigned char* to, int wv) {
+        read_ab<KK>(chunk, chunk + SideP::BYTES, fp, fl, an, bn);
+        ring_loads<H, COUNT>(sp, sl, from_p, from_l, to, wv);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(a, b);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <int H, int COUNT>
+    __device__ __forceinline__ static void ring_loads(const SideP& sp, const SideL& sl, const typename SideP::Source& from_p,
+                                                      const typename SideL::Source& from_l, PSGD_TLDS unsigned char* to, int wv) {
+        if constexpr (COUNT > 0) {
+            if constexpr (H < SideP::LOADS) sp.template load<H>(from_p, to, wv);
+            else if constexpr (H < LOADS) sl.template load<H - SideP::LOADS>(from_l, to + SideP::BYTES, wv);
+            ring_loads<H + 1, COUNT - 1>(sp, sl, from_p, from_l, to, wv);
+        }
+    }
+
+    // The smaller tiles: a ring of chunks, of which all but the one being read are loaded or on their way (with one workgroup per compute
+    // unit the loads' latency is what counts).  Fragments, barrier and what lies past the end as in run_full.
+    __device__ __forceinline__ void run_ring(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
+                                             const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
+                                             PSGD_TLDS unsigned char* lds) {
+        int left = n, pair = n0 / per, kc = n0 - pair * per, into = 0, from = 0;     // of the next chunk to load
+        typename SideP::Source from_p;
+        typename SideL::Source from_l;
+        auto next = [&]() {         // its place
+            const unsigned which = t.pairs >> (4 * pair);
+            from_p = SideP::source(t.P, which & 3, p0, kc * BK, K, left > 0);
+            from_l = SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, left > 0);
+            PSGD_TLDS unsigned char* const to = lds + into * STAGE_BYTES;
+            --left;
+            const bool wrap = ++kc == per;
+            kc = wrap ? 0 : kc;
+            pair = min(pair + (wrap ? 1 : 0), 7);
+            into = into + 1 == STAGES ? 0 : into + 1;
+            return to;
+        };
+        constexpr int THIRD = (LOADS + 2) / 3;
+        PSGD_TLDS unsigned char* to = nullptr;
+        for (int i = 0; i < STAGES - 1; ++i) {
+            to = next();
+            ring_loads<0, LOADS>(sp, sl, from_p, from_l, to, wv);
+        }
+        to = next();
+        ring_loads<0, THIRD>(sp, sl, from_p, from_l, to, wv);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * LOADS + THIRD) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        bf16x8 a0[FP], b0[FL], a1[FP], b1[FL];
+        read_ab<0>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
+        for (int it = 0; it < n; ++it) {
+            const PSGD_TLDS unsigned char* chunk = lds + from * STAGE_BYTES;
+            from = from + 1 == STAGES ? 0 : from + 1;
+            ring_round<1, THIRD, THIRD>(a0, b0, a1, b1, chunk, fp, fl, sp, sl, from_p, from_l, to, wv);
+            ring_round<2, 2 * THIRD, LOADS - 2 * THIRD>(a1, b1, a0, b0, chunk, fp, fl, sp, sl, from_p, from_l, to, wv);
+            ring_round<3, 0, 0>(a0, b0, a1, b1, chunk, fp, fl, sp, sl, from_p, from_l, to, wv);
+            // the next chunk has arrived, for every wave, and nobody reads this one's place any more: it is the next to be loaded
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * LOADS) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            to = next();
+            ring_round<0, 0, THIRD>(a1, b1, a0, b0, lds + from * STAGE_BYTES, fp, fl, sp, sl, from_p, from_l, to, wv);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    }
+
+    // One chunk in LDS: nothing of this workgroup goes on while it loads; the others of the compute unit do.
+    __device__ __forceinline__ void run_single(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
+                                               const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
+                                               PSGD_TLDS unsigned char* lds) {
+        int pair = n0 / per, kc = n0 - pair * per;
+        for (int it = 0; it < n; ++it) {
+            const unsigned which = t.pairs >> (4 * pair);
+            sp.load_all(SideP::source(t.P, which & 3, p0, kc * BK, K, true), lds, wv);
+            sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, true), lds + SideP::BYTES, wv);
+            if (++kc == per) { kc = 0; ++pair; }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            bf16x8 a0[FP], b0[FL], a1[FP], b1[FL];
+            read_ab<0>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
+            read_ab<1>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
+            multiply(a0, b0);
+            read_ab<2>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
+            multiply(a1, b1);
+            read_ab<3>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
+            multiply(a0, b0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();       // every wave is done with the chunk
+            asm volatile("" ::: "memory");
+            multiply(a1, b1);
         }
     }
 

@@ -9,11 +9,12 @@ namespace psgd {
 constexpr int kTileK = 64;      // contraction steps per chunk
 constexpr int kTileThreads = 256;
 
-// Elements of a tile of C along P and L: 256 x 256 where there are enough of them; 128 x 128 where smaller tiles fill the card better;
-// 128 x 64 for few rows
-enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2 };
+// Elements of a tile of C along P and L.  256 x 256, 128 x 128 (few tiles: one workgroup per compute unit, deep in loads) and 128 x 64 (few
+// rows) have a compute unit's LDS for themselves; of TILE_MANY, 128 x 128 with one chunk in LDS, a compute unit takes four, which hide each
+// other's loads and stores.
+enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2, TILE_MANY = 3, TILE_SHAPES = 4 };
 constexpr int tile_p(TileShape s) { return s == TILE_256 ? 256 : 128; }
-constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_128 ? 128 : 64; }
+constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_THIN ? 64 : 128; }
 
 struct TileOperand {
     const bf16_t* ptr;
