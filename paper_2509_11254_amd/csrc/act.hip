@@ -11,7 +11,8 @@
 // whole number is the addition of 1.5 * 2^23 (whose last bit is 1), the codes are the sums' low bytes; a code becomes a value by the
 // conversion of an unsigned byte and one multiply-add; what is not finite or beyond the largest scale is sought once per group, and sends the
 // wavefront the slow way.  16384 x 11008 in bf16, stored and restored: 201 -> 171 us, 6.4 TB/s; gated unit of 8192 x 11008, both ways: 293 -> 229, 6.4 TB/s.
-#include "tile_dev.h"
+#include "act_dev.h"
+#include "train.h"
 
 namespace psgd {
 
@@ -179,8 +180,6 @@ __device__ __forceinline__ void store_codes(const ActOut& k, const ActPlace& p, 
     if (p.in && (p.col & (kGroup - 1)) == 0) as_global(k.scales)[p.row * ((r.cols + kGroup - 1) / kGroup) + p.col / kGroup] = (unsigned char)scale;
 }
 
-// a piece's codes (kPiece / 4 words) and its group's scale
-template <int W> struct ActCodes { unsigned w[W]; float scale; };
 template <int W>
 __device__ __forceinline__ ActCodes<W> load_codes(const signed char* codes, const unsigned char* scales, const ActPlace& p, const ActRows& r, int64_t ldc) {
     ActCodes<W> c = {};
@@ -196,27 +195,6 @@ __device__ __forceinline__ ActCodes<W> load_codes(const signed char* codes, cons
     }
     return c;
 }
-template <int W>
-__device__ __forceinline__ void values(const ActCodes<W>& c, float (&x)[4 * W]) {
-    bool any = c.scale > 0x1p120f;       // (128 times the largest scale is infinite)
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const unsigned w = c.w[i] ^ 0x80808080u;        // code + 128
-        any |= ((w - 0x01010101u) & ~w & 0x80808080u) != 0;         // a byte that is zero
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[4 * i + k] = fmaf((float)((w >> (8 * k)) & 0xffu), c.scale, -128.f * c.scale);
-    }
-    if (__any(any)) {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const signed char code = (signed char)(c.w[i] >> (8 * k));
-                x[4 * i + k] = code == -128 ? __builtin_nanf("") : (float)code * c.scale;
-            }
-    }
-}
-
 template <class T, bool STREAM>
 __global__ __launch_bounds__(kThreads) void act_store_kernel(ActRows r, const T* x, int64_t ld, ActOut out, int64_t ldc) {
     constexpr int N = kPiece<T>;
@@ -394,12 +372,13 @@ static WgradPlan wgrad_plan(int64_t tokens, int64_t out, int64_t in, int dtype) 
     WgradPlan w;
     auto take = [&](size_t bytes) { const size_t at = w.bytes; w.bytes += up256(bytes); return at; };
     w.ldx = up8(in);
-    w.x = take((size_t)tokens * w.ldx * 2);
-    if (dtype == PSGD_F32) {
-        w.n_planes = 3;
-        w.planes = take((size_t)tokens * up8(out) * 2 * 3);
-    }
-    w.tile = tile_plan(in, out, (tokens + kTileK - 1) / kTileK * w.n_planes, true);
+    w.n_planes = dtype == PSGD_F32 ? 3 : 1;
+    // A launch of its own puts X's values into the workspace for all tiles, or each tile makes them of the codes as it goes, as often as there are tiles along
+    // `out`.  (Tokens x out x in, in us, the first way with its best tiles and the second: 64 x 1000 x 1000 11.4, 8.1; 400 x 2000 x 1000 14.8, 12.9; 64 x 4096 x 4096
+    // 16.1, 14.2; 300 x 11008 x 11008 112, 139; 2000 x 4096 x 4096 74, 100.)
+    w.tile = tile_plan(in, out, (tokens + kTileK - 1) / kTileK * w.n_planes, true, 3 + tokens * (double)in * 3e-6 / 5);
+    if (!w.tile.from_codes) w.x = take((size_t)tokens * w.ldx * 2);
+    if (dtype == PSGD_F32) w.planes = take((size_t)tokens * up8(out) * 2 * 3);
     w.part = take(tile_part_bytes(in, out, w.tile));
     return w;
 }
@@ -508,8 +487,10 @@ int psgd_act_wgrad(void* workspace, void* stream, int64_t tokens, int64_t out_fe
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     bf16_t* x = reinterpret_cast<bf16_t*>(ws + w.x);
     bf16_t* planes = reinterpret_cast<bf16_t*>(ws + w.planes);
+    const bool restore = !w.tile.from_codes;
     if (tokens > 0) {
-        if (int rc = act_restore(stream, tokens, in_features, codes, ldc, scales, x, PSGD_BF16, w.ldx, false)) return rc;
+        if (restore)
+            if (int rc = act_restore(stream, tokens, in_features, codes, ldc, scales, x, PSGD_BF16, w.ldx, false)) return rc;
         if (dtype == PSGD_F32 && launch_planes(dy, dtype, tokens, out_features, ldy, planes, 3, st) != hipSuccess) return PSGD_E_HIP;
     }
     TileArgs t = {};
@@ -526,7 +507,8 @@ int psgd_act_wgrad(void* workspace, void* stream, int64_t tokens, int64_t out_fe
     o.dtype = g_dtype;
     o.accumulate = accumulate != 0;
     o.part = reinterpret_cast<float*>(ws + w.part);
-    return launch_product(false, w.tile.shape, t, o, st) == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+    const TileCodes from = {codes, ldc, scales, (int)((in_features + kGroup - 1) / kGroup)};
+    return (restore ? launch_product(false, w.tile.shape, t, o, st) : launch_code_product(from, t, o, st)) == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
 
 }  // extern "C"

@@ -381,7 +381,7 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
     if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
     p.pieces = (int)((tokens + p.piece - 1) / p.piece);
-    p.logits = tile_plan(s.vocab, p.piece, (p.ldc + kTileK - 1) / kTileK * p.n_pairs, false);
+    p.logits = tile_plan(s.vocab, p.piece, (p.ldc + kTileK - 1) / kTileK * p.n_pairs, false, 0);
     p.tiles = (int)((s.vocab + tile_p(p.logits.shape) - 1) / tile_p(p.logits.shape));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
     p.count = take(4);
@@ -396,8 +396,8 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
         const size_t elems = (size_t)p.piece * p.ldv;
         p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
         p.D = p.keep == KEEP_F16 ? p.e : take(elems * 2 * p.d_planes);
-        p.dx = tile_plan(s.d, p.piece, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, true);
-        p.dw = tile_plan(s.d, s.vocab, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, true);
+        p.dx = tile_plan(s.d, p.piece, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, true, 0);
+        p.dw = tile_plan(s.d, s.vocab, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, true, 0);
         p.part = take(std::max(tile_part_bytes(s.d, p.piece, p.dx), tile_part_bytes(s.d, s.vocab, p.dw)));
         p.sum = p.pieces > 1 && s.grad_dtype == PSGD_BF16 ? take((size_t)s.vocab * p.ldc * 4) : 0;
     }

@@ -51,8 +51,8 @@ __device__ inline TileSize tile_size(const TileArgs& t) {
     return s;
 }
 
-template <bool LKC, TileShape SHAPE, int KIND>
-__global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kernel(TileArgs t, TileOut o) {
+template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
+__global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kernel(TileArgs t, TileOut o, TileCodes codes) {
     extern __shared__ __align__(16) unsigned char smem[];
     using T = Tile<false, LKC, SHAPE>;
     const TileSize size = tile_size(t);
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kerne
     if (at.split < 0 || (size.K == 0 && o.skip_empty)) return;
     const int p0 = at.p * T::BP, l0 = at.l * T::BL, nl = size.nl;
     T tile;
-    tile.run(t, p0, l0, nl, size.K, at.split, grid.n_split, (PSGD_TLDS unsigned char*)smem);
+    tile.template run<false, CODES>(t, p0, l0, nl, size.K, at.split, grid.n_split, (PSGD_TLDS unsigned char*)smem, codes);
     const float scale = KIND != TILE_PART && o.scale ? *o.scale : 1.f;
     tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, auto& v) {
         const int l = l0 + row, c = p0 + col, n = t.P.extent - c;
@@ -135,7 +135,7 @@ constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel f
 
 // Shape and splits by an estimate in microseconds.  A workgroup takes A before and after its chunks and C per chunk: 256 x 256 11 and 1.65 (the matrix
 // cores' rate), 128 x 128 5 and 0.57, 128 x 64 4.5 and 0.45, one to a compute unit; TILE_MANY 5 and 1 with up to two to a compute unit, 0.52 for each
-// of three and four.  A split contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for
+// of three and four (0.7 where it makes the operand of codes).  A split contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for
 // each that a thread adds up.  Weight gradients tokens x out x in, each shape with its best number of splits, in us:
 //                    256 x 256   128 x 128   128 x 64   TILE_MANY
 //   1 x 4096 x 4096       20.9        29.8       39.5        15.7
@@ -147,27 +147,30 @@ constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel f
 //   1000 x 2048 x 2048    34.6        23.4       29.9        29.2
 //   9001 x 256 x 1032     33.3        28.9       31.7        29.7
 //   4096 x 512 x 512      29.8        21.4       19.7
-TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split) {
-    static const double A[TILE_SHAPES] = {11, 5, 4.5, 5}, C[TILE_SHAPES] = {1.65, 0.57, 0.45, 0.52};
-    TilePlan best = {TILE_256, 1};
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore) {
+    struct Way { TileShape shape; bool from_codes; double before, chunk; };
+    static const Way ways[] = {{TILE_256, false, 11, 1.65}, {TILE_128, false, 5, 0.57}, {TILE_THIN, false, 4.5, 0.45}, {TILE_MANY, false, 5, 0.52},
+                               {TILE_MANY, true, 5, 0.70}};
+    TilePlan best = {TILE_256, 1, false};
     double least = 1e300;
-    for (TileShape shape : {TILE_256, TILE_128, TILE_THIN, TILE_MANY}) {
-        const int64_t tiles = (extent_p + tile_p(shape) - 1) / tile_p(shape) * ((extent_l + tile_l(shape) - 1) / tile_l(shape));
+    for (const Way& way : ways) {
+        if (way.from_codes && !(restore > 0)) continue;
+        const int64_t p = tile_p(way.shape), l = tile_l(way.shape), tiles = (extent_p + p - 1) / p * ((extent_l + l - 1) / l);
         const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
         for (int64_t want : {(int64_t)1, fill / 4, fill / 2, fill, 2 * fill}) {
             if (want < 1 || (want > 1 && (!may_split || want > 64 || want > chunks))) continue;
             const int64_t share = (chunks + want - 1) / want, split = share > 0 ? (chunks + share - 1) / share : 1;
             const int64_t blocks = tiles * split;
-            double us;
-            if (shape == TILE_MANY) {
+            double us = way.from_codes ? 0 : restore;
+            if (way.shape == TILE_MANY) {
                 const int64_t last = (blocks % (4 * kUnits) + kUnits - 1) / kUnits;        // workgroups to a compute unit in the last round
-                us = (double)(blocks / (4 * kUnits)) * (A[shape] + share * 4 * C[shape]);
-                if (last > 0) us += A[shape] + share * std::max(1.0, last * C[shape]);
+                us += (double)(blocks / (4 * kUnits)) * (way.before + share * 4 * way.chunk);
+                if (last > 0) us += way.before + share * std::max(1.0, last * way.chunk);
             } else {
-                us = (double)((blocks + kUnits - 1) / kUnits) * (A[shape] + share * C[shape]);
+                us += (double)((blocks + kUnits - 1) / kUnits) * (way.before + share * way.chunk);
             }
             if (split > 1) us += 4 + 0.08 * split + split * (double)extent_p * (double)extent_l * 8e-6 / 8;
-            if (us < least) least = us, best = {shape, (int)split};
+            if (us < least) least = us, best = {way.shape, (int)split, way.from_codes};
         }
     }
     return best;
@@ -179,32 +182,35 @@ size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan)
     return plan.n_split > 1 ? up256((size_t)plan.n_split * rows * up8(extent_p) * sizeof(float)) : 0;
 }
 
-template <bool LKC, TileShape SHAPE, int KIND>
-static hipError_t launch_kind(const TileArgs& t, const TileOut& o, hipStream_t st) {
-    auto kfn = product_kernel<LKC, SHAPE, KIND>;
+template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
+static hipError_t launch_kind(const TileArgs& t, const TileOut& o, const TileCodes& codes, hipStream_t st) {
+    auto kfn = product_kernel<LKC, SHAPE, KIND, CODES>;
     constexpr int lds = Tile<false, LKC, SHAPE>::LDS_BYTES;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kfn, dim3(t.blocks), dim3(kTileThreads), lds, st, t, o);
+    hipLaunchKernelGGL(kfn, dim3(t.blocks), dim3(kTileThreads), lds, st, t, o, codes);
     return hipGetLastError();
 }
-template <bool LKC, TileShape SHAPE>
-static hipError_t launch_shape(TileArgs t, const TileOut& o, hipStream_t st) {
+template <bool LKC, TileShape SHAPE, bool CODES = false>
+static hipError_t launch_shape(TileArgs t, TileOut o, hipStream_t st, const TileCodes& codes = {}) {
+    if (t.n_split == 1) o.part = nullptr;
+    o.part_ld = up8(t.P.extent);
     const int64_t n_p = (t.P.extent + tile_p(SHAPE) - 1) / tile_p(SHAPE), n_l = (t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE);
     if (n_p * n_l * t.n_split > INT32_MAX) return hipErrorInvalidValue;
     t.blocks = (int)(n_p * n_l * t.n_split);
-    if (!o.part) return o.dtype == PSGD_F32 ? launch_kind<LKC, SHAPE, TILE_F32>(t, o, st) : launch_kind<LKC, SHAPE, TILE_BF16>(t, o, st);
-    hipError_t e = launch_kind<LKC, SHAPE, TILE_PART>(t, o, st);
+    if (!o.part) return o.dtype == PSGD_F32 ? launch_kind<LKC, SHAPE, TILE_F32, CODES>(t, o, codes, st) : launch_kind<LKC, SHAPE, TILE_BF16, CODES>(t, o, codes, st);
+    hipError_t e = launch_kind<LKC, SHAPE, TILE_PART, CODES>(t, o, codes, st);
     if (e != hipSuccess) return e;
     const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 3) / 4);
     hipLaunchKernelGGL(split_sum_kernel<SHAPE>, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
     return hipGetLastError();
 }
 
-hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& out, hipStream_t st) {
-    TileOut o = out;
-    if (t.n_split == 1) o.part = nullptr;
-    o.part_ld = up8(t.P.extent);
+hipError_t launch_code_product(const TileCodes& codes, const TileArgs& t, const TileOut& o, hipStream_t st) {
+    return launch_shape<false, TILE_MANY, true>(t, o, st, codes);
+}
+
+hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& o, hipStream_t st) {
     if (l_contiguous) {
         if (shape == TILE_256) return launch_shape<true, TILE_256>(t, o, st);
         if (shape == TILE_128) return launch_shape<true, TILE_128>(t, o, st);

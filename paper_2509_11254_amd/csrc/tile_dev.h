@@ -10,6 +10,7 @@
 // P runs along the accumulators' registers and L along the lanes, so that a lane holds four consecutive elements of a row of C,
 // and half a wavefront's 32 lanes 32 rows.
 #pragma once
+#include "act_dev.h"
 #include "train.h"
 
 namespace psgd {
@@ -296,8 +297,9 @@ struct Tile {
 
     // acc = the tile at (p0, l0), part `split` of n_split of the contraction over K steps; nl: rows of C there are.  MINUS_INF: what lies beyond P's
     // extent comes out as -inf, where sums begin that only get zeros added
-    template <bool MINUS_INF = false>
-    __device__ void run(const TileArgs& t, int p0, int l0, int nl, int K, int split, int n_split, PSGD_TLDS unsigned char* lds) {
+    template <bool MINUS_INF = false, bool CODES = false>
+    __device__ void run(const TileArgs& t, int p0, int l0, int nl, int K, int split, int n_split, PSGD_TLDS unsigned char* lds,
+                        const TileCodes& codes = {}) {
         lane = threadIdx.x & 63;
         const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wp = wv % WP;
@@ -313,7 +315,7 @@ struct Tile {
             }
         SideP sp;
         SideL sl;
-        sp.init(t.P, p0, t.P.extent, wv, lane);
+        if constexpr (!CODES) sp.init(t.P, p0, t.P.extent, wv, lane);
         sl.init(t.L, l0, nl, wv, lane);
         TileFragment<PKC, BP, BK> fp;
         TileFragment<LKC, BL, BK> fl;
@@ -326,7 +328,8 @@ struct Tile {
         if constexpr (FULL) {
             run_full(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         } else {
-            if constexpr (STAGES == 1) run_single(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
+            if constexpr (CODES) run_codes(t, codes, p0, l0, K, n0, n, per, wv, sl, fp, fl, lds);
+            else if constexpr (STAGES == 1) run_single(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
             else run_ring(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         }
     }
@@ -415,19 +418,68 @@ struct Tile {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            bf16x8 a0[FP], b0[FL], a1[FP], b1[FL];
-            read_ab<0>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
-            read_ab<1>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
-            multiply(a0, b0);
-            read_ab<2>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
-            multiply(a1, b1);
-            read_ab<3>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
-            multiply(a0, b0);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();       // every wave is done with the chunk
-            asm volatile("" ::: "memory");
-            multiply(a1, b1);
+            multiply_chunk(lds, fp, fl);
         }
+    }
+
+    // The same with P from an 8-bit checkpoint: a thread has 32 codes of a row, a group, at a time, the next chunk's while this one is multiplied, and
+    // writes their values to LDS where the direct loads would have put them (16-byte pieces in an order that spreads four rows over the banks).
+    __device__ __forceinline__ void run_codes(const TileArgs& t, const TileCodes& codes, int p0, int l0, int K, int n0, int n, int per, int wv, const SideL& sl,
+                                              const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl, PSGD_TLDS unsigned char* lds) {
+        static_assert(!PKC && BP == 128 && kTileThreads == 256, "32 codes per thread and chunk");
+        const int row = threadIdx.x >> 2, col = p0 + 32 * (threadIdx.x & 3);
+        PSGD_TLDS unsigned char* const to = lds + row * 2 * BP + (((threadIdx.x & 3) ^ SideP::turn(row)) << 6);
+        uintx2 w[4];            // pieces of eight codes, in the order in which they are written
+        float scale;
+        auto fetch = [&](int k0) {
+            const int k = k0 + row;
+            const bool in = k < K && col < t.P.extent;
+            const PSGD_GLOBAL signed char* const at = as_global(codes.codes) + (int64_t)k * codes.ldc + col;
+            scale = 0.f;
+            if (in) scale = __uint_as_float((unsigned)as_global(codes.scales)[k * (int64_t)codes.groups + (col >> 5)] << 23);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int piece = 8 * (j ^ (row & 3));
+                w[j] = uintx2{0u, 0u};
+                if (in && col + piece < t.P.extent) w[j] = *reinterpret_cast<const PSGD_GLOBAL uintx2*>(at + piece);
+            }
+        };
+        int pair = n0 / per, kc = n0 - pair * per;
+        fetch(kc * BK);
+        for (int it = 0; it < n; ++it) {
+            const unsigned which = t.pairs >> (4 * pair);
+            sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, true), lds + SideP::BYTES, wv);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[8];
+                values(ActCodes<2>{{w[j][0], w[j][1]}, scale}, v);
+                bf16x8 piece;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) piece[u] = (bf16_t)v[u];
+                *reinterpret_cast<PSGD_TLDS bf16x8*>(to + 16 * (j ^ (row & 3))) = piece;
+            }
+            if (++kc == per) { kc = 0; ++pair; }
+            if (it + 1 < n) fetch(kc * BK);
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            multiply_chunk(lds, fp, fl);
+        }
+    }
+    // a chunk that is in LDS; the barrier says that every wave is done with it
+    __device__ __forceinline__ void multiply_chunk(const PSGD_TLDS unsigned char* lds, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl) {
+        bf16x8 a0[FP], b0[FL], a1[FP], b1[FL];
+        read_ab<0>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
+        read_ab<1>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
+        multiply(a0, b0);
+        read_ab<2>(lds, lds + SideP::BYTES, fp, fl, a0, b0);
+        multiply(a1, b1);
+        read_ab<3>(lds, lds + SideP::BYTES, fp, fl, a1, b1);
+        multiply(a0, b0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        multiply(a1, b1);
     }
 
     // row of C and first of the four columns of quad q (0..3) of fragment (i, j), relative to the tile; values acc[i][j][4 q ..]

@@ -40,6 +40,14 @@ constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048, kPairs22 = 
 // three planes each, six products: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
 constexpr unsigned kPairs33 = 0x014852;
 
+// An 8-bit checkpoint in the place of P, K-strided: codes [K][ldc], scales [K][groups]
+struct TileCodes {
+    const signed char* codes;
+    int64_t ldc;
+    const unsigned char* scales;
+    int groups;
+};
+
 // Where a product goes: C row l to row `rows[first + l]` (or l), columns as they are
 struct TileOut {
     void* ptr;
@@ -54,11 +62,14 @@ struct TileOut {
 };
 
 // shape and number of parts of the contraction of a product: extents of C, chunks of the contraction (of all pairs of planes)
-struct TilePlan { TileShape shape; int n_split; };
-TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split);
+struct TilePlan { TileShape shape; int n_split; bool from_codes; };
+// restore: microseconds that P's values take to get from an 8-bit checkpoint to memory first (0: P is no checkpoint); from_codes: do without
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore);
 size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan);
 // C = L P^T over the operands' orientations: P K-strided, L K-contiguous or K-strided
 hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& o, hipStream_t st);
+// the same from a checkpoint: L K-strided, TILE_MANY
+hipError_t launch_code_product(const TileCodes& codes, const TileArgs& t, const TileOut& o, hipStream_t st);
 // rows x cols (ld) of fp32 or bf16 to `planes` bf16 planes [rows][round_up(cols, 8)], zeros beyond cols
 hipError_t launch_planes(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bf16_t* dst, int planes, hipStream_t st);
 
