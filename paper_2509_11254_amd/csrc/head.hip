@@ -32,6 +32,7 @@ struct HeadDev {
     float* scale;        // the largest c_t: D is kept relative to it and its products are multiplied by it
     int* rows;           // which they are
     int* label;          // and their labels
+    uint64_t* counts;    // or, where X is taken as it is, a bit for every token
     float2* stats;       // [token of the piece][tile]: maximum, sum of exponentials without the label's
     float* at_label;     // logit of the label, by token of the piece
     void* e;             // exponentials, [token of the piece][ldv]
@@ -41,12 +42,12 @@ struct HeadDev {
     int direct;          // X is taken where it is: the tokens of the piece are all tokens
 };
 
-__device__ inline bool counts(int64_t label, int vocab) { return label >= 0 && label < vocab; }
+__device__ inline bool label_counts(int64_t label, int vocab) { return label >= 0 && label < vocab; }
 // label of token l of the piece from `first` on; -1: it does not count
 __device__ __forceinline__ int label_of(const HeadDev& h, int first, int l) {
     if (!h.direct) return h.label[first + l];
     const int64_t y = h.labels[first + l];
-    return counts(y, h.vocab) ? (int)y : -1;
+    return label_counts(y, h.vocab) ? (int)y : -1;
 }
 
 // ---- tokens that count ----------------------------------------------------------------------------------------------
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
     const int first = blockIdx.x * per, last = min(h.tokens, first + per);
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     int mine = 0;
-    for (int i = threadIdx.x; i < first; i += kGatherThreads) mine += counts(h.labels[i], h.vocab) ? 1 : 0;
+    for (int i = threadIdx.x; i < first; i += kGatherThreads) mine += label_counts(h.labels[i], h.vocab) ? 1 : 0;
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) mine += __shfl_xor(mine, s);
     if (lane == 0) sum[wv] = mine;
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
     for (int t0 = first; t0 < last; t0 += kGatherThreads) {
         const int t = t0 + threadIdx.x;
         const int64_t y = t < last ? h.labels[t] : -1;
-        const bool in = counts(y, h.vocab);
+        const bool in = label_counts(y, h.vocab);
         const unsigned long long mask = __ballot(in);
         __syncthreads();
         if (lane == 0) sum[wv] = __popcll(mask);
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
         // a token that its model gives no probability is -1)
         float most = 0.f;
         if (h.weight)
-            for (int i = threadIdx.x; i < h.tokens; i += kGatherThreads) most = fmaxf(most, counts(h.labels[i], h.vocab) ? fabsf(h.weight[i]) : 0.f);
+            for (int i = threadIdx.x; i < h.tokens; i += kGatherThreads) most = fmaxf(most, label_counts(h.labels[i], h.vocab) ? fabsf(h.weight[i]) : 0.f);
 #pragma unroll
         for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
         __syncthreads();
@@ -281,6 +282,32 @@ __device__ __forceinline__ RowSum row_sum(const HeadDev& h, int l, float* shared
     return {m, s};
 }
 
+// Where no launch before has looked at the labels: the largest weight of a token that counts, or one over their number (see head_gather_kernel).
+// write: their bits as well
+__device__ __forceinline__ float direct_scale(const HeadDev& h, float* shared, bool write) {
+    float x = 0.f;
+    for (int i0 = 0; i0 < h.tokens; i0 += kThreads) {
+        const int i = i0 + threadIdx.x;
+        const bool in = i < h.tokens && label_counts(h.labels[i], h.vocab);
+        if (in) x = h.weight ? fmaxf(x, fabsf(h.weight[i])) : x + 1.f;
+        const uint64_t bits = __ballot(in);
+        if (write && (threadIdx.x & 63) == 0 && i < h.tokens) h.counts[i >> 6] = bits;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const float o = __shfl_xor(x, d);
+        x = h.weight ? fmaxf(x, o) : x + o;
+    }
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = shared[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) x = h.weight ? fmaxf(x, shared[w]) : x + shared[w];
+    __syncthreads();
+    if (!h.weight) return 1.f / fmaxf(x, 1.f);
+    return x > 0.f && x < __builtin_inff() ? x : 1.f;
+}
+
 // block: one token's row, blockIdx.y its part of the vocabulary; without gradients one part and no D
 template <int KEEP, int PL>
 __global__ __launch_bounds__(kThreads) void head_rows_kernel(HeadDev h, int first, int most_rows, int span) {
@@ -288,34 +315,54 @@ __global__ __launch_bounds__(kThreads) void head_rows_kernel(HeadDev h, int firs
     const int l = blockIdx.x;
     if (l >= (h.direct ? most_rows : min(most_rows, *h.count - first))) return;
     const int token = h.direct ? first + l : h.rows[first + l], y = label_of(h, first, l);
+    const int end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
+    float scale = 1.f;
+    if (KEEP != KEEP_NONE && h.direct && (h.weight || (l == 0 && blockIdx.y == 0))) {
+        const bool write = l == 0 && blockIdx.y == 0;
+        scale = direct_scale(h, shared, write);
+        if (write && threadIdx.x == 0) *h.scale = scale;
+    }
     if (y < 0) {
         if (blockIdx.y == 0 && threadIdx.x == 0) h.loss[token] = 0.f;
+        if constexpr (KEEP != KEEP_NONE)
+            for (int v = blockIdx.y * span + 8 * threadIdx.x; v < end; v += 8 * kThreads)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL uintx4*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = uintx4{0u, 0u, 0u, 0u};
         return;
     }
+    // exponentials are read ahead (for the last time: the hint takes 8192 x 4096 x 64000 from 10.0 to 9.93 ms)
+    uintx4 e[KEEP == KEEP_F32 ? 2 : 1];
+    auto fetch = [&](int v) {
+        if constexpr (KEEP == KEEP_F16) {
+            e[0] = __builtin_nontemporal_load(reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global((_Float16*)h.e) + l * h.ldv + v));
+        } else if constexpr (KEEP == KEEP_F32) {
+            const PSGD_GLOBAL uintx4* p = reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global((float*)h.e) + l * h.ldv + v);
+            e[0] = __builtin_nontemporal_load(p), e[1] = __builtin_nontemporal_load(p + 1);
+        }
+    };
+    const int start = blockIdx.y * span + 8 * threadIdx.x;
+    if (KEEP != KEEP_NONE && start < end) fetch(start);
     const RowSum r = row_sum(h, l, shared);
     const float at_label = h.at_label[l], e_label = expf(at_label - r.most), total = r.others + e_label;
     // log(1 + others / label's) keeps the loss of a token that is all but certain, which the difference of two logits does not
     if (blockIdx.y == 0 && threadIdx.x == 0)
         h.loss[token] = r.others < e_label ? log1pf(r.others / e_label) : r.most - at_label + logf(total);
     if constexpr (KEEP == KEEP_NONE) return;
-    const float c = (h.weight ? h.weight[token] / *h.scale : 1.f) / total;
+    const float c = (h.weight ? h.weight[token] / (h.direct ? scale : *h.scale) : 1.f) / total;
     const float d_label = -r.others * c;        // (p - 1 as the sum of the other probabilities)
-    const int end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
-    for (int v = blockIdx.y * span + 8 * threadIdx.x; v < end; v += 8 * kThreads) {
+    for (int v = start; v < end; v += 8 * kThreads) {
         const float most = h.stats[(int64_t)l * h.tiles + v / h.tile_width].x;
         const float f = expf(most - r.most) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
         float x[8];
         if constexpr (KEEP == KEEP_F16) {
-            // (read for the last time: 10.0 -> 9.93 ms for 8192 x 4096 x 64000)
-            const halfx8 e = __builtin_nontemporal_load(reinterpret_cast<const PSGD_GLOBAL halfx8*>(as_global((_Float16*)h.e) + l * h.ldv + v));
+            const halfx8 q = __builtin_bit_cast(halfx8, e[0]);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = (float)e[u] * f;
+            for (int u = 0; u < 8; ++u) x[u] = (float)q[u] * f;
         } else {
-            const PSGD_GLOBAL floatx4* e = reinterpret_cast<const PSGD_GLOBAL floatx4*>(as_global((float*)h.e) + l * h.ldv + v);
-            const floatx4 a = __builtin_nontemporal_load(e), b = __builtin_nontemporal_load(e + 1);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { x[u] = a[u] * f; x[u + 4] = b[u] * f; }
+            for (int u = 0; u < 8; ++u) x[u] = __uint_as_float(e[KEEP == KEEP_F32 ? u >> 2 : 0][u & 3]) * f;
         }
+        if (v + 8 * kThreads < end) fetch(v + 8 * kThreads);
         bf16x8 out[PL];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -346,17 +393,20 @@ __global__ __launch_bounds__(kThreads) void head_round_kernel(const float* sum, 
 
 // ---- host --------------------------------------------------------------------------------------------------------------
 
+// (Loss and gradients, tokens x d x vocab, in us: 1 x 512 x 4400 35.5 -> 26.5, 512 x 512 x 4400 56.5 -> 47, 500 x 1024 x 10008 87.7 -> 81.  The products take all tokens then:
+// not where there may be many that do not count.)
+constexpr int64_t kDirectTokens = 512;
 constexpr size_t kPieceBytes = (size_t)1 << 30;     // what is kept of one piece of the tokens: exponentials and D, or statistics alone
 
 struct HeadPlan {
     size_t bytes = 0;
-    size_t count, scale, rows, label, xc, wc, stats, at_label, e, D, part, sum;
+    size_t count, scale, rows, label, counts, xc, wc, stats, at_label, e, D, part, dw_part, sum;
     int64_t ldc, ldv;
     int piece, pieces, tiles, x_planes, w_planes, d_planes, keep;
     TilePlan logits, dx, dw;
     unsigned pairs, dx_pairs, dw_pairs;
     int n_pairs, n_dx_pairs, n_dw_pairs;
-    bool copy_w;
+    bool copy_w, direct, pair;
 };
 
 static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
@@ -381,6 +431,9 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
     if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
     p.pieces = (int)((tokens + p.piece - 1) / p.piece);
+    // Few tokens: X is taken where it is, and those that do not count are sorted out by their labels -- losses of one tile of rows, where they cost
+    // nothing; gradients of up to kDirectTokens, whose launches are all there is to save.
+    p.direct = !p.copy_w && p.pieces == 1 && s.tokens > 0 && s.tokens <= (gradients ? kDirectTokens : tile_l(TILE_THIN));
     p.logits = tile_plan(s.vocab, p.piece, (p.ldc + kTileK - 1) / kTileK * p.n_pairs, false, 0);
     p.tiles = (int)((s.vocab + tile_p(p.logits.shape) - 1) / tile_p(p.logits.shape));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
@@ -388,7 +441,8 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.scale = take(4);
     p.rows = take((size_t)tokens * 4);
     p.label = take((size_t)tokens * 4);
-    p.xc = take((size_t)tokens * p.ldc * 2 * p.x_planes);
+    p.counts = take((size_t)(tokens + 63) / 64 * 8);
+    p.xc = p.direct ? 0 : take((size_t)tokens * p.ldc * 2 * p.x_planes);
     p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2 * p.w_planes) : 0;
     p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
     p.at_label = take((size_t)p.piece * 4);
@@ -396,9 +450,18 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
         const size_t elems = (size_t)p.piece * p.ldv;
         p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
         p.D = p.keep == KEEP_F16 ? p.e : take(elems * 2 * p.d_planes);
-        p.dx = tile_plan(s.d, p.piece, (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, true, 0);
-        p.dw = tile_plan(s.d, s.vocab, (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs, true, 0);
-        p.part = take(std::max(tile_part_bytes(s.d, p.piece, p.dx), tile_part_bytes(s.d, s.vocab, p.dw)));
+        const int64_t dx_chunks = (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, dw_chunks = (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs;
+        p.dx = tile_plan(s.d, p.piece, dx_chunks, true, 0);
+        p.dw = tile_plan(s.d, s.vocab, dw_chunks, true, 0, p.direct);
+        if (p.pieces == 1 && s.tokens > 0 && p.dw.shape == TILE_MANY) {
+            const TilePlan many = tile_plan(s.d, p.piece, dx_chunks, true, 0, true);
+            const int64_t wide = (s.d + 127) / 128;
+            p.pair = pair_pays({many, s.d, p.piece, wide * ((p.piece + 127) / 128), dx_chunks}, {p.dw, s.d, s.vocab, wide * ((s.vocab + 127) / 128), dw_chunks}, p.dx);
+            if (p.pair) p.dx = many;
+        }
+        p.part = take(tile_part_bytes(s.d, p.piece, p.dx));
+        p.dw_part = p.pair ? take(tile_part_bytes(s.d, s.vocab, p.dw)) : p.part;
+        if (!p.pair && tile_part_bytes(s.d, s.vocab, p.dw) > tile_part_bytes(s.d, p.piece, p.dx)) p.bytes = p.part + tile_part_bytes(s.d, s.vocab, p.dw);
         p.sum = p.pieces > 1 && s.grad_dtype == PSGD_BF16 ? take((size_t)s.vocab * p.ldc * 4) : 0;
     }
     return p;
@@ -416,8 +479,10 @@ static hipError_t launch_logits_as(const TileArgs& t, const HeadDev& h, hipStrea
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     auto kfn = head_logits_kernel<SHAPE, KEEP>;
     constexpr int lds = Tile<true, true, SHAPE>::LDS_BYTES;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
+    if (lds > 48 * 1024) {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(kTileThreads), lds, st, t, h);
     return hipGetLastError();
 }
@@ -470,6 +535,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     h.scale = reinterpret_cast<float*>(ws + p.scale);
     h.rows = reinterpret_cast<int*>(ws + p.rows);
     h.label = reinterpret_cast<int*>(ws + p.label);
+    h.counts = reinterpret_cast<uint64_t*>(ws + p.counts);
     h.stats = reinterpret_cast<float2*>(ws + p.stats);
     h.at_label = reinterpret_cast<float*>(ws + p.at_label);
     h.e = ws + p.e;
@@ -480,9 +546,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     const bf16_t* wc = static_cast<const bf16_t*>(w);
     int64_t ldwc = ldw, w_plane = 0;
 
-    // Losses of a few tokens: nothing is gained by leaving out the ones that do not count, and a row of logits only depends on its token.
-    // (One token, 4096 x 32000: 60 -> 55 us.)
-    h.direct = !gradients && !p.copy_w && s->tokens <= tile_l(TILE_THIN);
+    h.direct = p.direct;
     // at most 1024 blocks, each of which reads the labels before its own
     const int per = std::max(16, (int)((s->tokens + 1023) / 1024));
     const dim3 blocks((unsigned)std::max<int64_t>(1, (s->tokens + per - 1) / per));
@@ -497,39 +561,44 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     }
     for (int piece = 0; piece < p.pieces; ++piece) {
         const int first = piece * p.piece, rows = (int)std::min<int64_t>(p.piece, s->tokens - first);
-        const bf16_t* xp = xc + (int64_t)first * p.ldc;
-        const int64_t x_plane = s->tokens * p.ldc;
+        const TileOperand tokens = h.direct ? TileOperand{static_cast<const bf16_t*>(x) + (int64_t)first * ldx, ldx, 0, rows}
+                                            : TileOperand{xc + (int64_t)first * p.ldc, p.ldc, s->tokens * p.ldc, rows};
         TileArgs t = {};
         t.count = h.direct ? nullptr : h.count, t.first = first, t.n_split = 1;
         if (rows > 0) {
             t.P = {wc, ldwc, w_plane, (int)s->vocab};
-            if (h.direct) t.L = {(const bf16_t*)x + (int64_t)first * ldx, ldx, 0, rows};
-            else t.L = {xp, p.ldc, x_plane, rows};
+            t.L = tokens;
             t.K = (int)p.ldc;
             t.pairs = p.pairs, t.n_pairs = p.n_pairs;
             if (launch_logits(t, h, p.logits.shape, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
         }
         if (!gradients) continue;
-        TileOut o = {};
-        o.part = reinterpret_cast<float*>(ws + p.part);
-        o.scale = h.scale;
-        if (rows > 0) {
-            t.P = {wc, ldwc, w_plane, (int)s->d};
-            t.L = {h.D, p.ldv, h.d_plane, rows};
-            t.K = (int)s->vocab;
-            t.pairs = p.dx_pairs, t.n_pairs = p.n_dx_pairs, t.n_split = p.dx.n_split;
-            o.ptr = dx, o.ld = lddx, o.dtype = s->dtype, o.rows = h.rows;
-            if (launch_product(true, p.dx.shape, t, o, st) != hipSuccess) return PSGD_E_HIP;
+        TileArgs tx = t, tw = t;
+        TileOut ox = {}, ow = {};
+        ox.scale = ow.scale = h.scale;
+        tx.P = {wc, ldwc, w_plane, (int)s->d};
+        tx.L = {h.D, p.ldv, h.d_plane, rows};
+        tx.K = (int)s->vocab;
+        tx.pairs = p.dx_pairs, tx.n_pairs = p.n_dx_pairs, tx.n_split = p.dx.n_split;
+        ox.part = reinterpret_cast<float*>(ws + p.part);
+        ox.ptr = dx, ox.ld = lddx, ox.dtype = s->dtype;
+        tw.P = tokens;
+        tw.P.extent = (int)s->d;
+        tw.L = {h.D, p.ldv, h.d_plane, (int)s->vocab};
+        tw.K = rows, tw.count_is_k = 1;
+        tw.pairs = p.dw_pairs, tw.n_pairs = p.n_dw_pairs, tw.n_split = p.dw.n_split;
+        ow.part = reinterpret_cast<float*>(ws + p.dw_part);
+        if (h.direct) ox.tokens = tw.steps = h.counts;
+        else ox.rows = h.rows;
+        if (p.sum) { ow.ptr = ws + p.sum; ow.ld = p.ldc; ow.dtype = PSGD_F32; ow.accumulate = piece > 0; }
+        else { ow.ptr = dw; ow.ld = lddw; ow.dtype = s->grad_dtype; ow.accumulate = piece > 0 || accumulate; }
+        ow.skip_empty = ow.accumulate;
+        if (p.pair) {
+            if (launch_pair(tx, ox, tw, ow, st) != hipSuccess) return PSGD_E_HIP;
+        } else {
+            if (rows > 0 && launch_product(true, p.dx.shape, tx, ox, st) != hipSuccess) return PSGD_E_HIP;
+            if (launch_product(false, p.dw.shape, tw, ow, st) != hipSuccess) return PSGD_E_HIP;
         }
-        t.P = {xp, p.ldc, x_plane, (int)s->d};
-        t.L = {h.D, p.ldv, h.d_plane, (int)s->vocab};
-        t.K = rows, t.count_is_k = 1;
-        t.pairs = p.dw_pairs, t.n_pairs = p.n_dw_pairs, t.n_split = p.dw.n_split;
-        o.rows = nullptr;
-        if (p.sum) { o.ptr = ws + p.sum; o.ld = p.ldc; o.dtype = PSGD_F32; o.accumulate = piece > 0; }
-        else { o.ptr = dw; o.ld = lddw; o.dtype = s->grad_dtype; o.accumulate = piece > 0 || accumulate; }
-        o.skip_empty = o.accumulate;
-        if (launch_product(false, p.dw.shape, t, o, st) != hipSuccess) return PSGD_E_HIP;
     }
     if (gradients && p.sum) {
         hipLaunchKernelGGL(head_round_kernel, dim3(2048), dim3(kThreads), 0, st, (const float*)(ws + p.sum), s->vocab, (int)s->d, p.ldc, (bf16_t*)dw, lddw, accumulate);

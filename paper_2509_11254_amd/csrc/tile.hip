@@ -51,32 +51,47 @@ __device__ inline TileSize tile_size(const TileArgs& t) {
     return s;
 }
 
+// workgroup `id` of a product
 template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
-__global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kernel(TileArgs t, TileOut o, TileCodes codes) {
-    extern __shared__ __align__(16) unsigned char smem[];
+__device__ __forceinline__ void product_tile(int id, const TileArgs& t, const TileOut& o, const TileCodes& codes, PSGD_TLDS unsigned char* lds) {
     using T = Tile<false, LKC, SHAPE>;
     const TileSize size = tile_size(t);
     const TileGrid grid = tile_grid<SHAPE>(t, size.nl, size.chunks);
-    const TilePlace at = tile_place(blockIdx.x, grid);
+    const TilePlace at = tile_place(id, grid);
     if (at.split < 0 || (size.K == 0 && o.skip_empty)) return;
     const int p0 = at.p * T::BP, l0 = at.l * T::BL, nl = size.nl;
     T tile;
-    tile.template run<false, CODES>(t, p0, l0, nl, size.K, at.split, grid.n_split, (PSGD_TLDS unsigned char*)smem, codes);
+    tile.template run<false, CODES>(t, p0, l0, nl, size.K, at.split, grid.n_split, lds, codes);
     const float scale = KIND != TILE_PART && o.scale ? *o.scale : 1.f;
-    tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>((PSGD_TLDS unsigned char*)smem, [&](int row, int col, auto& v) {
+    tile.template for_rows<KIND == TILE_BF16 ? 8 : 4>(lds, [&](int row, int col, auto& v) {
         const int l = l0 + row, c = p0 + col, n = t.P.extent - c;
         if (l >= nl || n <= 0) return;
         if constexpr (KIND == TILE_PART) {
             PSGD_GLOBAL float* p = as_global(o.part) + ((int64_t)at.split * nl + l) * o.part_ld + c;
             *reinterpret_cast<PSGD_GLOBAL floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
         } else {
+            const bool in = token_counts(o.tokens, l);
 #pragma unroll
-            for (int u = 0; u < (KIND == TILE_BF16 ? 8 : 4); ++u) v[u] *= scale;
+            for (int u = 0; u < (KIND == TILE_BF16 ? 8 : 4); ++u) v[u] = in ? v[u] * scale : 0.f;
             const int64_t to = (o.rows ? o.rows[t.first + l] : l) * o.ld + c;
             if constexpr (KIND == TILE_F32) store_row(as_global((float*)o.ptr) + to, v, n, o.accumulate);
             else store_row(as_global((bf16_t*)o.ptr) + to, v, n, o.accumulate);
         }
     });
+}
+
+template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
+__global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void product_kernel(TileArgs t, TileOut o, TileCodes codes) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    product_tile<LKC, SHAPE, KIND, CODES>(blockIdx.x, t, o, codes, (PSGD_TLDS unsigned char*)smem);
+}
+
+// two products that do not depend on each other: together they fill the card better, and one launch is saved
+template <int KIND_A, int KIND_B>
+__global__ __launch_bounds__(kTileThreads, tile_share(TILE_MANY)) void pair_kernel(TileArgs ta, TileOut oa, TileArgs tb, TileOut ob) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if ((int)blockIdx.x < ta.blocks) product_tile<true, TILE_MANY, KIND_A, false>(blockIdx.x, ta, oa, {}, (PSGD_TLDS unsigned char*)smem);
+    else product_tile<false, TILE_MANY, KIND_B, false>(blockIdx.x - ta.blocks, tb, ob, {}, (PSGD_TLDS unsigned char*)smem);
 }
 
 // sum over the splits, in their order, of four elements per thread
@@ -101,7 +116,8 @@ __global__ __launch_bounds__(kThreads) void split_sum_kernel(TileArgs t, TileOut
             for (int u = 0; u < 8; ++u) s += x[u];
         }
         for (; k < n_split; ++k) s += *reinterpret_cast<const PSGD_GLOBAL floatx4*>(p + k * layer);
-        const float v[4] = {s[0] * scale, s[1] * scale, s[2] * scale, s[3] * scale};
+        const float c0 = token_counts(o.tokens, l) ? scale : 0.f;
+        const float v[4] = {c0 != 0.f ? s[0] * c0 : 0.f, c0 != 0.f ? s[1] * c0 : 0.f, c0 != 0.f ? s[2] * c0 : 0.f, c0 != 0.f ? s[3] * c0 : 0.f};
         const int64_t row = o.rows ? o.rows[t.first + l] : l;
         if (o.dtype == PSGD_F32) store_row(as_global((float*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
         else store_row(as_global((bf16_t*)o.ptr) + row * o.ld + c, v, t.P.extent - c, o.accumulate);
@@ -133,8 +149,12 @@ __global__ __launch_bounds__(kThreads) void planes_kernel(const T* src, int64_t 
 
 constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel fills one
 
+static double split_us(int split, int64_t extent_p, int64_t extent_l) {
+    return split > 1 ? 4 + 0.08 * split + split * (double)extent_p * (double)extent_l * 8e-6 / 8 : 0;
+}
+
 // Shape and splits by an estimate in microseconds.  A workgroup takes A before and after its chunks and C per chunk: 256 x 256 11 and 1.65 (the matrix
-// cores' rate), 128 x 128 5 and 0.57, 128 x 64 4.5 and 0.45, one to a compute unit; TILE_MANY 5 and 1 with up to two to a compute unit, 0.52 for each
+// cores' rate), 128 x 128 5 and 0.6, 128 x 64 4.5 and 0.45, one to a compute unit; TILE_MANY 5 and 1 with up to two to a compute unit, 0.52 for each
 // of three and four (0.7 where it makes the operand of codes).  A split contraction costs a launch (4), its partial sums written and read at 8 TB/s (they stay in the caches), and 0.08 for
 // each that a thread adds up.  Weight gradients tokens x out x in, each shape with its best number of splits, in us:
 //                    256 x 256   128 x 128   128 x 64   TILE_MANY
@@ -147,14 +167,13 @@ constexpr int kUnits = 256;     // compute units; a workgroup of a tile kernel f
 //   1000 x 2048 x 2048    34.6        23.4       29.9        29.2
 //   9001 x 256 x 1032     33.3        28.9       31.7        29.7
 //   4096 x 512 x 512      29.8        21.4       19.7
-TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore) {
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore, bool only_many) {
     struct Way { TileShape shape; bool from_codes; double before, chunk; };
-    static const Way ways[] = {{TILE_256, false, 11, 1.65}, {TILE_128, false, 5, 0.57}, {TILE_THIN, false, 4.5, 0.45}, {TILE_MANY, false, 5, 0.52},
+    static const Way ways[] = {{TILE_256, false, 11, 1.65}, {TILE_128, false, 5, 0.6}, {TILE_THIN, false, 4.5, 0.45}, {TILE_MANY, false, 5, 0.52},
                                {TILE_MANY, true, 5, 0.70}};
-    TilePlan best = {TILE_256, 1, false};
-    double least = 1e300;
+    TilePlan best = {only_many ? TILE_MANY : TILE_256, 1, false, 1e300};
     for (const Way& way : ways) {
-        if (way.from_codes && !(restore > 0)) continue;
+        if ((way.from_codes && !(restore > 0)) || (only_many && way.shape != TILE_MANY)) continue;
         const int64_t p = tile_p(way.shape), l = tile_l(way.shape), tiles = (extent_p + p - 1) / p * ((extent_l + l - 1) / l);
         const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
         for (int64_t want : {(int64_t)1, fill / 4, fill / 2, fill, 2 * fill}) {
@@ -165,15 +184,27 @@ TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_
             if (way.shape == TILE_MANY) {
                 const int64_t last = (blocks % (4 * kUnits) + kUnits - 1) / kUnits;        // workgroups to a compute unit in the last round
                 us += (double)(blocks / (4 * kUnits)) * (way.before + share * 4 * way.chunk);
-                if (last > 0) us += way.before + share * std::max(1.0, last * way.chunk);
+                if (last > 0) us += way.before + share * std::max(way.from_codes ? 1.3 : 1.0, last * way.chunk);
             } else {
                 us += (double)((blocks + kUnits - 1) / kUnits) * (way.before + share * way.chunk);
             }
-            if (split > 1) us += 4 + 0.08 * split + split * (double)extent_p * (double)extent_l * 8e-6 / 8;
-            if (us < least) least = us, best = {way.shape, (int)split, way.from_codes};
+            us += split_us((int)split, extent_p, extent_l);
+            if (us < best.us) best = {way.shape, (int)split, way.from_codes, us};
         }
     }
     return best;
+}
+
+// Both products' workgroups fill the compute units together and take as long as the longer contraction; a launch less (3 us).  (Gradients of the head, tokens x d x
+// vocab, in us without the pair and with it: 16 x 512 x 4400 32.0, 26.7; 512 x 512 x 4400 54.6, 47.5; 128 x 1024 x 10008 46.0, 39.7; what is not paired by this rule,
+// 200 x 1024 x 10008, was 57.2 and 59.)
+bool pair_pays(const TilePair& a, const TilePair& b, const TilePlan& a_alone) {
+    const int64_t blocks = a.tiles * a.plan.n_split + b.tiles * b.plan.n_split, rounds = (blocks + 4 * kUnits - 1) / (4 * kUnits);
+    const int64_t share = std::max((a.chunks + a.plan.n_split - 1) / a.plan.n_split, (b.chunks + b.plan.n_split - 1) / b.plan.n_split);
+    const double to_a_unit = (double)std::min<int64_t>(4, (blocks + kUnits - 1) / kUnits);
+    const double pair = rounds * (5 + share * std::max(1.0, 0.52 * to_a_unit)) + split_us(a.plan.n_split, a.extent_p, a.extent_l) +
+                        split_us(b.plan.n_split, b.extent_p, b.extent_l);
+    return pair < a_alone.us + b.plan.us + 3;
 }
 
 size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan) {
@@ -186,24 +217,63 @@ template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
 static hipError_t launch_kind(const TileArgs& t, const TileOut& o, const TileCodes& codes, hipStream_t st) {
     auto kfn = product_kernel<LKC, SHAPE, KIND, CODES>;
     constexpr int lds = Tile<false, LKC, SHAPE>::LDS_BYTES;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
+    if (lds > 48 * 1024) {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(kfn, dim3(t.blocks), dim3(kTileThreads), lds, st, t, o, codes);
+    return hipGetLastError();
+}
+// what a launch needs to know of a product
+template <TileShape SHAPE>
+static hipError_t complete(TileArgs& t, TileOut& o) {
+    if (t.n_split == 1) o.part = nullptr;
+    o.part_ld = up8(t.P.extent);
+    const int64_t n_p = (t.P.extent + tile_p(SHAPE) - 1) / tile_p(SHAPE), n_l = (t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE);
+    if (n_p * n_l * t.n_split > INT32_MAX / 2) return hipErrorInvalidValue;
+    t.blocks = (int)(n_p * n_l * t.n_split);
+    return hipSuccess;
+}
+template <TileShape SHAPE>
+static hipError_t launch_sum(const TileArgs& t, const TileOut& o, hipStream_t st) {
+    if (!o.part) return hipSuccess;
+    const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 3) / 4);
+    hipLaunchKernelGGL(split_sum_kernel<SHAPE>, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
     return hipGetLastError();
 }
 template <bool LKC, TileShape SHAPE, bool CODES = false>
 static hipError_t launch_shape(TileArgs t, TileOut o, hipStream_t st, const TileCodes& codes = {}) {
-    if (t.n_split == 1) o.part = nullptr;
-    o.part_ld = up8(t.P.extent);
-    const int64_t n_p = (t.P.extent + tile_p(SHAPE) - 1) / tile_p(SHAPE), n_l = (t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE);
-    if (n_p * n_l * t.n_split > INT32_MAX) return hipErrorInvalidValue;
-    t.blocks = (int)(n_p * n_l * t.n_split);
-    if (!o.part) return o.dtype == PSGD_F32 ? launch_kind<LKC, SHAPE, TILE_F32, CODES>(t, o, codes, st) : launch_kind<LKC, SHAPE, TILE_BF16, CODES>(t, o, codes, st);
-    hipError_t e = launch_kind<LKC, SHAPE, TILE_PART, CODES>(t, o, codes, st);
+    hipError_t e = complete<SHAPE>(t, o);
     if (e != hipSuccess) return e;
-    const int64_t pieces = (int64_t)t.L.extent * ((t.P.extent + 3) / 4);
-    hipLaunchKernelGGL(split_sum_kernel<SHAPE>, dim3((unsigned)std::min<int64_t>((pieces + kThreads - 1) / kThreads, 8 * kUnits)), dim3(kThreads), 0, st, t, o);
+    if (!o.part) return o.dtype == PSGD_F32 ? launch_kind<LKC, SHAPE, TILE_F32, CODES>(t, o, codes, st) : launch_kind<LKC, SHAPE, TILE_BF16, CODES>(t, o, codes, st);
+    e = launch_kind<LKC, SHAPE, TILE_PART, CODES>(t, o, codes, st);
+    return e != hipSuccess ? e : launch_sum<SHAPE>(t, o, st);
+}
+
+template <int KIND_A, int KIND_B>
+static hipError_t launch_pair_as(const TileArgs& ta, const TileOut& oa, const TileArgs& tb, const TileOut& ob, hipStream_t st) {
+    auto kfn = pair_kernel<KIND_A, KIND_B>;
+    constexpr int lds = Tile<false, false, TILE_MANY>::LDS_BYTES;
+    static_assert(lds == Tile<false, true, TILE_MANY>::LDS_BYTES, "one size for both");
+    static_assert(lds <= 48 * 1024, "no attribute");
+    hipLaunchKernelGGL(kfn, dim3(ta.blocks + tb.blocks), dim3(kTileThreads), lds, st, ta, oa, tb, ob);
     return hipGetLastError();
+}
+template <int KIND_A>
+static hipError_t launch_pair_from(const TileArgs& ta, const TileOut& oa, const TileArgs& tb, const TileOut& ob, hipStream_t st) {
+    if (ob.part) return launch_pair_as<KIND_A, TILE_PART>(ta, oa, tb, ob, st);
+    return ob.dtype == PSGD_F32 ? launch_pair_as<KIND_A, TILE_F32>(ta, oa, tb, ob, st) : launch_pair_as<KIND_A, TILE_BF16>(ta, oa, tb, ob, st);
+}
+hipError_t launch_pair(const TileArgs& first, const TileOut& first_out, const TileArgs& second, const TileOut& second_out, hipStream_t st) {
+    TileArgs ta = first, tb = second;
+    TileOut oa = first_out, ob = second_out;
+    hipError_t e = complete<TILE_MANY>(ta, oa);
+    if (e == hipSuccess) e = complete<TILE_MANY>(tb, ob);
+    if (e != hipSuccess) return e;
+    e = oa.part ? launch_pair_from<TILE_PART>(ta, oa, tb, ob, st)
+                : oa.dtype == PSGD_F32 ? launch_pair_from<TILE_F32>(ta, oa, tb, ob, st) : launch_pair_from<TILE_BF16>(ta, oa, tb, ob, st);
+    if (e == hipSuccess) e = launch_sum<TILE_MANY>(ta, oa, st);
+    return e != hipSuccess ? e : launch_sum<TILE_MANY>(tb, ob, st);
 }
 
 hipError_t launch_code_product(const TileCodes& codes, const TileArgs& t, const TileOut& o, hipStream_t st) {

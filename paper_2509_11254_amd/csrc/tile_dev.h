@@ -55,6 +55,8 @@ __device__ inline TilePlace tile_place(int id, const TileGrid& g) {
     return at;
 }
 
+__device__ __forceinline__ bool token_counts(TileTokens tokens, int i) { return !tokens || ((as_global(tokens)[i >> 6] >> (i & 63)) & 1); }
+
 // a value that is the same in all lanes, in a scalar register
 __device__ __forceinline__ unsigned scalar(unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); }
 
@@ -108,6 +110,22 @@ struct TileSide {
         // before each instruction of its own that takes it, of which these kernels have none.)
         const unsigned to = scalar((unsigned)(uintptr_t)(dst + (I * NW + wv) * 1024));
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(s.rsrc));
+    }
+    // K-strided: all loads of the chunk from step k0 on, without the steps that do not count
+    __device__ __forceinline__ void load_counted(const Source& s, PSGD_TLDS unsigned char* dst, int wv, int lane, TileTokens tokens, int k0) {
+        constexpr int LANES = E / 8, ROWS = 64 / LANES;
+        static_assert(BK == 64, "one word of bits");
+        const uint64_t counts = as_global(tokens)[k0 >> 6];
+        unsigned kept[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int k = (i * NW + wv) * ROWS + lane / LANES;
+            kept[i] = off[i];
+            off[i] = (counts >> k) & 1 ? off[i] : kOutside;
+        }
+        load_all(s, dst, wv);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) off[i] = kept[i];
     }
     __device__ __forceinline__ void load_all(const Source& s, PSGD_TLDS unsigned char* dst, int wv) const {
         load<0>(s, dst, wv);
@@ -406,14 +424,20 @@ struct Tile {
     }
 
     // One chunk in LDS: nothing of this workgroup goes on while it loads; the others of the compute unit do.
-    __device__ __forceinline__ void run_single(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
+    __device__ __forceinline__ void run_single(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, SideP& sp,
                                                const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
                                                PSGD_TLDS unsigned char* lds) {
         int pair = n0 / per, kc = n0 - pair * per;
         for (int it = 0; it < n; ++it) {
             const unsigned which = t.pairs >> (4 * pair);
-            sp.load_all(SideP::source(t.P, which & 3, p0, kc * BK, K, true), lds, wv);
+            const auto from_p = SideP::source(t.P, which & 3, p0, kc * BK, K, true);
             sl.load_all(SideL::source(t.L, (which >> 2) & 3, l0, kc * BK, K, true), lds + SideP::BYTES, wv);
+            if constexpr (!PKC && !LKC) {
+                if (t.steps) sp.load_counted(from_p, lds, wv, lane, t.steps, kc * BK);
+                else sp.load_all(from_p, lds, wv);
+            } else {
+                sp.load_all(from_p, lds, wv);
+            }
             if (++kc == per) { kc = 0; ++pair; }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();

@@ -16,6 +16,9 @@ enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2, TILE_MANY = 3, TILE_
 constexpr int tile_p(TileShape s) { return s == TILE_256 ? 256 : 128; }
 constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_THIN ? 64 : 128; }
 
+// Whether tokens count, a bit each.  Nullable: all do
+typedef const uint64_t* TileTokens;
+
 struct TileOperand {
     const bf16_t* ptr;
     int64_t ld;         // elements, multiple of 8
@@ -31,6 +34,7 @@ struct TileArgs {
     const int* count;   // nullable: device word, tokens that count; of them this call takes those from `first` on, at most K or L.extent ...
     int first;
     int count_is_k;     // ... as contraction steps (1) or as rows of C (0)
+    TileTokens steps;   // contraction steps that do not count bring zeros from P (TILE_MANY, both K-strided)
     unsigned pairs;
     int n_pairs;
     int n_split;        // parts of the contraction, each a workgroup of its own; more where fewer rows count (tile_grid)
@@ -56,18 +60,25 @@ struct TileOut {
     int accumulate;     // add to what is there
     int skip_empty;     // write nothing where no token counts (a later piece of an accumulated product)
     const int* rows;    // nullable
+    TileTokens tokens;  // rows of C that do not count come out as zeros
     const float* scale; // nullable: device word that C is multiplied by
     float* part;        // n_split > 1: partial sums [split][rows of C that count][part_ld]
     int64_t part_ld;
 };
 
 // shape and number of parts of the contraction of a product: extents of C, chunks of the contraction (of all pairs of planes)
-struct TilePlan { TileShape shape; int n_split; bool from_codes; };
+struct TilePlan { TileShape shape; int n_split; bool from_codes; double us; };     // us: the estimate it was chosen by
 // restore: microseconds that P's values take to get from an 8-bit checkpoint to memory first (0: P is no checkpoint); from_codes: do without
-TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore);
+// only_many: TILE_MANY or nothing
+TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore, bool only_many = false);
 size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan);
 // C = L P^T over the operands' orientations: P K-strided, L K-contiguous or K-strided
 hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& o, hipStream_t st);
+// two products of TILE_MANY in one launch: the first's L K-contiguous, the second's K-strided; whether that is faster than a and b each in its own
+// launch, or a_alone and b
+struct TilePair { TilePlan plan; int64_t extent_p, extent_l, tiles, chunks; };
+bool pair_pays(const TilePair& a, const TilePair& b, const TilePlan& a_alone);
+hipError_t launch_pair(const TileArgs& ta, const TileOut& oa, const TileArgs& tb, const TileOut& ob, hipStream_t st);
 // the same from a checkpoint: L K-strided, TILE_MANY
 hipError_t launch_code_product(const TileCodes& codes, const TileArgs& t, const TileOut& o, hipStream_t st);
 // rows x cols (ld) of fp32 or bf16 to `planes` bf16 planes [rows][round_up(cols, 8)], zeros beyond cols
