@@ -7,7 +7,7 @@
 // Tokens whose label lies outside [0, V) do not count: their rows are left out from the start (the others are copied together,
 // in order), so that what they hold, NaN or not, reaches neither sum nor product.
 //
-// The vocabulary is walked in tiles of 256.  A workgroup has the logits of 256 tokens and one tile in its accumulators, takes the
+// The vocabulary is walked in tiles of 256 (128 for few tokens, and in fp32).  A workgroup has the logits of a tile of tokens and one tile in its accumulators, takes the
 // tile's maximum and its sum of exponentials (the label's left out) per token, and writes these two numbers; for the gradients it writes the exponentials
 // relative to the tile's maximum as well, for one piece of the tokens at a time.  One more pass over a piece joins the tiles'
 // numbers to lse_t and turns the exponentials into D in place, and the two products with D follow.
@@ -402,10 +402,10 @@ struct HeadPlan {
     size_t bytes = 0;
     size_t count, scale, rows, label, counts, xc, wc, stats, at_label, e, D, part, dw_part, sum;
     int64_t ldc, ldv;
-    int piece, pieces, tiles, x_planes, w_planes, d_planes, keep;
+    int piece, pieces, tiles, x_planes, d_planes, keep;
     TilePlan logits, dx, dw;
-    unsigned pairs, dx_pairs, dw_pairs;
-    int n_pairs, n_dx_pairs, n_dw_pairs;
+    unsigned dw_pairs;
+    int n_dw_pairs;
     bool copy_w, direct, pair;
 };
 
@@ -414,15 +414,11 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     const bool f32 = s.dtype == PSGD_F32;
     p.ldc = up8(s.d);
     p.ldv = up8(s.vocab);
-    p.x_planes = p.w_planes = f32 ? 3 : 1;
-    p.copy_w = f32 || s.d % 8 != 0;
-    p.pairs = f32 ? kPairs33 : kPairs1;
-    p.n_pairs = f32 ? 6 : 1;
+    p.x_planes = f32 ? 3 : 1;
+    p.copy_w = !f32 && s.d % 8 != 0;        // (fp32 W is split into planes by the products)
     p.keep = !gradients ? KEEP_NONE : f32 || s.grad_dtype == PSGD_F32 ? KEEP_F32 : KEEP_F16;
     p.d_planes = f32 ? 3 : s.grad_dtype == PSGD_F32 ? 2 : 1;
-    p.dx_pairs = p.pairs, p.n_dx_pairs = p.n_pairs;
-    if (f32) { p.dw_pairs = s.grad_dtype == PSGD_F32 ? kPairs33 : kPairs22; p.n_dw_pairs = s.grad_dtype == PSGD_F32 ? 6 : 3; }
-    else { p.dw_pairs = s.grad_dtype == PSGD_F32 ? kPairsL2 : kPairs1; p.n_dw_pairs = s.grad_dtype == PSGD_F32 ? 2 : 1; }
+    p.dw_pairs = !f32 && s.grad_dtype == PSGD_F32 ? kPairsL2 : kPairs1, p.n_dw_pairs = !f32 && s.grad_dtype == PSGD_F32 ? 2 : 1;
     // tokens per piece
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
     const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
@@ -433,8 +429,9 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.pieces = (int)((tokens + p.piece - 1) / p.piece);
     // Few tokens: X is taken where it is, and those that do not count are sorted out by their labels -- losses of one tile of rows, where they cost
     // nothing; gradients of up to kDirectTokens, whose launches are all there is to save.
-    p.direct = !p.copy_w && p.pieces == 1 && s.tokens > 0 && s.tokens <= (gradients ? kDirectTokens : tile_l(TILE_THIN));
-    p.logits = tile_plan(s.vocab, p.piece, (p.ldc + kTileK - 1) / kTileK * p.n_pairs, false, 0);
+    p.direct = !f32 && !p.copy_w && p.pieces == 1 && s.tokens > 0 && s.tokens <= (gradients ? kDirectTokens : tile_l(TILE_THIN));
+    const int64_t step = f32 ? tile_k(TILE_SPLIT) : kTileK, d_chunks = (s.d + step - 1) / step;
+    p.logits = f32 ? split_plan(s.vocab, p.piece, d_chunks, false) : tile_plan(s.vocab, p.piece, d_chunks, false, 0);
     p.tiles = (int)((s.vocab + tile_p(p.logits.shape) - 1) / tile_p(p.logits.shape));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
     p.count = take(4);
@@ -443,16 +440,16 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.label = take((size_t)tokens * 4);
     p.counts = take((size_t)(tokens + 63) / 64 * 8);
     p.xc = p.direct ? 0 : take((size_t)tokens * p.ldc * 2 * p.x_planes);
-    p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2 * p.w_planes) : 0;
+    p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2) : 0;
     p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
     p.at_label = take((size_t)p.piece * 4);
     if (gradients) {
         const size_t elems = (size_t)p.piece * p.ldv;
         p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
         p.D = p.keep == KEEP_F16 ? p.e : take(elems * 2 * p.d_planes);
-        const int64_t dx_chunks = (s.vocab + kTileK - 1) / kTileK * p.n_dx_pairs, dw_chunks = (p.piece + kTileK - 1) / kTileK * p.n_dw_pairs;
-        p.dx = tile_plan(s.d, p.piece, dx_chunks, true, 0);
-        p.dw = tile_plan(s.d, s.vocab, dw_chunks, true, 0, p.direct);
+        const int64_t dx_chunks = (s.vocab + step - 1) / step, dw_chunks = (p.piece + step - 1) / step * p.n_dw_pairs;
+        p.dx = f32 ? split_plan(s.d, p.piece, dx_chunks, true) : tile_plan(s.d, p.piece, dx_chunks, true, 0);
+        p.dw = f32 ? split_plan(s.d, s.vocab, dw_chunks, true) : tile_plan(s.d, s.vocab, dw_chunks, true, 0, p.direct);
         if (p.pieces == 1 && s.tokens > 0 && p.dw.shape == TILE_MANY) {
             const TilePlan many = tile_plan(s.d, p.piece, dx_chunks, true, 0, true);
             const int64_t wide = (s.d + 127) / 128;
@@ -496,6 +493,8 @@ static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, TileShape s
     if (shape == TILE_256) return launch_logits_shape<TILE_256>(t, h, st);
     if (shape == TILE_128) return launch_logits_shape<TILE_128>(t, h, st);
     if (shape == TILE_MANY) return launch_logits_shape<TILE_MANY>(t, h, st);
+    if (shape == TILE_SPLIT) return h.keep == KEEP_NONE ? launch_logits_as<TILE_SPLIT, KEEP_NONE>(t, h, st) : launch_logits_as<TILE_SPLIT, KEEP_F32>(t, h, st);
+    if (shape == TILE_SPLIT_THIN) return h.keep == KEEP_NONE ? launch_logits_as<TILE_SPLIT_THIN, KEEP_NONE>(t, h, st) : launch_logits_as<TILE_SPLIT_THIN, KEEP_F32>(t, h, st);
     return launch_logits_shape<TILE_THIN>(t, h, st);
 }
 
@@ -543,8 +542,8 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     h.ldv = p.ldv, h.d_plane = (int64_t)p.piece * p.ldv;
     h.tiles = p.tiles, h.tile_width = tile_p(p.logits.shape), h.n_planes = p.d_planes, h.keep = p.keep;
     bf16_t* xc = reinterpret_cast<bf16_t*>(ws + p.xc);
-    const bf16_t* wc = static_cast<const bf16_t*>(w);
-    int64_t ldwc = ldw, w_plane = 0;
+    const bf16_t* wc = static_cast<const bf16_t*>(w);       // (fp32: cast, the products know)
+    int64_t ldwc = ldw;
 
     h.direct = p.direct;
     // at most 1024 blocks, each of which reads the labels before its own
@@ -556,8 +555,8 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     if (hipGetLastError() != hipSuccess) return PSGD_E_HIP;
     if (p.copy_w) {
         bf16_t* to = reinterpret_cast<bf16_t*>(ws + p.wc);
-        if (launch_planes(w, s->dtype, s->vocab, s->d, ldw, to, p.w_planes, st) != hipSuccess) return PSGD_E_HIP;
-        wc = to, ldwc = p.ldc, w_plane = s->vocab * p.ldc;
+        if (launch_planes(w, PSGD_BF16, s->vocab, s->d, ldw, to, 1, st) != hipSuccess) return PSGD_E_HIP;
+        wc = to, ldwc = p.ldc;
     }
     for (int piece = 0; piece < p.pieces; ++piece) {
         const int first = piece * p.piece, rows = (int)std::min<int64_t>(p.piece, s->tokens - first);
@@ -566,20 +565,20 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
         TileArgs t = {};
         t.count = h.direct ? nullptr : h.count, t.first = first, t.n_split = 1;
         if (rows > 0) {
-            t.P = {wc, ldwc, w_plane, (int)s->vocab};
+            t.P = {wc, ldwc, 0, (int)s->vocab};
             t.L = tokens;
-            t.K = (int)p.ldc;
-            t.pairs = p.pairs, t.n_pairs = p.n_pairs;
+            t.K = (int)(f32 ? s->d : p.ldc);
+            t.pairs = kPairs1, t.n_pairs = 1;
             if (launch_logits(t, h, p.logits.shape, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
         }
         if (!gradients) continue;
         TileArgs tx = t, tw = t;
         TileOut ox = {}, ow = {};
         ox.scale = ow.scale = h.scale;
-        tx.P = {wc, ldwc, w_plane, (int)s->d};
+        tx.P = {wc, ldwc, 0, (int)s->d};
         tx.L = {h.D, p.ldv, h.d_plane, rows};
         tx.K = (int)s->vocab;
-        tx.pairs = p.dx_pairs, tx.n_pairs = p.n_dx_pairs, tx.n_split = p.dx.n_split;
+        tx.n_split = p.dx.n_split;
         ox.part = reinterpret_cast<float*>(ws + p.part);
         ox.ptr = dx, ox.ld = lddx, ox.dtype = s->dtype;
         tw.P = tokens;

@@ -195,6 +195,28 @@ TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_
     return best;
 }
 
+// As above for fp32 operands.  Measured, us per chunk of 32 steps: a compute unit with one workgroup 2.0 (128 x 128) and 1.2 (128 x 64, which loads four
+// chunks ahead), full 1.4 and 0.85 for each of its three or two.  Logits of 64 x 4096 x 32000: 265 and 171 us; of 500 x 4096 x 32000: 702 and 852 us.
+TilePlan split_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split) {
+    TilePlan best = {TILE_SPLIT, 1, false, 1e300};
+    for (TileShape shape : {TILE_SPLIT, TILE_SPLIT_THIN}) {
+        const int64_t l = tile_l(shape), tiles = (extent_p + 127) / 128 * ((extent_l + l - 1) / l), share_cu = shape == TILE_SPLIT ? 3 : 2;
+        const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
+        for (int64_t want : {(int64_t)1, fill / 2, fill, share_cu * fill}) {
+            want = std::min({want, chunks, (int64_t)64});
+            if (want < 1 || (want > 1 && !may_split)) continue;
+            const int64_t share = (chunks + want - 1) / want, split = share > 0 ? (chunks + share - 1) / share : 1, blocks = tiles * split;
+            const double most = shape == TILE_SPLIT ? 1.4 : 0.85, least = shape == TILE_SPLIT ? 2.0 : 1.2;
+            const int64_t last = (blocks % (share_cu * kUnits) + kUnits - 1) / kUnits;
+            double us = (double)(blocks / (share_cu * kUnits)) * (6 + share * share_cu * most);
+            if (last > 0) us += 6 + share * std::max(least, last * most);
+            us += split_us((int)split, extent_p, extent_l);
+            if (us < best.us) best = {shape, (int)split, false, us};
+        }
+    }
+    return best;
+}
+
 // Both products' workgroups fill the compute units together and take as long as the longer contraction; a launch less (3 us).  (Gradients of the head, tokens x d x
 // vocab, in us without the pair and with it: 16 x 512 x 4400 32.0, 26.7; 512 x 512 x 4400 54.6, 47.5; 128 x 1024 x 10008 46.0, 39.7; what is not paired by this rule,
 // 200 x 1024 x 10008, was 57.2 and 59.)
@@ -285,11 +307,15 @@ hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t,
         if (shape == TILE_256) return launch_shape<true, TILE_256>(t, o, st);
         if (shape == TILE_128) return launch_shape<true, TILE_128>(t, o, st);
         if (shape == TILE_MANY) return launch_shape<true, TILE_MANY>(t, o, st);
+        if (shape == TILE_SPLIT) return launch_shape<true, TILE_SPLIT>(t, o, st);
+        if (shape == TILE_SPLIT_THIN) return launch_shape<true, TILE_SPLIT_THIN>(t, o, st);
         return launch_shape<true, TILE_THIN>(t, o, st);
     }
     if (shape == TILE_256) return launch_shape<false, TILE_256>(t, o, st);
     if (shape == TILE_128) return launch_shape<false, TILE_128>(t, o, st);
     if (shape == TILE_MANY) return launch_shape<false, TILE_MANY>(t, o, st);
+    if (shape == TILE_SPLIT) return launch_shape<false, TILE_SPLIT>(t, o, st);
+    if (shape == TILE_SPLIT_THIN) return launch_shape<false, TILE_SPLIT_THIN>(t, o, st);
     return launch_shape<false, TILE_THIN>(t, o, st);
 }
 

@@ -170,29 +170,32 @@ struct TileFragment {
 
 // Waves along P and L, chunks in LDS.  All have four waves, one per SIMD.
 // workgroups to a compute unit
-constexpr int tile_share(TileShape s) { return s == TILE_MANY ? 4 : 1; }
+constexpr int tile_share(TileShape s) { return s == TILE_MANY ? 4 : s == TILE_SPLIT ? 3 : s == TILE_SPLIT_THIN ? 2 : 1; }
 template <TileShape SHAPE> struct TileWaves;
 template <> struct TileWaves<TILE_256> { static constexpr int WP = 2, WL = 2, STAGES = 0; };
 template <> struct TileWaves<TILE_128> { static constexpr int WP = 2, WL = 2, STAGES = 5; };
 template <> struct TileWaves<TILE_MANY> { static constexpr int WP = 2, WL = 2, STAGES = 1; };
+template <> struct TileWaves<TILE_SPLIT> { static constexpr int WP = 2, WL = 2, STAGES = 1; };
+template <> struct TileWaves<TILE_SPLIT_THIN> { static constexpr int WP = 2, WL = 2, STAGES = 1; };
 template <> struct TileWaves<TILE_THIN> { static constexpr int WP = 2, WL = 2, STAGES = 6; };
 
 template <bool PKC, bool LKC, TileShape SHAPE>
 struct Tile {
     using S = TileWaves<SHAPE>;
-    static constexpr int BP = tile_p(SHAPE), BL = tile_l(SHAPE), WP = S::WP, WL = S::WL, NW = WP * WL, BK = kTileK, STAGES = S::STAGES;
-    static constexpr bool FULL = SHAPE == TILE_256;
+    static constexpr int BP = tile_p(SHAPE), BL = tile_l(SHAPE), WP = S::WP, WL = S::WL, NW = WP * WL, BK = tile_k(SHAPE), STAGES = S::STAGES;
+    static constexpr bool FULL = SHAPE == TILE_256, SPLIT = tile_is_split(SHAPE);
+    static constexpr int RING = SHAPE == TILE_SPLIT_THIN ? 4 : 1;      // chunks of L in LDS (SPLIT)
     static constexpr int FP = BP / WP / 32, FL = BL / WL / 32;      // fragments per wave
     using SideP = TileSide<PKC, BP, BK, NW>;
     using SideL = TileSide<LKC, BL, BK, NW>;
     static constexpr int STAGE_BYTES = SideP::BYTES + SideL::BYTES;
     static constexpr int ROWS_BYTES = NW * 32 * (32 * FP + 4) * 4;         // for_rows()
-    static constexpr int CHUNK_BYTES = FULL ? 5 * SideP::BYTES : STAGES * STAGE_BYTES;
+    static constexpr int CHUNK_BYTES = FULL ? 5 * SideP::BYTES : SPLIT ? kMaxPlanes * (SideP::BYTES + RING * SideL::BYTES) : STAGES * STAGE_BYTES;
     static constexpr int LDS_BYTES = CHUNK_BYTES > ROWS_BYTES ? CHUNK_BYTES : ROWS_BYTES;
     static constexpr int LOADS = SideP::LOADS + SideL::LOADS;
-    static_assert(FP >= 1 && FL >= 1 && FP <= 4 && FL <= 4 && BK == 64 && NW * 64 == kTileThreads && LDS_BYTES <= 160 * 1024, "waves");
-    static_assert((STAGES - 1) * LOADS <= 63 && (FULL || LOADS >= 3), "the wait counter's range, thirds");
-    static_assert(SHAPE != TILE_MANY || 4 * LDS_BYTES <= 160 * 1024, "four to a compute unit");
+    static_assert(FP >= 1 && FL >= 1 && FP <= 4 && FL <= 4 && NW * 64 == kTileThreads && LDS_BYTES <= 160 * 1024, "waves");
+    static_assert((STAGES - 1) * LOADS <= 63 && (STAGES < 2 || LOADS >= 3), "the wait counter's range, thirds");
+    static_assert(tile_share(SHAPE) * LDS_BYTES <= 160 * 1024, "workgroups to a compute unit");
 
     floatx16 acc[FP][FL];
     int wp, wl, lane;
@@ -333,20 +336,22 @@ struct Tile {
             }
         SideP sp;
         SideL sl;
-        if constexpr (!CODES) sp.init(t.P, p0, t.P.extent, wv, lane);
+        if constexpr (!CODES && !(SPLIT && LKC)) sp.init(t.P, p0, t.P.extent, wv, lane);
         sl.init(t.L, l0, nl, wv, lane);
         TileFragment<PKC, BP, BK> fp;
         TileFragment<LKC, BL, BK> fl;
         fp.init(wp * FP * 32, lane);
         fl.init(wl * FL * 32, lane);
 
-        const int per = (K + BK - 1) / BK, all = per * t.n_pairs, share = (all + n_split - 1) / n_split;
+        const int per = (K + BK - 1) / BK, all = SPLIT ? per : per * t.n_pairs, share = (all + n_split - 1) / n_split;
         const int n0 = min(all, split * share), n = min(all, n0 + share) - n0;
         if (n <= 0) return;
         if constexpr (FULL) {
             run_full(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         } else {
-            if constexpr (CODES) run_codes(t, codes, p0, l0, K, n0, n, per, wv, sl, fp, fl, lds);
+            if constexpr (SPLIT && LKC && RING > 1) run_split_ahead(t, p0, l0, K, n0, n, wv, sl, fp, fl, lds);
+            else if constexpr (SPLIT) run_split(t, p0, l0, K, n0, n, wv, sp, sl, fp, fl, lds);
+            else if constexpr (CODES) run_codes(t, codes, p0, l0, K, n0, n, per, wv, sl, fp, fl, lds);
             else if constexpr (STAGES == 1) run_single(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
             else run_ring(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
         }
@@ -490,6 +495,129 @@ struct Tile {
             multiply_chunk(lds, fp, fl);
         }
     }
+    // fp32 operands.  All three planes of a chunk of both sides are in LDS, and six products are made of each pair of chunks: a plane is loaded once, not
+    // once per product, which is what bounds fp32 products that stream pairs of planes (1000 x 2048 x 20000, loss and gradients: 1621 us with pairs, 1299 us
+    // so).  P's come from the fp32 matrix, four elements per load, split on the way (LKC): W is read as it is, where planes of it in memory cost six bytes
+    // written and twelve read per element (64 x 4096 x 32000, loss alone: 636 us with them, 166 us without).  Or like L's from memory.
+    static constexpr int RAW = BP * BK * 4 / (16 * kTileThreads);       // loads of a thread and chunk
+    // piece i of this thread: its element and step in the chunk
+    __device__ __forceinline__ static void raw_piece(int i, int wv, int lane, int& e, int& k) {
+        const int block = i * NW + wv;
+        if constexpr (PKC) e = block * 8 + (lane >> 3), k = 4 * (lane & 7);
+        else k = block * 2 + (lane >> 5), e = 4 * (lane & 31);
+    }
+    // (Loads without a branch, out of range where there is nothing: the waits below count them.)
+    __device__ __forceinline__ static void raw_fetch(const TileOperand& o, int p0, int k0, int K, int wv, int lane, floatx4 (&raw)[RAW]) {
+        const float* base = reinterpret_cast<const float*>(o.ptr) + (PKC ? (int64_t)p0 * o.ld + k0 : (int64_t)k0 * o.ld + p0);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, (int)kOutside, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) {
+            int e, k;
+            raw_piece(i, wv, lane, e, k);
+            const unsigned at = (unsigned)((PKC ? e * o.ld + k : k * o.ld + e) * 4);
+            raw[i] = __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(p0 + e < o.extent && k0 + k < K ? at : kOutside), 0, 0));
+        }
+    }
+    __device__ __forceinline__ static void raw_store(const floatx4 (&raw)[RAW], int k0, int K, int wv, int lane, PSGD_TLDS unsigned char* lds) {
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) {
+            int e, k;
+            raw_piece(i, wv, lane, e, k);
+            bf16x4 plane[kMaxPlanes];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                bf16_t q[kMaxPlanes];
+                split_planes<kMaxPlanes>(!PKC || k0 + k + u < K ? raw[i][u] : 0.f, q);      // (K may end inside a piece)
+#pragma unroll
+                for (int h = 0; h < kMaxPlanes; ++h) plane[h][u] = q[h];
+            }
+            const unsigned to = PKC ? (unsigned)(e * 2 * BK + (((k >> 3) ^ SideP::swizzle(e)) << 4) + 2 * (k & 4))
+                                    : (unsigned)(k * 2 * BP + ((2 * e) ^ (SideP::turn(k) << 6)));
+#pragma unroll
+            for (int h = 0; h < kMaxPlanes; ++h) *reinterpret_cast<PSGD_TLDS bf16x4*>(lds + h * SideP::BYTES + to) = plane[h];
+        }
+    }
+    __device__ __forceinline__ static void fence() { asm volatile("" ::: "memory"); }
+
+    __device__ __forceinline__ void run_split(const TileArgs& t, int p0, int l0, int K, int n0, int n, int wv, const SideP& sp, const SideL& sl,
+                                              const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl, PSGD_TLDS unsigned char* lds) {
+        PSGD_TLDS unsigned char* const lds_l = lds + kMaxPlanes * SideP::BYTES;
+        floatx4 raw[RAW];
+        if constexpr (LKC) raw_fetch(t.P, p0, n0 * BK, K, wv, lane, raw);
+        for (int kc = n0; kc < n0 + n; ++kc) {
+#pragma unroll
+            for (int q = 0; q < kMaxPlanes; ++q) {
+                sl.load_all(SideL::source(t.L, q, l0, kc * BK, K, true), lds_l + q * SideL::BYTES, wv);
+                if constexpr (!LKC) sp.load_all(SideP::source(t.P, q, p0, kc * BK, K, true), lds + q * SideP::BYTES, wv);
+            }
+            if constexpr (LKC) raw_store(raw, kc * BK, K, wv, lane, lds);
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            fence();
+            if constexpr (LKC) raw_fetch(t.P, p0, (kc + 1) * BK, K, wv, lane, raw);
+            split_step<0>(lds, lds_l, fp, fl);
+            split_step<1>(lds, lds_l, fp, fl);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();       // every wave is done with the chunk
+            fence();
+        }
+    }
+
+    // the same with the loads of RING chunks ahead, for few workgroups
+    __device__ __forceinline__ void run_split_ahead(const TileArgs& t, int p0, int l0, int K, int n0, int n, int wv, const SideL& sl,
+                                                    const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl, PSGD_TLDS unsigned char* lds) {
+        PSGD_TLDS unsigned char* const lds_l = lds + kMaxPlanes * SideP::BYTES;
+        const int end = n0 + n;
+        floatx4 raw[RING][RAW];
+        auto load_l = [&](int kc) {
+            fence();
+#pragma unroll
+            for (int q = 0; q < kMaxPlanes; ++q)
+                sl.load_all(SideL::source(t.L, q, l0, kc * BK, K, kc < end), lds_l + ((kc - n0) % RING * kMaxPlanes + q) * SideL::BYTES, wv);
+            fence();
+        };
+        raw_fetch(t.P, p0, n0 * BK, K, wv, lane, raw[0]);
+#pragma unroll
+        for (int i = 1; i < RING; ++i) {
+            load_l(n0 + i - 1);
+            raw_fetch(t.P, p0, (n0 + i) * BK, n0 + i < end ? K : 0, wv, lane, raw[i]);
+        }
+        for (int k4 = n0; k4 < end; k4 += RING)
+#pragma unroll
+            for (int i = 0; i < RING; ++i) {
+                const int kc = k4 + i;
+                if (kc >= end) break;
+                raw_store(raw[i], kc * BK, K, wv, lane, lds);
+                load_l(kc + RING - 1);
+                raw_fetch(t.P, p0, (kc + RING) * BK, kc + RING < end ? K : 0, wv, lane, raw[i]);
+                // all that was loaded after this chunk of L may be on its way
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(RING * RAW + (RING - 1) * kMaxPlanes * SideL::LOADS) : "memory");
+                __builtin_amdgcn_s_barrier();
+                fence();
+                const PSGD_TLDS unsigned char* const from = lds_l + i * kMaxPlanes * SideL::BYTES;
+                split_step<0>(lds, from, fp, fl);
+                split_step<1>(lds, from, fp, fl);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();       // every wave is done with the chunk
+                fence();
+            }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (LDS is the epilogue's next)
+        __builtin_amdgcn_s_barrier();
+        fence();
+    }
+    template <int KK>
+    __device__ __forceinline__ void split_step(const PSGD_TLDS unsigned char* lds, const PSGD_TLDS unsigned char* lds_l, const TileFragment<PKC, BP, BK>& fp,
+                                               const TileFragment<LKC, BL, BK>& fl) {
+        bf16x8 a[kMaxPlanes][FP], b[kMaxPlanes][FL];
+#pragma unroll
+        for (int q = 0; q < kMaxPlanes; ++q) read_ab<KK>(lds + q * SideP::BYTES, lds_l + q * SideL::BYTES, fp, fl, a[q], b[q]);
+        // smallest products first
+#pragma unroll
+        for (int sum = kMaxPlanes - 1; sum >= 0; --sum)
+#pragma unroll
+            for (int q = sum; q >= 0; --q) multiply(a[q], b[sum - q]);
+    }
+
     // a chunk that is in LDS; the barrier says that every wave is done with it
     __device__ __forceinline__ void multiply_chunk(const PSGD_TLDS unsigned char* lds, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl) {
         bf16x8 a0[FP], b0[FL], a1[FP], b1[FL];

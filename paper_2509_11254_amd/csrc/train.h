@@ -11,10 +11,12 @@ constexpr int kTileThreads = 256;
 
 // Elements of a tile of C along P and L.  256 x 256, 128 x 128 (few tiles: one workgroup per compute unit, deep in loads) and 128 x 64 (few
 // rows) have a compute unit's LDS for themselves; of TILE_MANY, 128 x 128 with one chunk in LDS, a compute unit takes four, which hide each
-// other's loads and stores.
-enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2, TILE_MANY = 3, TILE_SHAPES = 4 };
+// other's loads and stores.  The TILE_SPLIT shapes multiply fp32 operands, whose three bf16 planes are in LDS side by side.
+enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2, TILE_MANY = 3, TILE_SPLIT = 4, TILE_SPLIT_THIN = 5 };
+constexpr bool tile_is_split(TileShape s) { return s == TILE_SPLIT || s == TILE_SPLIT_THIN; }
 constexpr int tile_p(TileShape s) { return s == TILE_256 ? 256 : 128; }
-constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_THIN ? 64 : 128; }
+constexpr int tile_l(TileShape s) { return s == TILE_256 ? 256 : s == TILE_THIN || s == TILE_SPLIT_THIN ? 64 : 128; }
+constexpr int tile_k(TileShape s) { return tile_is_split(s) ? 32 : kTileK; }
 
 // Whether tokens count, a bit each.  Nullable: all do
 typedef const uint64_t* TileTokens;
@@ -26,6 +28,8 @@ struct TileOperand {
     int extent;         // rows or columns of C that it covers
 };
 
+// (TILE_SPLIT shapes: three planes of each side and the six products of two whose places add up to at most two.  Where L is K-contiguous P is the fp32
+// matrix itself, cast, and `ld` counts its elements.)
 // What every kernel on tiles gets.  An operand may have several bf16 planes whose sum it is; `pairs` lists the products of planes to
 // add up, smallest first, four bits each: P's plane in the lower two, L's in the upper two.
 struct TileArgs {
@@ -40,9 +44,7 @@ struct TileArgs {
     int n_split;        // parts of the contraction, each a workgroup of its own; more where fewer rows count (tile_grid)
     int blocks;         // workgroups of the launch (set by it)
 };
-constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048, kPairs22 = 0x014;
-// three planes each, six products: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-constexpr unsigned kPairs33 = 0x014852;
+constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048;
 
 // An 8-bit checkpoint in the place of P, K-strided: codes [K][ldc], scales [K][groups]
 struct TileCodes {
@@ -71,6 +73,8 @@ struct TilePlan { TileShape shape; int n_split; bool from_codes; double us; };  
 // restore: microseconds that P's values take to get from an 8-bit checkpoint to memory first (0: P is no checkpoint); from_codes: do without
 // only_many: TILE_MANY or nothing
 TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split, double restore, bool only_many = false);
+// the same for fp32 operands; chunks: of one plane
+TilePlan split_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split);
 size_t tile_part_bytes(int64_t extent_p, int64_t extent_l, const TilePlan& plan);
 // C = L P^T over the operands' orientations: P K-strided, L K-contiguous or K-strided
 hipError_t launch_product(bool l_contiguous, TileShape shape, const TileArgs& t, const TileOut& o, hipStream_t st);
