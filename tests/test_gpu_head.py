@@ -107,6 +107,12 @@ def test_weights_sums_and_pieces(dtype, g_dtype, weighted, accumulate, piece):
     run(333, 136, 700, dtype, g_dtype, weighted=weighted, accumulate=accumulate, piece=piece)
 
 
+@pytest.mark.parametrize("tokens,d,vocab", [(1, 41, 9001), (65, 95, 33000), (130, 1028, 5000), (900, 33, 6001), (1500, 260, 3001)])
+def test_fp32_over_tiles(tokens, d, vocab):
+    """Wide and narrow tiles, contractions in parts that end inside four elements, one token to many."""
+    run(tokens, d, vocab, "f32", "f32", masked=0.1)
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("piece", [0, 32])
 @pytest.mark.parametrize("dtype,g_dtype", [("bf16", "bf16"), ("f32", "f32")])

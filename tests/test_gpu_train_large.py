@@ -90,3 +90,31 @@ def test_a_piece_of_many_tokens():
     assert torch.equal(got[0][0], got[1][0])        # a token's loss does not depend on the piece it is in
     assert (got[0][1].float() - got[1][1].float()).norm() <= 2.0 ** -8 * got[0][1].float().norm()
     assert (got[0][2] - got[1][2]).norm() <= 2.0 ** -16 * got[0][2].norm()
+
+
+def test_head_with_a_large_fp32_matrix():
+    tokens, d, vocab = 5, 8200, 140000
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    w = torch.randn((vocab, d), generator=gen, device="cuda").mul_(d ** -0.5)
+    x = torch.randn((tokens, d), generator=gen, device="cuda")
+    labels = torch.tensor([vocab - 1, -1, 131000, 0, 70000], device="cuda")
+    loss, dx, dw = torch.empty(tokens, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    psgd.HeadLoss(tokens, d, vocab, psgd.PSGD_F32, psgd.PSGD_F32).loss_grad(x, w, labels, loss, dx, dw)
+    on = [0, 2, 3, 4]
+    x64 = x[on].double()
+    logits = torch.cat([x64 @ part.double().t() for part in w.split(20000)], 1)
+    lse = torch.logsumexp(logits, 1)
+    want = lse - logits[torch.arange(4), labels[on]]
+    # fp32 sums of 8200 products, sixteen at a time
+    assert (loss[on].double() - want).abs().max() < 1e-4 and float(loss[1]) == 0
+    p = torch.exp(logits - lse[:, None])
+    p[torch.arange(4), labels[on]] -= 1
+    p /= 4
+    rows = [0, 1, 70000, 130899, 131000, vocab - 2, vocab - 1]
+    dw64 = p[:, rows].t() @ x64
+    # the exponentials' error is the logits': 8200 / 16 steps of 2^-24 of a sum of unit variance
+    assert ((dw[rows].double() - dw64).abs() <= 2.0 ** -12 * (p[:, rows].abs().t() @ x64.abs()) + 1e-12).all()
+    dx64 = sum(p[:, 20000 * i:20000 * i + part.shape[0]] @ part.double() for i, part in enumerate(w.split(20000)))
+    size = sum(p[:, 20000 * i:20000 * i + part.shape[0]].abs() @ part.double().abs() for i, part in enumerate(w.split(20000)))
+    assert ((dx[on].double() - dx64).abs() <= 2.0 ** -12 * size).all() and (dx[1] == 0).all()
