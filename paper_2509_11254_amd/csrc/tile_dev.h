@@ -496,7 +496,7 @@ struct Tile {
         }
     }
     // fp32 operands.  All three planes of a chunk of both sides are in LDS, and six products are made of each pair of chunks: a plane is loaded once, not
-    // once per product, which is what bounds fp32 products that stream pairs of planes (1000 x 2048 x 20000, loss and gradients: 1621 us with pairs, 1299 us
+    // once per product, which is what bounds fp32 products that stream pairs of planes (1000 x 2048 x 20000, loss and gradients: 1621 us with pairs, 1264 us
     // so).  P's come from the fp32 matrix, four elements per load, split on the way (LKC): W is read as it is, where planes of it in memory cost six bytes
     // written and twelve read per element (64 x 4096 x 32000, loss alone: 636 us with them, 166 us without).  Or like L's from memory.
     static constexpr int RAW = BP * BK * 4 / (16 * kTileThreads);       // loads of a thread and chunk
@@ -504,7 +504,7 @@ struct Tile {
     __device__ __forceinline__ static void raw_piece(int i, int wv, int lane, int& e, int& k) {
         const int block = i * NW + wv;
         if constexpr (PKC) e = block * 8 + (lane >> 3), k = 4 * (lane & 7);
-        else k = block * 2 + (lane >> 5), e = 4 * (lane & 31);
+        else k = block * (256 / BP) + lane / (BP / 4), e = 4 * (lane % (BP / 4));
     }
     // (Loads without a branch, out of range where there is nothing: the waits below count them.)
     __device__ __forceinline__ static void raw_fetch(const TileOperand& o, int p0, int k0, int K, int wv, int lane, floatx4 (&raw)[RAW]) {
