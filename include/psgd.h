@@ -308,7 +308,7 @@ int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
  * A token whose label lies outside [0, vocab) does not count: its loss and its row of dX are 0 and its row of X is not
  * looked at.  Exponentials and D exist for one piece of the tokens at a time, in the workspace.
  * Arithmetic: bf16 X and W are multiplied on the matrix cores as they are, fp32 ones as three bf16 planes (24 bits); sums, statistics and losses are fp32.  D is
- * rounded once to bf16 for results in bf16; for dW in fp32 it has two bf16 planes (16 bits), with fp32 X and W three. */
+ * rounded once to bf16 for results in bf16; for results in fp32 it has three bf16 planes. */
 typedef struct {
     int64_t tokens, d, vocab;   /* X: tokens x d, W: vocab x d; tokens may be 0                      */
     int64_t ldx, ldw;           /* leading dimensions; 0 = d, which is then a multiple of 8          */

@@ -45,7 +45,7 @@ struct TileArgs {
     int n_split;        // parts of the contraction, each a workgroup of its own; more where fewer rows count (tile_grid)
     int blocks;         // workgroups of the launch (set by it)
 };
-constexpr unsigned kPairs1 = 0x0, kPairsL2 = 0x04, kPairsL3 = 0x048;
+constexpr unsigned kPairs1 = 0x0, kPairsL3 = 0x048;
 
 // An 8-bit checkpoint in the place of P, K-strided: codes [K][ldc], scales [K][groups]
 struct TileCodes {
