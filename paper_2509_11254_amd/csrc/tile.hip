@@ -195,15 +195,18 @@ TilePlan tile_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_
     return best;
 }
 
-// As above for fp32 operands.  Measured, us per chunk of 32 steps: a compute unit with one workgroup 2.0 (128 x 128) and 0.7 (64 x 64, which loads four
-// chunks ahead), full 1.4 and 0.55 for each of its three or two.  Loss, tokens x d x vocab: 1 x 4096 x 32000 on wide tiles 243 us, narrow 132;
-// 256 x 4096 x 32000 382 and 520; 256 x 512 x 4400 39 and 28.
+// As above for fp32 operands.  Measured, us per chunk of 32 steps: a compute unit with one workgroup 2.0 (128 x 128) and 0.7 (64 x 64, which loads three
+// chunks ahead), full 1.4 and 0.55 for each of its three.  Loss, tokens x d x vocab: 1 x 4096 x 32000 on wide tiles 243 us, narrow 132;
+// 256 x 4096 x 32000 382 and 520; 256 x 512 x 4400 39 and 26.  Two narrow ones to a compute unit with four chunks ahead: 512 x 512 x 4400 with gradients 100 us
+// in place of 90, 200 x 1024 x 10008 141 in place of 131.
 TilePlan split_plan(int64_t extent_p, int64_t extent_l, int64_t chunks, bool may_split) {
+    constexpr int share_cu = tile_share(TILE_SPLIT);
+    static_assert(share_cu == tile_share(TILE_SPLIT_THIN), "workgroups to a compute unit");
     TilePlan best = {TILE_SPLIT, 1, false, 1e300};
     for (TileShape shape : {TILE_SPLIT, TILE_SPLIT_THIN}) {
-        const int64_t w = tile_p(shape), l = tile_l(shape), tiles = (extent_p + w - 1) / w * ((extent_l + l - 1) / l), share_cu = shape == TILE_SPLIT ? 3 : 2;
+        const int64_t w = tile_p(shape), l = tile_l(shape), tiles = (extent_p + w - 1) / w * ((extent_l + l - 1) / l);
         const int64_t fill = tiles > 0 ? kUnits / tiles : 1;
-        for (int64_t want : {(int64_t)1, fill / 2, fill, share_cu * fill}) {
+        for (int64_t want : {(int64_t)1, fill / 2, fill, 2 * fill, share_cu * fill}) {
             want = std::min({want, chunks, (int64_t)64});
             if (want < 1 || (want > 1 && !may_split)) continue;
             const int64_t share = (chunks + want - 1) / want, split = share > 0 ? (chunks + share - 1) / share : 1, blocks = tiles * split;

@@ -170,7 +170,7 @@ struct TileFragment {
 
 // Waves along P and L, chunks in LDS.  All have four waves, one per SIMD.
 // workgroups to a compute unit
-constexpr int tile_share(TileShape s) { return s == TILE_MANY ? 4 : s == TILE_SPLIT ? 3 : s == TILE_SPLIT_THIN ? 2 : 1; }
+constexpr int tile_share(TileShape s) { return s == TILE_MANY ? 4 : tile_is_split(s) ? 3 : 1; }
 template <TileShape SHAPE> struct TileWaves;
 template <> struct TileWaves<TILE_256> { static constexpr int WP = 2, WL = 2, STAGES = 0; };
 template <> struct TileWaves<TILE_128> { static constexpr int WP = 2, WL = 2, STAGES = 5; };
@@ -184,7 +184,7 @@ struct Tile {
     using S = TileWaves<SHAPE>;
     static constexpr int BP = tile_p(SHAPE), BL = tile_l(SHAPE), WP = S::WP, WL = S::WL, NW = WP * WL, BK = tile_k(SHAPE), STAGES = S::STAGES;
     static constexpr bool FULL = SHAPE == TILE_256, SPLIT = tile_is_split(SHAPE);
-    static constexpr int RING = SHAPE == TILE_SPLIT_THIN ? 4 : 1;      // chunks of L in LDS (SPLIT)
+    static constexpr int RING = SHAPE == TILE_SPLIT_THIN ? 3 : 1;      // chunks of L in LDS (SPLIT)
     static constexpr int FP = BP / WP / 32, FL = BL / WL / 32;      // fragments per wave
     using SideP = TileSide<PKC, BP, BK, NW>;
     using SideL = TileSide<LKC, BL, BK, NW>;

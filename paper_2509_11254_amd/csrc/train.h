@@ -12,7 +12,7 @@ constexpr int kTileThreads = 256;
 // Elements of a tile of C along P and L.  256 x 256, 128 x 128 (few tiles: one workgroup per compute unit, deep in loads) and 128 x 64 (few
 // rows) have a compute unit's LDS for themselves; of TILE_MANY, 128 x 128 with one chunk in LDS, a compute unit takes four, which hide each
 // other's loads and stores.  TILE_SPLIT, 128 x 128, and TILE_SPLIT_THIN, 64 x 64 (few tiles), multiply fp32 operands, whose three bf16 planes are in LDS side
-// by side; a compute unit takes three and two of them.
+// by side; a compute unit takes three of them.
 enum TileShape { TILE_256 = 0, TILE_128 = 1, TILE_THIN = 2, TILE_MANY = 3, TILE_SPLIT = 4, TILE_SPLIT_THIN = 5 };
 constexpr bool tile_is_split(TileShape s) { return s == TILE_SPLIT || s == TILE_SPLIT_THIN; }
 constexpr int tile_p(TileShape s) { return s == TILE_256 ? 256 : s == TILE_SPLIT_THIN ? 64 : 128; }
