@@ -428,7 +428,7 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     // tokens per piece
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
     const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
-    const int64_t most = s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256);
+    const int64_t most = std::min(tokens, s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256));
     p.pieces = (int)((tokens + most - 1) / most);
     p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
     if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
