@@ -401,6 +401,8 @@ __global__ __launch_bounds__(kThreads) void head_round_kernel(const float* sum, 
 // not where there may be many that do not count.)
 constexpr int64_t kDirectTokens = 512;
 constexpr size_t kPieceBytes = (size_t)1 << 30;     // what is kept of one piece of the tokens: exponentials and D, or statistics alone
+// A launch has fewer than 2^32 threads: 256 to a token of a piece, and 256 to a tile of its logits, at least 64 x 64 (half of either, for what borders add).
+constexpr int64_t kMaxPiece = (int64_t)1 << 23, kMaxPieceLogits = (int64_t)1 << 35;
 
 struct HeadPlan {
     size_t bytes = 0;
@@ -428,7 +430,8 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     // tokens per piece
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
     const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
-    const int64_t most = std::min(tokens, s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256));
+    const int64_t launch = std::min(kMaxPiece, std::max<int64_t>(1, kMaxPieceLogits / s.vocab));
+    const int64_t most = std::min(std::min(tokens, launch), s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256));
     p.pieces = (int)((tokens + most - 1) / most);
     p.piece = (int)((tokens + p.pieces - 1) / p.pieces);
     if (p.pieces > 1 && s.piece_tokens <= 0) p.piece = (p.piece + 255) / 256 * 256;
