@@ -339,9 +339,10 @@ static ActGrid act_grid(int64_t rows, int64_t cols, int dtype) {
     g.grid = dim3((unsigned)((rows * g.rows.per + kThreads * kActItems - 1) / (kThreads * kActItems)));
     return g;
 }
-static int act_shape(int64_t rows, int64_t cols) {
+static int act_shape(int64_t rows, int64_t cols, int dtype) {
     if (rows < 0 || cols < 1 || rows > kMaxExtent || cols > kMaxExtent) return PSGD_E_SHAPE;
-    if (rows * (8 * ((cols + kGroup - 1) / kGroup)) > (int64_t)INT32_MAX * kThreads) return PSGD_E_SHAPE;
+    const int64_t per = (cols + kGroup - 1) / kGroup * (kGroup / (dtype == PSGD_F32 ? kPiece<float> : kPiece<bf16_t>));
+    if (rows * per >= ((int64_t)kActItems << 32) - kActItems * kThreads) return PSGD_E_SHAPE;      // a launch has fewer than 2^32 threads
     return PSGD_OK;
 }
 static bool bad_codes(const void* codes, const void* scales) { return !codes || !scales; }
@@ -385,7 +386,7 @@ static WgradPlan wgrad_plan(int64_t tokens, int64_t out, int64_t in, int dtype) 
 static int wgrad_shape(int64_t tokens, int64_t out, int64_t in) {
     if (tokens < 0 || out < 1 || in < 1 || tokens > kMaxExtent || out > kMaxExtent || in > kMaxExtent) return PSGD_E_SHAPE;
     if (up8(in) > kMaxLd || up8(out) > kMaxLd) return PSGD_E_SHAPE;
-    return act_shape(tokens, in);
+    return act_shape(tokens, in, PSGD_BF16);
 }
 
 }  // namespace psgd
@@ -396,7 +397,7 @@ extern "C" {
 
 int psgd_act_store(void* stream, int64_t rows, int64_t cols, const void* x, int dtype, int64_t ld, int8_t* codes, int64_t ldc, uint8_t* scales) {
     if ((rows != 0 && (!x || bad_codes(codes, scales))) || bad_dtype(dtype)) return PSGD_E_INVALID_ARG;
-    if (int rc = act_shape(rows, cols)) return rc;
+    if (int rc = act_shape(rows, cols, dtype)) return rc;
     if (bad_ld(ld, cols) || bad_ldc(ldc, cols) || misaligned(x) || misaligned(codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;
     const ActGrid g = act_grid(rows, cols, dtype);
@@ -412,7 +413,7 @@ int psgd_act_store(void* stream, int64_t rows, int64_t cols, const void* x, int 
 
 int psgd_act_restore(void* stream, int64_t rows, int64_t cols, const int8_t* codes, int64_t ldc, const uint8_t* scales, void* x, int dtype, int64_t ld) {
     if ((rows != 0 && (!x || bad_codes(codes, scales))) || bad_dtype(dtype)) return PSGD_E_INVALID_ARG;
-    if (int rc = act_shape(rows, cols)) return rc;
+    if (int rc = act_shape(rows, cols, dtype)) return rc;
     if (bad_ld(ld, cols) || bad_ldc(ldc, cols) || misaligned(x) || misaligned(codes)) return PSGD_E_ALIGN;
     return act_restore(stream, rows, cols, codes, ldc, scales, x, dtype, ld, act_stream(rows, cols, dtype, 1));
 }
@@ -422,7 +423,7 @@ int psgd_act_glu(void* stream, int64_t rows, int64_t cols, int act, int dtype, c
     if (bad_dtype(dtype) || (act != PSGD_SILU && act != PSGD_GELU)) return PSGD_E_INVALID_ARG;
     if (rows != 0 && (!gate || !h || bad_codes(gate_codes, gate_scales))) return PSGD_E_INVALID_ARG;
     if (rows != 0 && (up ? bad_codes(up_codes, up_scales) : (up_codes || up_scales))) return PSGD_E_INVALID_ARG;
-    if (int rc = act_shape(rows, cols)) return rc;
+    if (int rc = act_shape(rows, cols, dtype)) return rc;
     if (bad_ld(ld_in, cols) || bad_ld(ld_h, cols) || bad_ldc(ldc, cols) || misaligned(gate) || misaligned(up) || misaligned(h) ||
         misaligned(gate_codes) || misaligned(up_codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;
@@ -450,7 +451,7 @@ int psgd_act_glu_backward(void* stream, int64_t rows, int64_t cols, int act, int
     const bool gated = up_codes != nullptr;
     if (rows != 0 && (!dh || !dgate || bad_codes(gate_codes, gate_scales))) return PSGD_E_INVALID_ARG;
     if (rows != 0 && (gated ? (!up_scales || !dup) : (up_scales || dup))) return PSGD_E_INVALID_ARG;
-    if (int rc = act_shape(rows, cols)) return rc;
+    if (int rc = act_shape(rows, cols, dtype)) return rc;
     if (bad_ld(ld_h, cols) || bad_ld(ld_out, cols) || bad_ldc(ldc, cols) || misaligned(dh) || misaligned(dgate) || misaligned(dup) ||
         misaligned(gate_codes) || misaligned(up_codes)) return PSGD_E_ALIGN;
     if (rows == 0) return PSGD_OK;

@@ -30,3 +30,17 @@ def test_a_piece_that_one_launch_takes(lib, vocab, most):
 
     assert size(1 << 26) == size(most) != size(most // 2)
     assert size(0) <= size(most)
+
+
+@pytest.mark.parametrize("dtype,cols", [(psgd.PSGD_BF16, 32 * 2048), (psgd.PSGD_F32, 32 * 1024)])
+def test_more_than_one_launch_of_activations(lib, dtype, cols):
+    """2^33 pieces of 16 bytes, two to a thread, would be 2^32 threads: refused as sizes, not by the launch."""
+    P, rows = 4096, 1 << 20
+    for n in (rows, rows + 1):
+        assert lib.psgd_act_store(None, n, cols, P, dtype, cols, P, cols, P) == psgd.PSGD_E_SHAPE
+        assert lib.psgd_act_restore(None, n, cols, P, cols, P, P, dtype, cols) == psgd.PSGD_E_SHAPE
+        assert lib.psgd_act_glu(None, n, cols, 0, dtype, P, None, cols, P, cols, P, P, None, None, cols) == psgd.PSGD_E_SHAPE
+        assert lib.psgd_act_glu_backward(None, n, cols, 0, dtype, P, P, None, None, cols, P, cols, P, None, cols) == psgd.PSGD_E_SHAPE
+    # (that one row less is taken shows where nothing is launched)
+    assert lib.psgd_act_wgrad_workspace_bytes(rows, 8, 32 * 2048, psgd.PSGD_BF16) == 0
+    assert lib.psgd_act_wgrad_workspace_bytes(rows - 1, 8, 32 * 2048, psgd.PSGD_BF16) > 0
