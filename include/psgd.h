@@ -305,8 +305,9 @@ int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
 /* The output head: logits l = X W^T of tokens x vocab, softmax cross entropy against labels, without logits in memory.
  *   lse_t = log sum_v exp(l_tv);  loss_t = lse_t - l_t,label(t);
  *   D_tv = c_t (exp(l_tv - lse_t) - [v = label(t)]);  dX = D W;  dW = D^T X.
- * A token whose label lies outside [0, vocab) does not count: its loss and its row of dX are 0 and its row of X is not
- * looked at.  Exponentials and D exist for one piece of the tokens at a time, in the workspace.
+ * A token whose label lies outside [0, vocab) does not count: its loss and its row of dX are 0, and what its row of X holds,
+ * NaN or not, reaches no result.  dX may take X's place (the same pointer and leading dimension); apart from that loss, dX and dW overlap neither each other nor
+ * X, W, labels and weights (INVALID_ARG).  Exponentials and D exist for one piece of the tokens at a time, in the workspace.
  * Arithmetic: bf16 X and W are multiplied on the matrix cores as they are, fp32 ones as three bf16 planes (24 bits); sums, statistics and losses are fp32.  D is
  * rounded once to bf16 for results in bf16; for results in fp32 it has three bf16 planes. */
 typedef struct {

@@ -448,7 +448,7 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.rows = take((size_t)tokens * 4);
     p.label = take((size_t)tokens * 4);
     p.counts = take((size_t)(tokens + 63) / 64 * 8);
-    p.xc = p.direct ? 0 : take((size_t)tokens * p.ldc * 2 * p.x_planes);
+    p.xc = p.direct && !gradients ? 0 : take((size_t)tokens * p.ldc * 2 * p.x_planes);      // (direct: where dX takes X's place)
     p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2) : 0;
     p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
     p.at_label = take((size_t)p.piece * 4);
@@ -522,6 +522,22 @@ static hipError_t launch_rows(const HeadDev& h, int first, int rows, hipStream_t
     return hipGetLastError();
 }
 
+// rows of `width` bytes, `stride` bytes apart
+struct HeadArea { const void* ptr; int64_t rows, stride, width; };
+// (columns of one buffer beside each other do not overlap; areas with different strides do where their ranges do)
+static bool overlap(HeadArea a, HeadArea b) {
+    if (a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0 || !a.ptr || !b.ptr) return false;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr));
+    if (apart >= (a.rows - 1) * a.stride + a.width || -apart >= (b.rows - 1) * b.stride + b.width) return false;
+    if (a.rows == 1) a.stride = b.stride;
+    if (b.rows == 1) b.stride = a.stride;
+    if (a.stride != b.stride || a.width > a.stride || b.width > b.stride) return true;
+    // b's first row begins in row `down` of a, at column `right`
+    const int64_t down = apart >= 0 ? apart / a.stride : -((-apart + a.stride - 1) / a.stride), right = apart - down * a.stride;
+    auto rows_meet = [&](int64_t d) { return d < a.rows && d + b.rows > 0; };
+    return (right < a.width && rows_meet(down)) || (right + b.width > a.stride && rows_meet(down + 1));
+}
+
 static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
                     const float* weight, float* loss, void* dx, void* dw, int accumulate) {
     if (int rc = head_shape(s)) return rc;
@@ -530,6 +546,15 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     if (ldx > kMaxLd || ldw > kMaxLd || lddx > kMaxLd || lddw > kMaxLd) return PSGD_E_SHAPE;
     if (bad_ld(ldx, s->d) || bad_ld(ldw, s->d) || misaligned(x) || misaligned(w) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
     if (gradients && (bad_ld(lddx, s->d) || bad_ld(lddw, s->d) || misaligned(dx) || misaligned(dw))) return PSGD_E_ALIGN;
+    const int64_t size = s->dtype == PSGD_F32 ? 4 : 2, g_size = s->grad_dtype == PSGD_F32 ? 4 : 2;
+    const bool in_place = gradients && x && x == dx && (ldx == lddx || s->tokens == 1);
+    const HeadArea in[] = {{x, s->tokens, ldx * size, s->d * size}, {w, s->vocab, ldw * size, s->d * size}, {labels, 1, 0, s->tokens * 8},
+                           {weight, 1, 0, s->tokens * 4}};
+    const HeadArea out[] = {{dx, s->tokens, lddx * size, s->d * size}, {dw, s->vocab, lddw * g_size, s->d * g_size}, {loss, 1, 0, s->tokens * 4}};
+    for (const HeadArea& o : out)
+        for (const HeadArea& i : in)
+            if (overlap(o, i) && !(in_place && &o == out && &i == in)) return PSGD_E_INVALID_ARG;
+    if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return PSGD_E_INVALID_ARG;
     const HeadPlan p = head_plan(*s, gradients);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -566,9 +591,14 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
         if (launch_planes(w, PSGD_BF16, s->vocab, s->d, ldw, to, 1, st) != hipSuccess) return PSGD_E_HIP;
         wc = to, ldwc = p.ldc;
     }
+    if (p.direct && in_place) {        // dW takes X after dX, or beside it
+        if (launch_planes(x, PSGD_BF16, s->tokens, s->d, ldx, xc, 1, st) != hipSuccess) return PSGD_E_HIP;
+        x = xc;
+    }
+    const int64_t ld_direct = in_place ? p.ldc : ldx;
     for (int piece = 0; piece < p.pieces; ++piece) {
         const int first = piece * p.piece, rows = (int)std::min<int64_t>(p.piece, s->tokens - first);
-        const TileOperand tokens = h.direct ? TileOperand{static_cast<const bf16_t*>(x) + (int64_t)first * ldx, ldx, 0, rows}
+        const TileOperand tokens = h.direct ? TileOperand{static_cast<const bf16_t*>(x) + (int64_t)first * ld_direct, ld_direct, 0, rows}
                                             : TileOperand{xc + (int64_t)first * p.ldc, p.ldc, s->tokens * p.ldc, rows};
         TileArgs t = {};
         t.count = h.direct ? nullptr : h.count, t.first = first, t.n_split = 1;

@@ -395,7 +395,7 @@ class HeadLoss:
 
     def loss_grad(self, X, W, labels, loss, dX, dW, weight=None, accumulate: bool = False, stream=None) -> None:
         """loss as above; dX <- gradient of sum_t weight[t] loss[t] (weight None: the mean over the tokens that count), and
-        dW <- (accumulate: +=) its gradient."""
+        dW <- (accumulate: +=) its gradient.  dX may be X itself; otherwise results overlap nothing."""
         import torch
         if not self.grad:
             raise ValueError("this HeadLoss has no workspace for gradients (grad=False)")

@@ -3,6 +3,8 @@ import pytest
 import torch
 
 from paper_2509_11254_amd import psgd
+from test_gpu_act import CODE, DT, padded
+from test_gpu_head import inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +25,38 @@ def test_losses_of_more_tokens_than_one_launch_takes():
         want = torch.logsumexp(logits, 1) - logits.gather(1, labels[part].clamp(min=0)[:, None])[:, 0]
         # eight products summed in fp32, here and there: 8 x 2^-24 of |x| |w|, up to 30, twice in a loss
         assert (loss[part] - torch.where(labels[part] >= 0, want, 0.0)).abs().max() < 1e-4
+
+
+# up to 512 tokens whose rows need no padding X is multiplied where it is: few launches, two products in one or in two; else a copy of it
+@pytest.mark.parametrize("tokens,d,vocab,dtype", [(200, 136, 1000, "bf16"), (16, 512, 4400, "bf16"), (500, 1024, 10008, "bf16"), (200, 131, 1000, "bf16"),
+                                                 (700, 136, 1000, "bf16"), (90, 67, 300, "f32")])
+def test_gradient_in_the_place_of_the_tokens(tokens, d, vocab, dtype):
+    x, w, labels = inputs(tokens, d, vocab, DT[dtype], 4)
+    plan = psgd.HeadLoss(tokens, d, vocab, CODE[dtype], psgd.PSGD_F32)
+    results = []
+    for in_place in (False, True):
+        here = padded(x, DT[dtype], 8)[0]
+        loss, dw = torch.empty(tokens, device="cuda"), torch.empty((vocab, (d + 7) // 8 * 8), device="cuda")[:, :d]
+        dx = here if in_place else padded(torch.zeros((tokens, d)), DT[dtype], 8)[0]
+        plan.workspace.fill_(0xFF)
+        plan.loss_grad(here, w, labels, loss, dx, dw)
+        results.append((loss, dx, dw))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert torch.isfinite(results[1][2]).all() and (results[1][1] != 0).any()
+
+
+def test_gradient_beside_the_tokens():
+    """X and dX as columns of one buffer."""
+    tokens, d, vocab = 100, 64, 300
+    x, w, labels = inputs(tokens, d, vocab, torch.bfloat16, 5)
+    plan = psgd.HeadLoss(tokens, d, vocab)
+    results = []
+    for right in (True, False, None):
+        buf = torch.zeros((tokens, 2 * d), dtype=torch.bfloat16, device="cuda")
+        here, dx = (buf[:, :d], buf[:, d:]) if right else (buf[:, d:], buf[:, :d])
+        dx = torch.zeros((tokens, d), dtype=torch.bfloat16, device="cuda") if right is None else dx
+        here.copy_(x)
+        loss, dw = torch.empty(tokens, device="cuda"), torch.empty((vocab, d), dtype=torch.bfloat16, device="cuda")
+        plan.loss_grad(here, w, labels, loss, dx, dw)
+        results.append((loss, dx.clone(), dw))
+    assert all(torch.equal(a, b) for r in results[:2] for a, b in zip(r, results[2]))

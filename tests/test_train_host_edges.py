@@ -44,3 +44,25 @@ def test_more_than_one_launch_of_activations(lib, dtype, cols):
     # (that one row less is taken shows where nothing is launched)
     assert lib.psgd_act_wgrad_workspace_bytes(rows, 8, 32 * 2048, psgd.PSGD_BF16) == 0
     assert lib.psgd_act_wgrad_workspace_bytes(rows - 1, 8, 32 * 2048, psgd.PSGD_BF16) > 0
+
+
+def test_head_refuses_results_over_inputs(lib):
+    """100 tokens, d = 64, 1000 words, bf16 with dW in fp32: X and dX have 12800 bytes, W 128000, dW 256000, labels 800, losses and weights 400."""
+    place = dict(x=1 << 20, w=2 << 20, labels=3 << 20, weight=4 << 20, loss=5 << 20, dx=6 << 20, dw=7 << 20)
+
+    def call(desc=None, **change):
+        a = dict(place, **change)
+        return lib.psgd_head_loss_grad(C.byref(desc or head()), 4096, None, a["x"], a["w"], a["labels"], a["weight"], a["loss"], a["dx"], a["dw"], 0)
+
+    last = dict(x=12800, w=128000, labels=800, weight=400, loss=400, dx=12800, dw=256000)
+    for out in ("loss", "dx", "dw"):
+        for other in set(place) - {out}:
+            # begins in the other's last 16 bytes, or ends in its first
+            for at in (place[other] + last[other] // 16 * 16 - 16, place[other] - last[out] // 16 * 16 + 16):
+                assert call(**{out: at}) == psgd.PSGD_E_INVALID_ARG, (out, other)
+    assert call(dx=place["x"], desc=head(ldx=72)) == psgd.PSGD_E_INVALID_ARG         # X's place, but other rows
+    # columns of one buffer: the last of one are the first of the other's
+    for shift in (-56, 56, 128 - 56, 56 - 128):
+        assert call(dx=place["x"] + 2 * shift, desc=head(ldx=128, lddx=128)) == psgd.PSGD_E_INVALID_ARG, shift
+    loss = lib.psgd_head_loss(C.byref(head()), 4096, None, place["x"], place["w"], place["labels"], place["labels"] + 796)
+    assert loss == psgd.PSGD_E_INVALID_ARG
