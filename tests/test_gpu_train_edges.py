@@ -1,4 +1,6 @@
 """The training operators at the ends of what their arguments may be."""
+import math
+
 import pytest
 import torch
 
@@ -60,3 +62,33 @@ def test_gradient_beside_the_tokens():
         plan.loss_grad(here, w, labels, loss, dx, dw)
         results.append((loss, dx.clone(), dw))
     assert all(torch.equal(a, b) for r in results[:2] for a, b in zip(r, results[2]))
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_gelu_far_below_zero(gated):
+    """fp32, to -12, where the distribution function is 1e-33: its relative error, not that of one minus nearly one."""
+    x = torch.linspace(-12, 0, 4096, dtype=torch.float64).reshape(16, 256)
+    gate, _ = padded(x, torch.float32)
+    up = padded(torch.full_like(x, 0.75), torch.float32)[0] if gated else None
+    dh, _ = padded(torch.full_like(x, 0.5), torch.float32)
+    h, dgate = (padded(torch.zeros_like(x), torch.float32)[0] for _ in range(2))
+    dup = padded(torch.zeros_like(x), torch.float32)[0] if gated else None
+    kg, ku = psgd.act_empty(16, 256), psgd.act_empty(16, 256) if gated else None
+    psgd.act_glu(gate, up, h, kg, ku, act=psgd.PSGD_GELU)
+    psgd.act_glu_backward(kg, ku, dh, dgate, dup, act=psgd.PSGD_GELU)
+    kept, _ = padded(torch.zeros_like(x), torch.float32)
+    psgd.act_restore(kg, kept)
+    factor = 0.75 if gated else 1.0          # (0.75 is 96 times a power of two: exact in 8 bits)
+
+    def parts(t):
+        # the function and its density; an error of 2^-23 of x or of x^2 / 2 is x^2 times as much of either, the functions' own is a few 2^-24
+        t = t.double().cpu()
+        return t, 0.5 * torch.erfc(-t / math.sqrt(2)), torch.exp(-t * t / 2) / math.sqrt(2 * math.pi), 2.0 ** -20 + t * t * 2.0 ** -22
+
+    g, cdf, _, unit = parts(gate)
+    assert ((h.double().cpu() - g * cdf * factor).abs() <= unit * (g * cdf * factor).abs() + 1e-37).all()
+    g, cdf, density, unit = parts(kept)
+    want = 0.5 * factor * (cdf + g * density)
+    assert ((dgate.double().cpu() - want).abs() <= unit * 0.5 * factor * (cdf + (g * density).abs()) + 1e-37).all()
+    if gated:
+        assert ((dup.double().cpu() - 0.5 * g * cdf).abs() <= unit * (0.5 * g * cdf).abs() + 1e-37).all()
