@@ -41,13 +41,14 @@ __device__ __forceinline__ void store_row(PSGD_GLOBAL bf16_t* p, const float (&v
 // what a product kernel writes
 enum TileKind { TILE_PART = 0, TILE_F32 = 1, TILE_BF16 = 2 };
 
-// contraction steps and rows of C that count
+// contraction steps and rows of C that count, and the chunks that the shape takes them in
 struct TileSize { int K, nl, chunks; };
+template <TileShape SHAPE>
 __device__ inline TileSize tile_size(const TileArgs& t) {
     TileSize s;
     s.K = t.count_is_k ? counted(t, t.K) : t.K;
     s.nl = t.count_is_k ? t.L.extent : counted(t, t.L.extent);
-    s.chunks = (s.K + kTileK - 1) / kTileK * t.n_pairs;
+    s.chunks = (s.K + tile_k(SHAPE) - 1) / tile_k(SHAPE) * t.n_pairs;
     return s;
 }
 
@@ -55,7 +56,7 @@ __device__ inline TileSize tile_size(const TileArgs& t) {
 template <bool LKC, TileShape SHAPE, int KIND, bool CODES>
 __device__ __forceinline__ void product_tile(int id, const TileArgs& t, const TileOut& o, const TileCodes& codes, PSGD_TLDS unsigned char* lds) {
     using T = Tile<false, LKC, SHAPE>;
-    const TileSize size = tile_size(t);
+    const TileSize size = tile_size<SHAPE>(t);
     const TileGrid grid = tile_grid<SHAPE>(t, size.nl, size.chunks);
     const TilePlace at = tile_place(id, grid);
     if (at.split < 0 || (size.K == 0 && o.skip_empty)) return;
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(kTileThreads, tile_share(TILE_MANY)) void pair_kern
 // sum over the splits, in their order, of four elements per thread
 template <TileShape SHAPE>
 __global__ __launch_bounds__(kThreads) void split_sum_kernel(TileArgs t, TileOut o) {
-    const TileSize size = tile_size(t);
+    const TileSize size = tile_size<SHAPE>(t);
     if (size.K == 0 && o.skip_empty) return;
     const int nl = size.nl, n_split = tile_grid<SHAPE>(t, nl, size.chunks).n_split;
     const float scale = o.scale ? *o.scale : 1.f;
