@@ -344,6 +344,8 @@ def _matrix(name: str, t, rows: int, cols: int, dtype: Optional[int] = None) -> 
         raise ValueError("%s: wrong element type %s" % (name, t.dtype))
     # (with one row the stride says nothing)
     ld = int(t.stride(0)) if rows > 1 else (cols + 7) // 8 * 8
+    if ld < cols:
+        raise ValueError("%s: rows that lie over each other (%d elements apart, %d columns)" % (name, ld, cols))
     if rows and t.storage_offset() + (rows - 1) * ld + (cols + 7) // 8 * 8 > t.untyped_storage().nbytes() // t.element_size():
         raise ValueError("%s: the last row ends before the next multiple of 8 columns, up to which rows may be read" % name)
     return ld
