@@ -475,6 +475,7 @@ def act_glu(gate, up, h, kept_gate: Act8, kept_up: Optional[Act8], act: int = PS
     lib = load_library()
     rows, cols, dt = kept_gate.rows, kept_gate.cols, _dtype_code(gate)
     ld_in, ld_h = _matrix("gate", gate, rows, cols), _matrix("h", h, rows, cols, dt)
+    _same("presence of up and of its checkpoint", up is None, kept_up is None)
     if up is not None:
         _same("leading dimensions of gate and up", ld_in, _matrix("up", up, rows, cols, dt))
         _same("checkpoints of gate and up", (rows, cols, kept_gate.ldc), (kept_up.rows, kept_up.cols, kept_up.ldc))

@@ -106,3 +106,15 @@ def test_tensors_of_another_device(monkeypatch, name):
                 call(*[a(1 - device if j == i else device) for j, a in enumerate(args)], stream)
     with pytest.raises(ValueError, match="cuda"):
         call(*[a(1) for a in args], None)
+
+
+def test_a_gated_unit_has_both_checkpoints_or_neither(monkeypatch):
+    """up without a place for its checkpoint, and a checkpoint that would be left as it was."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    m, k = (lambda: matrix(6, 40)), (lambda: checkpoint(6, 40))
+    for up, kept_up in ((m(), None), (None, k())):
+        with pytest.raises(ValueError, match="up"):
+            psgd.act_glu(m(), up, m(), k(), kept_up)
+    for kept_up, dup in ((k(), None), (None, m())):
+        with pytest.raises(ValueError, match="up"):
+            psgd.act_glu_backward(k(), kept_up, m(), m(), dup)
