@@ -297,9 +297,10 @@ int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
 /* ---- the training step around the compressor: the output head's loss, 8-bit activations, weight gradients -------------
  *
  * The calls below have no context.  Matrices are row-major device memory with a leading dimension in elements, a multiple of 8 (codes:
- * of 16) that is at least the columns and at most 2^22; bases are 16-byte aligned.  Elements beyond the columns are never taken as data nor written,
+ * of 16) that is at least the columns and, of the matrices that are multiplied, at most 2^22; bases are 16-byte aligned.  Unless a call says otherwise, what is written overlaps nothing else.  Elements beyond the columns are never taken as data nor written,
  * up to the next multiple of 8 they may be read, so the last row's are part of the buffer as well.  Work is enqueued on `stream`, nothing is kept from one call to the next, and a
- * workspace (256-byte aligned, of the bytes that the call's _workspace_bytes function gives; 0 = the arguments are refused) holds nothing between calls.  The calls launch kernels only and
+ * workspace (256-byte aligned, of the bytes that the call's _workspace_bytes function gives; 0 = the arguments are refused) holds nothing between calls.  Calls
+ * that may run at the same time, on streams that do not wait for each other, have a workspace each.  The calls launch kernels only and
  * may be recorded by a capturing stream at any time.  Where there are no rows (tokens) the matrices that have them may be NULL.  Results do not depend on the order in which the GPU runs their parts.  */
 
 /* The output head: logits l = X W^T of tokens x vocab, softmax cross entropy against labels, without logits in memory.

@@ -5,14 +5,17 @@
 //   (D is kept relative to the largest c_t, which the products are multiplied by at their end)
 //
 // Tokens whose label lies outside [0, V) do not count: their rows are left out from the start (the others are copied together,
-// in order), so that what they hold, NaN or not, reaches neither sum nor product.
+// in order), or, of few tokens, out of all that is made of their logits, so that what they hold, NaN or not, reaches no result.
 //
-// The vocabulary is walked in tiles of 256 (128 for few tokens, and in fp32).  A workgroup has the logits of a tile of tokens and one tile in its accumulators, takes the
+// The vocabulary is walked in tiles of 256 (128 for few tokens; in fp32 128 or 64).  A workgroup has the logits of a tile of tokens and one tile in its accumulators, takes the
 // tile's maximum and its sum of exponentials (the label's left out) per token, and writes these two numbers; for the gradients it writes the exponentials
 // relative to the tile's maximum as well, for one piece of the tokens at a time.  One more pass over a piece joins the tiles'
 // numbers to lse_t and turns the exponentials into D in place, and the two products with D follow.
 //
-// The three products bound it: of 8192 x 4096 x 64000 in bf16 (10.0 ms) the logits take 3.2 ms, 1.33 PFLOP/s, D W 3.1 and D^T X 3.2; the pass that makes D reads and writes 2.1 GB in
+// For results in bf16 D is rounded to bf16, like the result itself: errors against 64 bits of 1.8e-3 (8192 x 4096 x 64000) to 2.2e-3 (200 x 1024 x 10007) of the gradients' norm,
+// where D in 32 bits and the result rounded has 1.7e-3.  A second plane of D would take the two products' time, most of the whole, once more.
+//
+// The three products bound it: of 8192 x 4096 x 64000 in bf16 (9.9 to 10.1 ms) the logits take 3.2 to 3.3 ms, 1.3 PFLOP/s, D W 3.1 and D^T X 3.2; the pass that makes D reads and writes 2.1 GB in
 // 0.34 ms, 6.1 TB/s, and the tokens' copy takes 0.03.  Of one token the loss alone reads W at 5 TB/s.
 #include "tile_dev.h"
 
@@ -427,7 +430,7 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     // (Two planes of D for dW in fp32 from bf16 X: 2124 us in place of 2830 for 4096 x 2048 x 32000, 81 in place of 88 for 1391 x 384 x 4477, and an error of
     // dW of 1.5e-6 in place of 3e-7, where products in fp32 have 7e-7.)
     p.dw_pairs = !f32 && p.d_planes == 3 ? kPairsL3 : kPairs1, p.n_dw_pairs = !f32 ? p.d_planes : 1;
-    // tokens per piece
+    // tokens per piece (statistics: 8 bytes for each tile of 128 words; tiles of 64 are not taken for so many tokens, but where all words are in one)
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
     const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
     const int64_t launch = std::min(kMaxPiece, std::max<int64_t>(1, kMaxPieceLogits / s.vocab));

@@ -259,7 +259,7 @@ struct Tile {
     // P's of the next.  The barrier is before a chunk's last 16 steps, when their fragments are in registers: every wave is then done
     // with both places of the chunk, and its loads of the next chunk have arrived.  After it L's part of the chunk after the next goes to
     // one of the places, and then P's of the chunk after that.  Past the end the loads bring zeros, so that no wait depends on where one is.
-    // 8192 x 11008 x 4096 (both operands K-strided) takes 600 us, 1.23 PFLOP/s; eight waves of 64 x 128 in two stages reached 0.85.  Without its loads the loop does
+    // 8192 x 11008 x 4096 (both operands K-strided) takes 600 to 615 us in passes after each other, 1.20 to 1.23 PFLOP/s; eight waves of 64 x 128 in two stages reached 0.85.  Without its loads the loop does
     // 1.7 to 1.8 PFLOP/s, and with zeros for data 1.5: what bounds it is the power that its operands' bits take.
     __device__ __forceinline__ void run_full(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
                                              const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
@@ -453,8 +453,9 @@ struct Tile {
         }
     }
 
-    // The same with P from an 8-bit checkpoint: a thread has 32 codes of a row, a group, at a time, the next chunk's while this one is multiplied, and
-    // writes their values to LDS where the direct loads would have put them (16-byte pieces in an order that spreads four rows over the banks).
+    // The same with P from an 8-bit checkpoint: a thread has 32 codes of a row, a group, at a time and writes their values to LDS where the direct loads would have
+    // put them (16-byte pieces in an order that spreads four rows over the banks).  The next chunk's codes are loaded beside this one's part of L, with one wait
+    // for both: a latency less per chunk, though none of it runs beside the products.
     __device__ __forceinline__ void run_codes(const TileArgs& t, const TileCodes& codes, int p0, int l0, int K, int n0, int n, int per, int wv, const SideL& sl,
                                               const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl, PSGD_TLDS unsigned char* lds) {
         static_assert(!PKC && BP == 128 && kTileThreads == 256, "32 codes per thread and chunk");

@@ -378,7 +378,8 @@ class HeadLoss:
     """Softmax cross entropy of X W^T against labels without logits in memory, and its gradients: psgd_head_loss and
     psgd_head_loss_grad with a torch-allocated workspace, for one set of sizes and types.
 
-    A token whose label lies outside [0, vocab) does not count.  grad=False: losses alone (a smaller workspace).
+    A token whose label lies outside [0, vocab) does not count.  grad=False: losses alone (a smaller workspace).  Calls on streams
+    that do not wait for each other need an object each: they would share the workspace.
     """
 
     def __init__(self, tokens: int, d: int, vocab: int, dtype: int = PSGD_BF16, grad_dtype: Optional[int] = None, *,
@@ -502,7 +503,7 @@ def act_glu_backward(kept_gate: Act8, kept_up: Optional[Act8], dh, dgate, dup, a
 
 class WeightGrad:
     """psgd_act_wgrad with a torch-allocated workspace, for one set of sizes and types: G = dY^T X from dY and the 8-bit
-    checkpoint of X."""
+    checkpoint of X.  Calls on streams that do not wait for each other need an object each: they would share the workspace."""
 
     def __init__(self, tokens: int, out_features: int, in_features: int, dtype: int = PSGD_BF16,
                  grad_dtype: Optional[int] = None, *, device: str = "cuda"):
