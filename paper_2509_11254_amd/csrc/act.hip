@@ -357,6 +357,7 @@ static int act_restore(void* stream, int64_t rows, int64_t cols, const int8_t* c
     if (rows == 0) return PSGD_OK;
     const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
 #define PSGD_RESTORE(T, STREAM) hipLaunchKernelGGL((act_restore_kernel<T, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, codes, scales, ldc, (T*)x, ld)
     if (dtype == PSGD_F32) { if (stream_it) PSGD_RESTORE(float, true); else PSGD_RESTORE(float, false); }
     else                   { if (stream_it) PSGD_RESTORE(bf16_t, true); else PSGD_RESTORE(bf16_t, false); }
@@ -403,6 +404,7 @@ int psgd_act_store(void* stream, int64_t rows, int64_t cols, const void* x, int 
     if (rows == 0) return PSGD_OK;
     const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
     const ActOut out = {codes, scales};
 #define PSGD_STORE(T, STREAM) hipLaunchKernelGGL((act_store_kernel<T, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, (const T*)x, ld, out, ldc)
     const bool stream_it = act_stream(rows, cols, dtype, 1);
@@ -430,6 +432,7 @@ int psgd_act_glu(void* stream, int64_t rows, int64_t cols, int act, int dtype, c
     if (rows == 0) return PSGD_OK;
     const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
     const ActOut kg = {gate_codes, gate_scales}, ku = {up_codes, up_scales};
     const bool stream_it = act_stream(rows, cols, dtype, up ? 3 : 2);
 #define PSGD_GLU(T, ACT, GATED, STREAM)                                                                                                       \
@@ -458,6 +461,7 @@ int psgd_act_glu_backward(void* stream, int64_t rows, int64_t cols, int act, int
     if (rows == 0) return PSGD_OK;
     const ActGrid g = act_grid(rows, cols, dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
     const bool stream_it = act_stream(rows, cols, dtype, gated ? 3 : 2);
 #define PSGD_GLU(T, ACT, GATED, STREAM)                                                                                                       \
     hipLaunchKernelGGL((act_glu_backward_kernel<T, ACT, GATED, STREAM>), g.grid, dim3(kThreads), 0, st, g.rows, gate_codes,    \
@@ -485,6 +489,7 @@ int psgd_act_wgrad(void* workspace, void* stream, int64_t tokens, int64_t out_fe
     if (bad_ld(ldy, out_features) || bad_ld(ldg, in_features) || bad_ldc(ldc, in_features) || misaligned(dy) || misaligned(g) ||
         misaligned(codes) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
     const WgradPlan w = wgrad_plan(tokens, out_features, in_features, dtype);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     bf16_t* x = reinterpret_cast<bf16_t*>(ws + w.x);

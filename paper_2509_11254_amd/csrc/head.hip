@@ -560,6 +560,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return PSGD_E_INVALID_ARG;
     const HeadPlan p = head_plan(*s, gradients);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const bool f32 = s->dtype == PSGD_F32;
 

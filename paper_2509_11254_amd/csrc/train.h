@@ -89,6 +89,8 @@ hipError_t launch_code_product(const TileCodes& codes, const TileArgs& t, const 
 // rows x cols (ld) of fp32 or bf16 to `planes` bf16 planes [rows][round_up(cols, 8)], zeros beyond cols
 hipError_t launch_planes(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bf16_t* dst, int planes, hipStream_t st);
 
+// Whether a launch succeeded is asked of hipGetLastError(), which keeps what any earlier call of the program left: each entry point begins without it.
+inline void forget_errors() { (void)hipGetLastError(); }
 inline int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline bool bad_dtype(int t) { return t != PSGD_F32 && t != PSGD_BF16; }

@@ -92,3 +92,32 @@ def test_gelu_far_below_zero(gated):
     assert ((dgate.double().cpu() - want).abs() <= unit * 0.5 * factor * (cdf + (g * density).abs()) + 1e-37).all()
     if gated:
         assert ((dup.double().cpu() - 0.5 * g * cdf).abs() <= unit * (0.5 * g * cdf).abs() + 1e-37).all()
+
+
+@pytest.mark.parametrize("tokens", [20, 600])
+def test_errors_of_others_before_the_call(tokens):
+    """An error that an earlier HIP call of the program left behind (here: a device that does not exist) is not the library's: its calls do their work and
+    say so."""
+    d, vocab = 64, 300
+    lib = psgd.load_library()
+    x, w, labels = inputs(tokens, d, vocab, torch.bfloat16, 6)
+    head, wgrad = psgd.HeadLoss(tokens, d, vocab), psgd.WeightGrad(tokens, d, d)
+    gate = padded(torch.randn((tokens, d)), torch.bfloat16)[0]
+
+    def step(before):
+        loss, dx, dw = torch.zeros(tokens, device="cuda"), torch.zeros_like(gate), torch.zeros((vocab, d), dtype=torch.bfloat16, device="cuda")
+        h, y, dg, du = (torch.zeros_like(gate) for _ in range(4))
+        g = torch.zeros((d, d), dtype=torch.bfloat16, device="cuda")
+        alone = torch.zeros_like(loss)
+        kg, ku, kh = (psgd.act_empty(tokens, d) for _ in range(3))
+        for call in (lambda: head.loss(x, w, labels, alone), lambda: head.loss_grad(x, w, labels, loss, dx, dw), lambda: psgd.act_glu(gate, gate, h, kg, ku),
+                     lambda: psgd.act_store(h, kh), lambda: psgd.act_restore(kh, y), lambda: wgrad.run(gate, kh, g),
+                     lambda: psgd.act_glu_backward(kg, ku, gate, dg, du)):
+            before()
+            call()
+        return alone, loss, dx, dw, h, y, g, dg, du
+
+    want = step(lambda: None)
+    got = step(lambda: lib["hipSetDevice"](1 << 20))
+    assert lib["hipGetLastError"]() in (0, 101)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
