@@ -309,7 +309,8 @@ int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
  * A token whose label lies outside [0, vocab) does not count: its loss and its row of dX are 0, and what its row of X holds,
  * NaN or not, reaches no result.  dX may take X's place (the same pointer and leading dimension); apart from that loss, dX and dW overlap neither each other nor
  * X, W, labels and weights (INVALID_ARG).  Exponentials and D exist for one piece of the tokens at a time, in the workspace.
- * Arithmetic: bf16 X and W are multiplied on the matrix cores as they are, fp32 ones as three bf16 planes (24 bits); sums, statistics and losses are fp32.  D is
+ * Arithmetic: bf16 X and W are multiplied on the matrix cores as they are, fp32 ones as three bf16 planes (24 bits; what is infinite or beyond
+ * bf16's largest number, 3.39e38, makes NaN of the sums it enters); sums, statistics and losses are fp32.  D is
  * rounded once to bf16 for results in bf16; for results in fp32 it has three bf16 planes. */
 typedef struct {
     int64_t tokens, d, vocab;   /* X: tokens x d, W: vocab x d; tokens may be 0                      */
@@ -357,7 +358,7 @@ int psgd_act_glu_backward(void *stream, int64_t rows, int64_t cols, int act, int
 
 /* The weight gradient of Y = X W^T from dY and the checkpoint of X:  G = dY^T X, or with accumulate != 0 G += dY^T X.
  * dY: tokens x out_features (dtype, ldy); checkpoint: tokens x in_features; G: out_features x in_features (g_dtype, ldg), as psgd_compress takes it.
- * tokens may be 0.  bf16 dY is multiplied as it is, fp32 as three bf16 planes; sums are fp32. */
+ * tokens may be 0.  bf16 dY is multiplied as it is, fp32 as three bf16 planes (as the head's); sums are fp32. */
 size_t psgd_act_wgrad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features, int dtype);
 int psgd_act_wgrad(void *workspace, void *stream, int64_t tokens, int64_t out_features, int64_t in_features,
                    const void *dy, int dtype, int64_t ldy, const int8_t *codes, int64_t ldc, const uint8_t *scales,
