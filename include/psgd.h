@@ -294,7 +294,7 @@ int psgd_profile_enable(psgd_ctx *ctx, int max_records);
 int psgd_profile_select(psgd_ctx *ctx, int tag_mask);
 int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
 
-/* ---- the training step around the compressor: the output head's loss, 8-bit activations, weight gradients -------------
+/* ---- the training step around the compressor: the output head's loss, 8-bit activations, weight gradients, norms, experts ----
  *
  * The calls below have no context.  Matrices are row-major device memory with a leading dimension in elements, a multiple of 8 (codes:
  * of 16) that is at least the columns and, of the matrices that are multiplied, at most 2^22; bases are 16-byte aligned.  Unless a call says otherwise, what is written overlaps nothing else.  Elements beyond the columns are never taken as data nor written,
@@ -363,6 +363,47 @@ size_t psgd_act_wgrad_workspace_bytes(int64_t tokens, int64_t out_features, int6
 int psgd_act_wgrad(void *workspace, void *stream, int64_t tokens, int64_t out_features, int64_t in_features,
                    const void *dy, int dtype, int64_t ldy, const int8_t *codes, int64_t ldc, const uint8_t *scales,
                    void *g, int g_dtype, int64_t ldg, int accumulate);
+
+/* Layer normalisation of the rows of s = x, or with add (total and add are there both or neither) s = x + add, rounded to the type and written to total:
+ *   mean = sum_c s / cols, var = sum_c (s - mean)^2 / cols, r = 1 / sqrt(var + eps);  y = (s - mean) r weight + bias.
+ * weight, bias: cols elements of w_dtype, or NULL (1 and 0).  stats, nullable: rows x 2 fp32, mean and r, for the backward pass.  total and y have ld_out, x and add
+ * ld_in; total or y may take the place of x or add (the same pointer and leading dimension).  Statistics and sums are fp32 (squares beyond 3.4e38 are not held).
+ * cols: at most 16384.  rows may be 0.  Errors: INVALID_ARG (null pointer, bad enum, eps negative or not finite, an overlap), SHAPE, ALIGN, HIP. */
+int psgd_norm(void *stream, int64_t rows, int64_t cols, int dtype, const void *x, const void *add /* nullable */, int64_t ld_in,
+              const void *weight /* nullable */, const void *bias /* nullable */, int w_dtype, float eps, void *total /* nullable */,
+              void *y, int64_t ld_out, float *stats /* nullable */);
+/* With u = (x - mean) r and g = dy weight:  dx = r (g - mean_c g - u mean_c(g u)) + dtotal;  dweight = sum_rows dy u, dbias = sum_rows dy,
+ * written or, with accumulate != 0, added to.  x: what was normalised (total, where there was one); stats: psgd_norm's; dtotal: the gradient that reaches
+ * it past the norm (ld_dx), or NULL.  dx may take the place of dy, x or dtotal.  dweight, dbias: cols elements of g_dtype, each nullable;
+ * without either the workspace may be NULL. */
+size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype);
+int psgd_norm_backward(void *workspace, void *stream, int64_t rows, int64_t cols, int dtype, const void *dy, int64_t ld_dy,
+                       const void *x, int64_t ld_x, const void *weight /* nullable */, int w_dtype, const float *stats,
+                       const void *dtotal /* nullable */, void *dx, int64_t ld_dx, void *dweight /* nullable */,
+                       void *dbias /* nullable */, int g_dtype, int accumulate);
+
+/* Tokens sorted by the experts they chose, `slots` choices each (choice: tokens x slots; outside [0, experts): the choice does not count).
+ * Rows are counted through the experts in their order, within an expert through the choices in theirs (token by token):
+ *   offsets[e]   (experts + 1)      first row of expert e; offsets[experts]: rows in all, at most tokens * slots
+ *   place[t, s]  (tokens x slots)   row of choice s of token t, -1 where it does not count
+ *   order[j]     (tokens * slots)   t * slots + s of row j, -1 behind the last
+ * All contiguous.  tokens may be 0.  At most 1024 experts and 2^30 choices.  Errors: INVALID_ARG (null pointer, an overlap), SHAPE, ALIGN, HIP. */
+size_t psgd_expert_sort_workspace_bytes(int64_t tokens, int64_t slots, int64_t experts);
+int psgd_expert_sort(void *workspace, void *stream, int64_t tokens, int64_t slots, int64_t experts, const int64_t *choice,
+                     int32_t *place, int32_t *order, int32_t *offsets);
+/* Xs[place[t, s]] = X[t].  X: tokens x cols; Xs: tokens * slots rows, of which those behind the last are left as they were.
+ * (The gradient of X is psgd_expert_combine of Xs' with weight = NULL.)  Places outside [0, tokens * slots) count for none, here and below;
+ * apart from that they are all different.  Errors, here and below: INVALID_ARG (null pointer, bad enum, an overlap), SHAPE (cols at most 2^22), ALIGN, HIP. */
+int psgd_expert_rows(void *stream, int64_t tokens, int64_t slots, int64_t cols, int dtype, const void *x, int64_t ld_x,
+                     const int32_t *place, void *xs, int64_t ld_xs);
+/* Y[t] = sum_s weight[t, s] Ys[place[t, s]] (weight: tokens x slots fp32, or NULL: 1), summed in fp32 in the order of s; a token without a row gets zeros. */
+int psgd_expert_combine(void *stream, int64_t tokens, int64_t slots, int64_t cols, int dtype, const void *ys, int64_t ld_ys,
+                        const int32_t *place, const float *weight /* nullable */, void *y, int64_t ld_y);
+/* Its gradients: dYs[place[t, s]] = weight[t, s] dY[t], rows behind the last left as they were; dweight[t, s] = dY[t] . Ys[place[t, s]]
+ * in fp32, 0 where there is no row.  dweight may be NULL, and then Ys.  dYs may take the place of Ys. */
+int psgd_expert_combine_backward(void *stream, int64_t tokens, int64_t slots, int64_t cols, int dtype, const void *dy, int64_t ld_dy,
+                                 const void *ys /* nullable */, int64_t ld_ys, const int32_t *place,
+                                 const float *weight /* nullable */, void *dys, int64_t ld_dys, float *dweight /* nullable */);
 
 int psgd_last_hip_error(const psgd_ctx *ctx);
 const char *psgd_strerror(int code);

@@ -21,21 +21,12 @@ constexpr int kActItems = 2;        // pieces per thread, all of whose loads are
 // From this many bytes of activations in a call on they are loaded and stored with the non-temporal hint (16384 x 11008 in bf16 and back 200 -> 180 us,
 // gated unit of 8192 x 11008 forward and backward 260 -> 228); what is smaller, the next kernel may find in the caches.  Codes never have it (188, 240).
 constexpr int64_t kActStream = 96 << 20;
-template <bool STREAM, class V> __device__ __forceinline__ V ld_act(const PSGD_GLOBAL V* p) {
-    if constexpr (STREAM) return __builtin_nontemporal_load(p); else return *p;
-}
-template <bool STREAM, class V> __device__ __forceinline__ void st_act(PSGD_GLOBAL V* p, V v) {
-    if constexpr (STREAM) __builtin_nontemporal_store(v, p); else *p = v;
-}
-
-template <class T> constexpr int kPiece = 16 / (int)sizeof(T);      // columns of a piece
 constexpr unsigned kInfBits = 0x7f800000u;
 constexpr unsigned kTopBits = 0x7f7e0000u;      // 127 * 2^121, the largest number that the largest scale holds
 constexpr float kWhole = 12582912.f;            // 1.5 * 2^23
 
 // piece i of this thread: row and first column.  `per`: pieces of a row, of whole groups; inv_per its reciprocal.
 struct ActRows { int64_t rows; int cols, per; double inv_per; };
-struct ActPlace { int64_t row; int col; bool in; };
 template <int N>
 __device__ __forceinline__ ActPlace act_place(const ActRows& r, int i) {
     const int64_t first = ((int64_t)blockIdx.x * kActItems + i) * kThreads;
@@ -55,49 +46,6 @@ __device__ __forceinline__ ActPlace act_place(const ActRows& r, int i) {
     p.col = N * (int)at;
     p.in = p.row < r.rows && p.col < r.cols;
     return p;
-}
-
-// A piece as it is stored; zeros beyond cols.  A piece that begins inside the row is read as a whole.
-template <bool STREAM, class T>
-__device__ __forceinline__ uintx4 load_raw(const T* x, int64_t ld, const ActPlace& p) {
-    uintx4 w = {0u, 0u, 0u, 0u};
-    if (p.in) w = ld_act<STREAM>(reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global(x) + p.row * ld + p.col));
-    return w;
-}
-template <class T>
-__device__ __forceinline__ void clear_beyond(uintx4& w, const ActPlace& p, int cols) {
-    if (p.col + kPiece<T> > cols) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if constexpr (sizeof(T) == 4) w[u] = p.col + u < cols ? w[u] : 0u;
-            else w[u] &= (p.col + 2 * u < cols ? 0xffffu : 0u) | (p.col + 2 * u + 1 < cols ? 0xffff0000u : 0u);
-        }
-    }
-}
-template <class T, int N = kPiece<T>>
-__device__ __forceinline__ void widen(const uintx4& w, float (&v)[N]) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        if constexpr (N == 4) v[u] = __uint_as_float(w[u]);
-        else { v[2 * u] = __uint_as_float(w[u] << 16); v[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
-    }
-}
-// nothing beyond cols is written
-template <bool STREAM, class T, int N = kPiece<T>>
-__device__ __forceinline__ void store_piece(T* x, int64_t ld, const ActPlace& p, int cols, const float (&v)[N]) {
-    if (!p.in) return;
-    PSGD_GLOBAL T* at = as_global(x) + p.row * ld + p.col;
-    if (p.col + N <= cols) {
-        typedef __attribute__((__vector_size__(16))) T piece;
-        piece q;
-#pragma unroll
-        for (int u = 0; u < N; ++u) q[u] = (T)v[u];
-        st_act<STREAM>(reinterpret_cast<PSGD_GLOBAL uintx4*>(at), __builtin_bit_cast(uintx4, q));
-    } else {
-#pragma unroll
-        for (int u = 0; u < N; ++u)
-            if (p.col + u < cols) at[u] = (T)v[u];
-    }
 }
 
 // the largest magnitude of a group as fp32 bits, what is not finite included (all lanes of the group come here)

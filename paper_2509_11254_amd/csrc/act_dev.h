@@ -1,8 +1,61 @@
-// Values of 8-bit checkpoints (act.hip) in kernels that read them.
+// Activations in kernels that read and write them piece by piece (act.hip, norm.hip), and the values of 8-bit checkpoints.
 #pragma once
 #include "psgd_dev.h"
 
 namespace psgd {
+
+// An activation is loaded and stored 16 bytes at a time, with the non-temporal hint or without.
+template <bool STREAM, class V> __device__ __forceinline__ V ld_act(const PSGD_GLOBAL V* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p); else return *p;
+}
+template <bool STREAM, class V> __device__ __forceinline__ void st_act(PSGD_GLOBAL V* p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p); else *p = v;
+}
+template <class T> constexpr int kPiece = 16 / (int)sizeof(T);      // columns of a piece
+struct ActPlace { int64_t row; int col; bool in; };
+
+// A piece as it is stored; zeros beyond cols.  A piece that begins inside the row is read as a whole.
+template <bool STREAM, class T>
+__device__ __forceinline__ uintx4 load_raw(const T* x, int64_t ld, const ActPlace& p) {
+    uintx4 w = {0u, 0u, 0u, 0u};
+    if (p.in) w = ld_act<STREAM>(reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global(x) + p.row * ld + p.col));
+    return w;
+}
+template <class T>
+__device__ __forceinline__ void clear_beyond(uintx4& w, const ActPlace& p, int cols) {
+    if (p.col + kPiece<T> > cols) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if constexpr (sizeof(T) == 4) w[u] = p.col + u < cols ? w[u] : 0u;
+            else w[u] &= (p.col + 2 * u < cols ? 0xffffu : 0u) | (p.col + 2 * u + 1 < cols ? 0xffff0000u : 0u);
+        }
+    }
+}
+template <class T, int N = kPiece<T>>
+__device__ __forceinline__ void widen(const uintx4& w, float (&v)[N]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if constexpr (N == 4) v[u] = __uint_as_float(w[u]);
+        else { v[2 * u] = __uint_as_float(w[u] << 16); v[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
+    }
+}
+// nothing beyond cols is written
+template <bool STREAM, class T, int N = kPiece<T>>
+__device__ __forceinline__ void store_piece(T* x, int64_t ld, const ActPlace& p, int cols, const float (&v)[N]) {
+    if (!p.in) return;
+    PSGD_GLOBAL T* at = as_global(x) + p.row * ld + p.col;
+    if (p.col + N <= cols) {
+        typedef __attribute__((__vector_size__(16))) T piece;
+        piece q;
+#pragma unroll
+        for (int u = 0; u < N; ++u) q[u] = (T)v[u];
+        st_act<STREAM>(reinterpret_cast<PSGD_GLOBAL uintx4*>(at), __builtin_bit_cast(uintx4, q));
+    } else {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            if (p.col + u < cols) at[u] = (T)v[u];
+    }
+}
 
 // four codes to a word, and their group's scale
 template <int W> struct ActCodes { unsigned w[W]; float scale; };

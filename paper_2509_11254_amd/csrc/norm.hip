@@ -1,0 +1,450 @@
+// Layer normalisation and its gradients.
+//
+//   s = x, or x + add rounded to the type it is kept in;  mean = sum_c s / n,  var = sum_c (s - mean)^2 / n,  r = 1 / sqrt(var + eps)
+//   u = (s - mean) r,  y = u w + b
+//   g = dy w,  ds = r (g - sum_c g / n - u sum_c(g u) / n) (+ the gradient that comes past the norm),  dw = sum_rows dy u,  db = sum_rows dy
+//
+// A row is in the registers of one wavefront, of four or of sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
+// first mean is subtracted, and corrected by what is left of the mean in that: a row far from zero loses nothing to it.
+//
+// Backward, a workgroup goes through rows that are the grid apart and keeps its columns' sums of dy u and dy in registers, in fp32; it
+// writes them once at its end, and a second launch adds up the workgroups' sums in their order.
+#include "act_dev.h"
+#include "train.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace psgd {
+
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr int64_t kNormMaxCols = 16384;
+
+struct NormParam { const void* ptr; int dtype; };
+struct NormDev {
+    int64_t rows;
+    int cols;
+    float eps;
+    const void *x, *add;
+    int64_t ld_in;
+    void *total, *y;
+    int64_t ld_out;
+    NormParam w, b;
+    floatx2* stats;
+};
+struct NormGradDev {
+    int64_t rows;
+    int cols;
+    const void *dy, *x, *past;      // past: the gradient that comes past the norm
+    int64_t ld_dy, ld_x, ld_dx;
+    void* dx;
+    NormParam w;
+    const floatx2* stats;
+    float* part;                    // nullable; [workgroup][2][ldp]: sums of dy u and of dy
+    int64_t ldp;
+};
+
+// N columns of a vector that ends at `cols`; `otherwise` where there is no vector, zeros beyond cols
+template <int N>
+__device__ __forceinline__ void load_param(const NormParam& p, int col, int cols, float otherwise, float (&v)[N]) {
+    if (!p.ptr) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] = col + u < cols ? otherwise : 0.f;
+    } else if (p.dtype == PSGD_F32) {
+        const PSGD_GLOBAL float* at = as_global(static_cast<const float*>(p.ptr)) + col;
+        if (col + N <= cols) {
+#pragma unroll
+            for (int u = 0; u < N; u += 4) {
+                const floatx4 q = *reinterpret_cast<const PSGD_GLOBAL floatx4*>(at + u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[u + k] = q[k];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[u] = col + u < cols ? at[u] : 0.f;
+        }
+    } else {
+        const PSGD_GLOBAL bf16_t* at = as_global(static_cast<const bf16_t*>(p.ptr)) + col;
+        if (col + N <= cols) {
+#pragma unroll
+            for (int u = 0; u < N; u += 4) {
+                const bf16x4 q = *reinterpret_cast<const PSGD_GLOBAL bf16x4*>(at + u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[u + k] = (float)q[k];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[u] = col + u < cols ? (float)at[u] : 0.f;
+        }
+    }
+}
+
+// Threads of a workgroup: WAVES to a row, and where that is one, four rows at a time.
+template <int WAVES> constexpr int kNormThreads = WAVES == 16 ? 1024 : 256;
+template <int WAVES> constexpr int kNormRows = WAVES == 1 ? 4 : 1;
+
+// sums over a row's lanes; `shared`: two sets of [K][WAVES], used in turn, so that one barrier is enough
+template <int WAVES, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float* shared, int& turn) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) v[k] += __shfl_xor(v[k], d);
+    if constexpr (WAVES > 1) {
+        float* to = shared + turn * 2 * WAVES;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) to[k * WAVES + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = to[k * WAVES];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[k] += to[k * WAVES + w];
+        }
+    }
+}
+
+// A rounded product: fused into the subtraction in one place and not in another, the mean would not be the same for all columns.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+template <class T, int WAVES, int PIECES, bool ADD, bool STREAM>
+__global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
+    constexpr int N = kPiece<T>;
+    __shared__ float shared[4 * WAVES];
+    int turn = 0;
+    const int at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, group = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const float inv_n = 1.f / (float)a.cols;
+    float w[PIECES][N], b[PIECES][N];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int col = N * (at + 64 * WAVES * i);
+        load_param<N>(a.w, col, a.cols, 1.f, w[i]);
+        load_param<N>(a.b, col, a.cols, 0.f, b[i]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group; row < a.rows; row += (int64_t)gridDim.x * kNormRows<WAVES>) {
+        uintx4 raw[PIECES], raw_add[PIECES];
+        ActPlace p[PIECES];
+        float v[PIECES][N];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
+            raw[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_in, p[i]);
+            if constexpr (ADD) raw_add[i] = load_raw<STREAM>(static_cast<const T*>(a.add), a.ld_in, p[i]);
+        }
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            clear_beyond<T>(raw[i], p[i], a.cols);
+            widen<T>(raw[i], v[i]);
+            if constexpr (ADD) {
+                float o[N];
+                clear_beyond<T>(raw_add[i], p[i], a.cols);
+                widen<T>(raw_add[i], o);
+#pragma unroll
+                for (int u = 0; u < N; ++u) v[i][u] = (float)(T)(v[i][u] + o[u]);       // (what is normalised is what is kept)
+                store_piece<STREAM>(static_cast<T*>(a.total), a.ld_out, p[i], a.cols, v[i]);
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) sum[0] += v[i][u];
+        }
+        row_sums<WAVES>(sum, shared, turn);
+        const float first = rounded_product(sum[0], inv_n);
+        float rest[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[i][u] -= first;
+            if (p[i].col + N > a.cols)
+#pragma unroll
+                for (int u = 0; u < N; ++u) v[i][u] = p[i].col + u < a.cols ? v[i][u] : 0.f;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                rest[0] += v[i][u];
+                rest[1] = fmaf(v[i][u], v[i][u], rest[1]);
+            }
+        }
+        row_sums<WAVES>(rest, shared, turn);
+        const float more = rounded_product(rest[0], inv_n);
+        float var = fmaf(rest[1], inv_n, -more * more);
+        var = var < 0.f ? 0.f : var;
+        const float r = 1.f / sqrtf(var + a.eps);
+        if (a.stats && at == 0) as_global(a.stats)[row] = floatx2{first + more, r};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) v[i][u] = fmaf((v[i][u] - more) * r, w[i][u], b[i][u]);
+            store_piece<STREAM>(static_cast<T*>(a.y), a.ld_out, p[i], a.cols, v[i]);
+        }
+    }
+}
+
+template <class T, int WAVES, int PIECES, bool PAST, bool STREAM>
+__global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(NormGradDev a) {
+    constexpr int N = kPiece<T>;
+    __shared__ float shared[4 * WAVES];
+    int turn = 0;
+    const int at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, group = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const float inv_n = 1.f / (float)a.cols;
+    float w[PIECES][N], dw[PIECES][N], db[PIECES][N];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        load_param<N>(a.w, N * (at + 64 * WAVES * i), a.cols, 1.f, w[i]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) dw[i][u] = db[i][u] = 0.f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group; row < a.rows; row += (int64_t)gridDim.x * kNormRows<WAVES>) {
+        uintx4 raw_x[PIECES], raw_dy[PIECES], raw_past[PIECES];
+        ActPlace p[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
+            raw_x[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_x, p[i]);
+            raw_dy[i] = load_raw<STREAM>(static_cast<const T*>(a.dy), a.ld_dy, p[i]);
+            if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_dx, p[i]);
+        }
+        const floatx2 st = as_global(a.stats)[row];
+        float u[PIECES][N], g[PIECES][N], sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            clear_beyond<T>(raw_x[i], p[i], a.cols);
+            clear_beyond<T>(raw_dy[i], p[i], a.cols);
+            widen<T>(raw_x[i], u[i]);
+            widen<T>(raw_dy[i], g[i]);
+            // (beyond the columns g is 0; u is not, but finite where the row's are)
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                u[i][k] = (u[i][k] - st.x) * st.y;
+                dw[i][k] = fmaf(g[i][k], u[i][k], dw[i][k]);
+                db[i][k] += g[i][k];
+                g[i][k] *= w[i][k];
+                sums[0] += g[i][k];
+                sums[1] = fmaf(g[i][k], u[i][k], sums[1]);
+            }
+        }
+        row_sums<WAVES>(sums, shared, turn);
+        const float c1 = sums[0] * inv_n, c2 = sums[1] * inv_n;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            float o[N];
+            if constexpr (PAST) widen<T>(raw_past[i], o);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float d = st.y * (g[i][k] - fmaf(u[i][k], c2, c1));
+                g[i][k] = PAST ? o[k] + d : d;
+            }
+            store_piece<STREAM>(static_cast<T*>(a.dx), a.ld_dx, p[i], a.cols, g[i]);
+        }
+    }
+    if (!a.part) return;
+    constexpr int SPAN = 64 * WAVES * PIECES * N;
+    if constexpr (WAVES == 1) {         // the four rows' sums, in their order
+        __shared__ float joined[2 * SPAN];
+        for (int from = 0; from < 4; ++from) {
+            if (group == from)
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const int c = N * (at + 64 * i) + k;
+                        joined[c] = from ? joined[c] + dw[i][k] : dw[i][k];
+                        joined[SPAN + c] = from ? joined[SPAN + c] + db[i][k] : db[i][k];
+                    }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < a.cols; c += 256) {
+            as_global(a.part)[(int64_t)blockIdx.x * 2 * a.ldp + c] = joined[c];
+            as_global(a.part)[((int64_t)blockIdx.x * 2 + 1) * a.ldp + c] = joined[SPAN + c];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                const int c = N * (at + 64 * WAVES * i) + k;
+                if (c >= a.cols) break;         // (the rows of `part` are a multiple of 8 long)
+                PSGD_GLOBAL float* to = as_global(a.part) + (int64_t)blockIdx.x * 2 * a.ldp + c;
+                *reinterpret_cast<PSGD_GLOBAL floatx4*>(to) = floatx4{dw[i][k], dw[i][k + 1], dw[i][k + 2], dw[i][k + 3]};
+                *reinterpret_cast<PSGD_GLOBAL floatx4*>(to + a.ldp) = floatx4{db[i][k], db[i][k + 1], db[i][k + 2], db[i][k + 3]};
+            }
+    }
+}
+
+// sums of the workgroups' sums: 64 columns to a block, 16 threads to a column; blockIdx.y: the weight's or the bias's
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int64_t ldp, int n_parts, int cols, void* dw, void* db, int dtype, int accumulate) {
+    __shared__ float shared[16][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    void* out = blockIdx.y ? db : dw;
+    if (!out) return;
+    float s = 0.f;
+    if (c < cols) {
+#pragma unroll 4
+        for (int i = slice; i < n_parts; i += 16) s += as_global(part)[((int64_t)i * 2 + blockIdx.y) * ldp + c];
+    }
+    shared[slice][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (slice == 0 && c < cols) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += shared[i][threadIdx.x];
+        if (dtype == PSGD_F32) {
+            PSGD_GLOBAL float* to = as_global(static_cast<float*>(out)) + c;
+            *to = accumulate ? *to + s : s;
+        } else {
+            PSGD_GLOBAL bf16_t* to = as_global(static_cast<bf16_t*>(out)) + c;
+            *to = (bf16_t)(accumulate ? (float)*to + s : s);
+        }
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------
+
+// wavefronts to a row and pieces to a lane: as few of the former as have the row in four pieces each (in two of several wavefronts)
+struct NormShape { int waves, pieces; };
+static NormShape norm_variant(int64_t cols, int dtype) {
+    const int64_t n = (cols + (dtype == PSGD_F32 ? 3 : 7)) / (dtype == PSGD_F32 ? 4 : 8);
+    if (n <= 64) return {1, 1};
+    if (n <= 128) return {1, 2};
+    if (n <= 256) return {1, 4};
+    if (n <= 512) return {4, 2};
+    if (n <= 1024) return {4, 4};
+    return {16, n <= 2048 ? 2 : 4};
+}
+constexpr int kNormBlocks = 2048;           // forward
+constexpr int kNormGradBlocks = 1024;       // backward: each has its sums written and read
+static int norm_blocks(int64_t rows, const NormShape& v, int most) {
+    const int per = v.waves == 1 ? 4 : 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, v.waves == 16 ? most / 4 : most));
+}
+// From this many bytes in a call on activations have the non-temporal hint (as those of act.hip).
+constexpr int64_t kNormStream = 96 << 20;
+
+static int norm_shape(int64_t rows, int64_t cols) {
+    return rows < 0 || cols < 1 || rows > kMaxExtent || cols > kNormMaxCols ? PSGD_E_SHAPE : PSGD_OK;
+}
+// an output may take the place of an input of the same layout
+static bool bad_place(const RowArea& out, const RowArea& in) {
+    return overlap(out, in) && !(out.ptr == in.ptr && (out.stride == in.stride || out.rows == 1) && out.width == in.width);
+}
+
+// launch(waves, pieces) with constants
+template <class T, class F>
+static hipError_t norm_dispatch(const NormShape& v, F launch) {
+    if (v.waves == 1) return v.pieces == 1 ? launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
+                           : v.pieces == 2 ? launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{})
+                                           : launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+    if (v.waves == 4) return v.pieces == 2 ? launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{})
+                                           : launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+    if constexpr (sizeof(T) == 4)
+        if (v.pieces == 4) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+    return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+}
+
+template <class T, bool ADD, bool STREAM>
+static hipError_t launch_norm_as(const NormDev& a, const NormShape& v, hipStream_t st) {
+    const int blocks = norm_blocks(a.rows, v, kNormBlocks);
+    return norm_dispatch<T>(v, [&](auto waves, auto pieces) {
+        hipLaunchKernelGGL((norm_kernel<T, waves.value, pieces.value, ADD, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
+        return hipGetLastError();
+    });
+}
+template <class T, bool PAST, bool STREAM>
+static hipError_t launch_backward_as(const NormGradDev& a, const NormShape& v, int blocks, hipStream_t st) {
+    return norm_dispatch<T>(v, [&](auto waves, auto pieces) {
+        hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, PAST, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace psgd
+
+using namespace psgd;
+
+extern "C" {
+
+int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x, const void* add, int64_t ld_in, const void* weight, const void* bias,
+              int w_dtype, float eps, void* total, void* y, int64_t ld_out, float* stats) {
+    if (bad_dtype(dtype) || bad_dtype(w_dtype) || !(eps >= 0.f && eps < __builtin_inff())) return PSGD_E_INVALID_ARG;
+    if (rows != 0 && (!x || !y || (add == nullptr) != (total == nullptr))) return PSGD_E_INVALID_ARG;
+    if (int rc = norm_shape(rows, cols)) return rc;
+    if (bad_ld(ld_in, cols) || bad_ld(ld_out, cols) || misaligned(x) || misaligned(add) || misaligned(weight) || misaligned(bias) || misaligned(total) ||
+        misaligned(y) || misaligned(stats)) return PSGD_E_ALIGN;
+    if (ld_in > kMaxLd || ld_out > kMaxLd) return PSGD_E_SHAPE;
+    if (rows == 0) return PSGD_OK;
+    const int64_t size = dtype == PSGD_F32 ? 4 : 2, w_size = w_dtype == PSGD_F32 ? 4 : 2;
+    const RowArea in[] = {{x, rows, ld_in * size, cols * size}, {add, rows, ld_in * size, cols * size}};
+    const RowArea params[] = {{weight, 1, 0, cols * w_size}, {bias, 1, 0, cols * w_size}};
+    const RowArea out[] = {{total, rows, ld_out * size, cols * size}, {y, rows, ld_out * size, cols * size}, {stats, 1, 0, rows * 8}};
+    for (int i = 0; i < 3; ++i) {
+        for (const RowArea& a : in)
+            if (i == 2 ? overlap(out[i], a) : bad_place(out[i], a)) return PSGD_E_INVALID_ARG;
+        for (const RowArea& a : params)
+            if (overlap(out[i], a)) return PSGD_E_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return PSGD_E_INVALID_ARG;
+    }
+    const NormDev a = {rows, (int)cols, eps, x, add, ld_in, total, y, ld_out, {weight, w_dtype}, {bias, w_dtype}, reinterpret_cast<floatx2*>(stats)};
+    const NormShape v = norm_variant(cols, dtype);
+    const bool stream_it = rows * cols * size * (add ? 4 : 2) >= kNormStream;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
+    hipError_t e;
+#define PSGD_NORM(T, ADD) (stream_it ? launch_norm_as<T, ADD, true>(a, v, st) : launch_norm_as<T, ADD, false>(a, v, st))
+    if (dtype == PSGD_F32) e = add ? PSGD_NORM(float, true) : PSGD_NORM(float, false);
+    else e = add ? PSGD_NORM(bf16_t, true) : PSGD_NORM(bf16_t, false);
+#undef PSGD_NORM
+    return e == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+}
+
+size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype) {
+    if (bad_dtype(dtype) || norm_shape(rows, cols)) return 0;
+    return up256((size_t)norm_blocks(rows, norm_variant(cols, dtype), kNormGradBlocks) * 2 * up8(cols) * sizeof(float));
+}
+
+int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols, int dtype, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                       const void* weight, int w_dtype, const float* stats, const void* dtotal, void* dx, int64_t ld_dx, void* dweight, void* dbias,
+                       int g_dtype, int accumulate) {
+    const bool sums = dweight || dbias;
+    if (bad_dtype(dtype) || bad_dtype(w_dtype) || bad_dtype(g_dtype) || (sums && !workspace)) return PSGD_E_INVALID_ARG;
+    if (rows != 0 && (!dy || !x || !stats || !dx)) return PSGD_E_INVALID_ARG;
+    if (int rc = norm_shape(rows, cols)) return rc;
+    if (bad_ld(ld_dy, cols) || bad_ld(ld_x, cols) || bad_ld(ld_dx, cols) || misaligned(dy) || misaligned(x) || misaligned(weight) || misaligned(stats) ||
+        misaligned(dtotal) || misaligned(dx) || misaligned(dweight) || misaligned(dbias) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
+    if (ld_dy > kMaxLd || ld_x > kMaxLd || ld_dx > kMaxLd) return PSGD_E_SHAPE;
+    const int64_t size = dtype == PSGD_F32 ? 4 : 2, w_size = w_dtype == PSGD_F32 ? 4 : 2, g_size = g_dtype == PSGD_F32 ? 4 : 2;
+    const RowArea in[] = {{dy, rows, ld_dy * size, cols * size}, {x, rows, ld_x * size, cols * size}, {dtotal, rows, ld_dx * size, cols * size},
+                          {weight, 1, 0, cols * w_size}, {stats, 1, 0, rows * 8}};
+    const RowArea out[] = {{dx, rows, ld_dx * size, cols * size}, {dweight, 1, 0, cols * g_size}, {dbias, 1, 0, cols * g_size}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 5; ++j)
+            if (i == 0 && j < 3 ? bad_place(out[i], in[j]) : overlap(out[i], in[j])) return PSGD_E_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return PSGD_E_INVALID_ARG;
+    }
+    if (rows == 0 && (!sums || accumulate)) return PSGD_OK;
+    NormGradDev a = {rows, (int)cols, dy, x, dtotal, ld_dy, ld_x, ld_dx, dx, {weight, w_dtype}, reinterpret_cast<const floatx2*>(stats),
+                     sums ? static_cast<float*>(workspace) : nullptr, up8(cols)};
+    const NormShape v = norm_variant(cols, dtype);
+    const int blocks = norm_blocks(rows, v, kNormGradBlocks);
+    const bool stream_it = rows * cols * size * (dtotal ? 4 : 3) >= kNormStream;
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    forget_errors();
+    if (rows != 0) {
+        hipError_t e;
+#define PSGD_NORM(T, PAST) (stream_it ? launch_backward_as<T, PAST, true>(a, v, blocks, st) : launch_backward_as<T, PAST, false>(a, v, blocks, st))
+        if (dtype == PSGD_F32) e = dtotal ? PSGD_NORM(float, true) : PSGD_NORM(float, false);
+        else e = dtotal ? PSGD_NORM(bf16_t, true) : PSGD_NORM(bf16_t, false);
+#undef PSGD_NORM
+        if (e != hipSuccess) return PSGD_E_HIP;
+    }
+    if (!sums) return PSGD_OK;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 63) / 64), 2), dim3(1024), 0, st, a.part, a.ldp, rows ? blocks : 0, (int)cols, dweight, dbias,
+                       g_dtype, accumulate != 0);
+    return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+}
+
+}  // extern "C"

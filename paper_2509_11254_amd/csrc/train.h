@@ -99,4 +99,20 @@ inline bool bad_ld(int64_t ld, int64_t cols) { return ld < cols || (ld & 7) != 0
 constexpr int64_t kMaxLd = 1 << 22;     // 255 rows * ld * 2 bytes stay within a buffer descriptor's range
 constexpr int64_t kMaxExtent = 1 << 30;
 
+// rows of `width` bytes, `stride` bytes apart
+struct RowArea { const void* ptr; int64_t rows, stride, width; };
+// (columns of one buffer beside each other do not overlap; areas with different strides do where their ranges do)
+inline bool overlap(RowArea a, RowArea b) {
+    if (a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0 || !a.ptr || !b.ptr) return false;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.ptr) - reinterpret_cast<uintptr_t>(a.ptr));
+    if (apart >= (a.rows - 1) * a.stride + a.width || -apart >= (b.rows - 1) * b.stride + b.width) return false;
+    if (a.rows == 1) a.stride = b.stride;
+    if (b.rows == 1) b.stride = a.stride;
+    if (a.stride != b.stride || a.width > a.stride || b.width > b.stride) return true;
+    // b's first row begins in row `down` of a, at column `right`
+    const int64_t down = apart >= 0 ? apart / a.stride : -((-apart + a.stride - 1) / a.stride), right = apart - down * a.stride;
+    auto rows_meet = [&](int64_t d) { return d < a.rows && d + b.rows > 0; };
+    return (right < a.width && rows_meet(down)) || (right + b.width > a.stride && rows_meet(down + 1));
+}
+
 }  // namespace psgd

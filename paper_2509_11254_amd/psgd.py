@@ -26,6 +26,8 @@ EXPORTS = [
     "psgd_strerror", "psgd_destroy", "psgd_profile_enable", "psgd_profile_select", "psgd_profile_read",
     "psgd_head_workspace_bytes", "psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore",
     "psgd_act_glu", "psgd_act_glu_backward", "psgd_act_wgrad_workspace_bytes", "psgd_act_wgrad",
+    "psgd_norm", "psgd_norm_backward_workspace_bytes", "psgd_norm_backward", "psgd_expert_sort_workspace_bytes", "psgd_expert_sort",
+    "psgd_expert_rows", "psgd_expert_combine", "psgd_expert_combine_backward",
 ]
 PSGD_SILU, PSGD_GELU = 0, 1
 ACT_GROUP = 32      # columns of an activation that share a scale
@@ -134,8 +136,19 @@ def load_library() -> C.CDLL:
     lib.psgd_act_wgrad_workspace_bytes.argtypes = [l, l, l, i]
     lib.psgd_act_wgrad_workspace_bytes.restype = C.c_size_t
     lib.psgd_act_wgrad.argtypes = [vp, vp, l, l, l, vp, i, l, vp, l, vp, vp, i, l, i]
+    lib.psgd_norm.argtypes = [vp, l, l, i, vp, vp, l, vp, vp, i, C.c_float, vp, vp, l, vp]
+    lib.psgd_norm_backward_workspace_bytes.argtypes = [l, l, i]
+    lib.psgd_norm_backward_workspace_bytes.restype = C.c_size_t
+    lib.psgd_norm_backward.argtypes = [vp, vp, l, l, i, vp, l, vp, l, vp, i, vp, vp, vp, l, vp, vp, i, i]
+    lib.psgd_expert_sort_workspace_bytes.argtypes = [l, l, l]
+    lib.psgd_expert_sort_workspace_bytes.restype = C.c_size_t
+    lib.psgd_expert_sort.argtypes = [vp, vp, l, l, l, vp, vp, vp, vp]
+    lib.psgd_expert_rows.argtypes = [vp, l, l, l, i, vp, l, vp, vp, l]
+    lib.psgd_expert_combine.argtypes = [vp, l, l, l, i, vp, l, vp, vp, vp, l]
+    lib.psgd_expert_combine_backward.argtypes = [vp, l, l, l, i, vp, l, vp, l, vp, vp, vp, l, vp]
     for name in ("psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore", "psgd_act_glu",
-                 "psgd_act_glu_backward", "psgd_act_wgrad"):
+                 "psgd_act_glu_backward", "psgd_act_wgrad", "psgd_norm", "psgd_norm_backward", "psgd_expert_sort",
+                 "psgd_expert_rows", "psgd_expert_combine", "psgd_expert_combine_backward"):
         getattr(lib, name).restype = C.c_int
     lib.psgd_destroy.argtypes = [vp]
     lib.psgd_destroy.restype = None
@@ -523,3 +536,165 @@ class WeightGrad:
         _check(self.lib, None, self.lib.psgd_act_wgrad(
             self._ws_ptr, _stream_for(stream, self.workspace, dY, G, kept.codes, kept.scales), tokens, out_features, in_features, dY.data_ptr(), self.dtype, ldy,
             kept.codes.data_ptr(), kept.ldc, kept.scales.data_ptr(), G.data_ptr(), self.grad_dtype, ldg, 1 if accumulate else 0))
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def norm(X, weight, bias, Y, stats=None, eps: float = 1e-5, add=None, total=None, stream=None) -> None:
+    """psgd_norm: Y <- layer norm of the rows of X, or with add of total <- X + add (rounded to the type), times weight plus bias
+    (one type; None: 1 and 0).  stats (rows x 2, float32): what NormGrad needs.  total or Y may be X or add itself."""
+    import torch
+    lib = load_library()
+    _same("presence of add and of total", add is None, total is None)
+    rows, cols, dt = int(X.shape[0]), int(X.shape[1]), _dtype_code(X)
+    ld_in, ld_out = _matrix("X", X, rows, cols), _matrix("Y", Y, rows, cols, dt)
+    if add is not None:
+        _same("leading dimensions of X and add", ld_in, _matrix("add", add, rows, cols, dt))
+        _same("leading dimensions of Y and total", ld_out, _matrix("total", total, rows, cols, dt))
+    if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or not stats.is_contiguous() or not stats.is_cuda):
+        raise ValueError("stats: a contiguous %d x 2 float32 matrix on the GPU expected" % rows)
+    w_dt = _params(cols, weight=weight, bias=bias)
+    _check(lib, None, lib.psgd_norm(_stream_for(stream, X, weight, bias, Y, stats, add, total), rows, cols, dt, X.data_ptr(), _ptr(add), ld_in,
+                                    _ptr(weight), _ptr(bias), w_dt, float(eps), _ptr(total), Y.data_ptr(), ld_out, _ptr(stats)))
+
+
+def _params(cols: int, **vectors) -> int:
+    """Checks vectors of one type, each of which may be None; their type."""
+    code = None
+    for name, t in vectors.items():
+        if t is None:
+            continue
+        if code is not None and _dtype_code(t) != code:
+            raise ValueError("%s: wrong element type %s" % (name, t.dtype))
+        code = _dtype_code(t)
+        _vector(name, t, cols, t.dtype)
+    return PSGD_F32 if code is None else code
+
+
+class NormGrad:
+    """psgd_norm_backward with a torch-allocated workspace, for one set of sizes and types.  Calls on streams that do not wait for
+    each other need an object each: they would share the workspace."""
+
+    def __init__(self, rows: int, cols: int, dtype: int = PSGD_BF16, w_dtype: Optional[int] = None, grad_dtype: Optional[int] = None, *,
+                 device: str = "cuda"):
+        self.lib = load_library()
+        self.shape, self.dtype = (int(rows), int(cols)), int(dtype)
+        self.w_dtype = int(dtype if w_dtype is None else w_dtype)
+        self.grad_dtype = int(self.w_dtype if grad_dtype is None else grad_dtype)
+        self.workspace_bytes = int(self.lib.psgd_norm_backward_workspace_bytes(*self.shape, self.dtype))
+        if self.workspace_bytes == 0 or self.w_dtype not in (PSGD_F32, PSGD_BF16) or self.grad_dtype not in (PSGD_F32, PSGD_BF16):
+            raise PsgdError(PSGD_E_INVALID_ARG, "sizes or types of the norm")
+        self.workspace, self._ws_ptr = _work_area(self.workspace_bytes, device)
+
+    def run(self, dY, X, weight, stats, dX, dweight=None, dbias=None, dtotal=None, accumulate: bool = False, stream=None) -> None:
+        """X: what was normalised (norm's total, where there was one); dtotal: the gradient that reaches it past the norm.
+        dX <- its gradient; dweight, dbias <- (accumulate: +=) theirs, each of which may be None.  dX may be dY, X or dtotal itself."""
+        import torch
+        rows, cols = self.shape
+        ld_dy, ld_x, ld_dx = (_matrix("dY", dY, rows, cols, self.dtype), _matrix("X", X, rows, cols, self.dtype),
+                              _matrix("dX", dX, rows, cols, self.dtype))
+        if dtotal is not None:
+            _same("leading dimensions of dX and dtotal", ld_dx, _matrix("dtotal", dtotal, rows, cols, self.dtype))
+        if stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or not stats.is_contiguous() or not stats.is_cuda:
+            raise ValueError("stats: a contiguous %d x 2 float32 matrix on the GPU expected" % rows)
+        if weight is not None:
+            _same("element types of weight", _params(cols, weight=weight), self.w_dtype)
+        if dweight is not None or dbias is not None:
+            _same("element types of dweight and dbias", _params(cols, dweight=dweight, dbias=dbias), self.grad_dtype)
+        _check(self.lib, None, self.lib.psgd_norm_backward(
+            self._ws_ptr, _stream_for(stream, self.workspace, dY, X, weight, stats, dX, dweight, dbias, dtotal), rows, cols, self.dtype, dY.data_ptr(),
+            ld_dy, X.data_ptr(), ld_x, _ptr(weight), self.w_dtype, stats.data_ptr(), _ptr(dtotal), dX.data_ptr(), ld_dx, _ptr(dweight), _ptr(dbias),
+            self.grad_dtype, 1 if accumulate else 0))
+
+
+class ExpertOrder:
+    """Tokens sorted by expert: place (tokens x slots int32: the row of each choice, -1 where it does not count), order (tokens * slots
+    int32: the choice of each row, -1 behind the last) and offsets (experts + 1 int32: each expert's first row, and their number)."""
+
+    def __init__(self, place, order, offsets):
+        import torch
+        if place.dim() != 2 or offsets.dim() != 1 or offsets.shape[0] < 2:
+            raise ValueError("place: tokens x slots, offsets: experts + 1 elements expected, got %s and %s" % (tuple(place.shape), tuple(offsets.shape)))
+        self.tokens, self.slots, self.experts = int(place.shape[0]), int(place.shape[1]), int(offsets.shape[0]) - 1
+        if place.dtype != torch.int32 or not place.is_contiguous() or not place.is_cuda:
+            raise ValueError("place: a contiguous int32 matrix on the GPU expected")
+        _vector("order", order, self.tokens * self.slots, torch.int32)
+        _vector("offsets", offsets, self.experts + 1, torch.int32)
+        self.place, self.order, self.offsets = place, order, offsets
+
+    def _tensors(self):
+        return (self.place, self.order, self.offsets)
+
+
+def expert_order_empty(tokens: int, slots: int, experts: int, device: str = "cuda") -> ExpertOrder:
+    """Buffers for the order of tokens that choose `slots` of `experts` each."""
+    import torch
+    return ExpertOrder(torch.empty((tokens, slots), dtype=torch.int32, device=device), torch.empty(tokens * slots, dtype=torch.int32, device=device),
+                       torch.empty(experts + 1, dtype=torch.int32, device=device))
+
+
+class ExpertSort:
+    """psgd_expert_sort with a torch-allocated workspace, for one set of sizes.  Calls on streams that do not wait for each other need an
+    object each: they would share the workspace."""
+
+    def __init__(self, tokens: int, slots: int, experts: int, *, device: str = "cuda"):
+        self.lib = load_library()
+        self.shape = (int(tokens), int(slots), int(experts))
+        self.workspace_bytes = int(self.lib.psgd_expert_sort_workspace_bytes(*self.shape))
+        if self.workspace_bytes == 0:
+            raise PsgdError(PSGD_E_INVALID_ARG, "sizes of the sort")
+        self.workspace, self._ws_ptr = _work_area(self.workspace_bytes, device)
+
+    def run(self, choice, order: ExpertOrder, stream=None) -> None:
+        """order <- the tokens sorted by choice (tokens x slots int64; outside [0, experts): the choice does not count)."""
+        import torch
+        _same("sizes of the order", (order.tokens, order.slots, order.experts), self.shape)
+        if choice.dtype != torch.int64 or tuple(choice.shape) != self.shape[:2] or not choice.is_contiguous() or not choice.is_cuda:
+            raise ValueError("choice: a contiguous %d x %d int64 matrix on the GPU expected" % self.shape[:2])
+        _check(self.lib, None, self.lib.psgd_expert_sort(
+            self._ws_ptr, _stream_for(stream, self.workspace, choice, *order._tensors()), *self.shape, choice.data_ptr(), order.place.data_ptr(),
+            order.order.data_ptr(), order.offsets.data_ptr()))
+
+
+def _choice_weights(name: str, t, order: ExpertOrder):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (order.tokens, order.slots) or not t.is_contiguous() or not t.is_cuda):
+        raise ValueError("%s: a contiguous %d x %d float32 matrix on the GPU expected" % (name, order.tokens, order.slots))
+
+
+def expert_rows(X, order: ExpertOrder, Xs, stream=None) -> None:
+    """psgd_expert_rows: row place[t, s] of Xs (tokens * slots rows) <- row t of X; rows behind the last stay as they are.
+    The gradient of X is expert_combine of the gradient of Xs."""
+    lib = load_library()
+    cols, dt = int(X.shape[1]), _dtype_code(X)
+    ld, ld_s = _matrix("X", X, order.tokens, cols), _matrix("Xs", Xs, order.tokens * order.slots, cols, dt)
+    _check(lib, None, lib.psgd_expert_rows(_stream_for(stream, X, Xs, *order._tensors()), order.tokens, order.slots, cols, dt, X.data_ptr(), ld,
+                                           order.place.data_ptr(), Xs.data_ptr(), ld_s))
+
+
+def expert_combine(Ys, order: ExpertOrder, Y, weight=None, stream=None) -> None:
+    """psgd_expert_combine: row t of Y <- the sum of its choices' rows of Ys times weight[t, s] (None: 1)."""
+    lib = load_library()
+    cols, dt = int(Y.shape[1]), _dtype_code(Y)
+    ld_s, ld = _matrix("Ys", Ys, order.tokens * order.slots, cols, dt), _matrix("Y", Y, order.tokens, cols)
+    _choice_weights("weight", weight, order)
+    _check(lib, None, lib.psgd_expert_combine(_stream_for(stream, Ys, Y, weight, *order._tensors()), order.tokens, order.slots, cols, dt, Ys.data_ptr(),
+                                              ld_s, order.place.data_ptr(), _ptr(weight), Y.data_ptr(), ld))
+
+
+def expert_combine_backward(dY, Ys, order: ExpertOrder, dYs, weight=None, dweight=None, stream=None) -> None:
+    """psgd_expert_combine_backward: row place[t, s] of dYs <- weight[t, s] times row t of dY, rows behind the last stay as they are;
+    dweight[t, s] <- dY[t] . Ys[place[t, s]], 0 where there is no row (dweight None: Ys may be None).  dYs may be Ys itself."""
+    lib = load_library()
+    cols, dt, rows = int(dY.shape[1]), _dtype_code(dY), order.tokens * order.slots
+    ld, ld_ds = _matrix("dY", dY, order.tokens, cols), _matrix("dYs", dYs, rows, cols, dt)
+    ld_s = _matrix("Ys", Ys, rows, cols, dt) if Ys is not None else 0
+    if dweight is not None and Ys is None:
+        raise ValueError("dweight needs Ys")
+    _choice_weights("weight", weight, order)
+    _choice_weights("dweight", dweight, order)
+    _check(lib, None, lib.psgd_expert_combine_backward(
+        _stream_for(stream, dY, Ys, dYs, weight, dweight, *order._tensors()), order.tokens, order.slots, cols, dt, dY.data_ptr(), ld, _ptr(Ys), ld_s,
+        order.place.data_ptr(), _ptr(weight), dYs.data_ptr(), ld_ds, _ptr(dweight)))
