@@ -334,6 +334,22 @@ int psgd_head_loss_grad(const psgd_head_desc *desc, void *workspace, void *strea
                         const int64_t *labels, const float *weight /* nullable */, float *loss, void *dx, void *dw,
                         int accumulate);
 
+/* The same head against a teacher whose `top` largest logits are known (distillation).  With l = X W^T / temperature:
+ *   p_tv = softmax_v(l_t);  q_t = softmax of teacher / temperature over the entries of token t that count, 0 for all other words;
+ *   loss_t = sum_v q_tv log(q_tv / p_tv);  D_tv = c_t (p_tv - q_tv) / temperature;  dX = D W;  dW = D^T X.
+ * index: tokens x top int64, teacher: tokens x top of teacher_dtype, entries of a token adjacent, tokens ld_top entries apart in both.
+ * An entry counts whose index lies in [0, vocab) and whose logit is not -infinity; what the others hold is not looked at.  The order of entries does not matter; a word that
+ * is named by several has their probabilities added up.  A token without entries that count does not count (as one whose label lies
+ * outside the vocabulary).  top: at most 1024.  Weights, pieces, types, overlaps, accumulation and errors as above; INVALID_ARG as well where
+ * temperature or one over it is not a positive number. */
+size_t psgd_head_distill_workspace_bytes(const psgd_head_desc *desc, int64_t top, int gradients);
+int psgd_head_distill(const psgd_head_desc *desc, void *workspace, void *stream, const void *x, const void *w, int64_t top,
+                      const int64_t *index, const void *teacher, int teacher_dtype, int64_t ld_top, float temperature,
+                      float *loss);
+int psgd_head_distill_grad(const psgd_head_desc *desc, void *workspace, void *stream, const void *x, const void *w, int64_t top,
+                           const int64_t *index, const void *teacher, int teacher_dtype, int64_t ld_top, float temperature,
+                           const float *weight /* nullable */, float *loss, void *dx, void *dw, int accumulate);
+
 /* 8-bit checkpoints of an activation (rows x cols).  A row is cut into groups of 32 columns; a group's scale is the smallest power of two
  * 2^e with max|x| <= 127 * 2^e (-126 <= e <= 121; kept as the byte e + 127, 0 for a group of zeros), an element's code is x / 2^e rounded to the nearest whole number, ties to even.  What is not
  * finite has code -128, does not enter the maximum and comes back as NaN.  Values that come back are exact in bf16.

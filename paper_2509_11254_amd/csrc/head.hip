@@ -28,14 +28,29 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 enum HeadKeep { KEEP_NONE = 0, KEEP_F16 = 1, KEEP_F32 = 2 };
 constexpr float kHalfScale = 32768.f;
 
+// A teacher's entries in the place of labels.  Per token of the piece a list of the words that its entries name, ascending, each once.
+struct HeadTop {
+    const int64_t* index;
+    const void* teacher;
+    int dtype, top;
+    int64_t ld;
+    // in the workspace
+    int* word;           // [token of the piece][top]
+    float *q, *log_q;    // the teacher's probability of the word
+    float* logit;        // its logit
+    unsigned short* start;      // [token of the piece][tiles + 1]: the first of the list that is in a tile, and at the end their number
+};
+
 struct HeadDev {
-    const int64_t* labels;
+    const int64_t* labels;      // (of a teacher: 0 where there is an entry, -1 where there is none)
+    HeadTop top;
+    float inv_t;         // one over the temperature, which logits are multiplied by
     const float* weight;
     float* loss;
     int tokens, d, vocab;
     // in the workspace
     int* count;          // tokens that count
-    float* scale;        // the largest c_t: D is kept relative to it and its products are multiplied by it
+    float* scale;        // the largest c_t (in the second word): D is kept relative to it, and its products are multiplied by it over the temperature (the first)
     int* rows;           // which they are
     int* label;          // and their labels
     uint64_t* counts;    // or, where X is taken as it is, a bit for every token
@@ -161,14 +176,161 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
 #pragma unroll
             for (int w = 0; w < kGatherThreads / 64; ++w) most = fmaxf(most, all[w]);
             *h.count = before;
-            *h.scale = !h.weight ? 1.f / (float)max(before, 1) : most > 0.f && most < __builtin_inff() ? most : 1.f;
+            const float scale = !h.weight ? 1.f / (float)max(before, 1) : most > 0.f && most < __builtin_inff() ? most : 1.f;
+            h.scale[0] = scale * h.inv_t, h.scale[1] = scale;
         }
     }
 }
 
+// ---- a teacher's entries -------------------------------------------------------------------------------------------------
+
+constexpr int kMaxTop = 1024;
+
+__device__ __forceinline__ float teacher_logit(const HeadTop& k, int64_t i) {
+    return k.dtype == PSGD_F32 ? as_global(static_cast<const float*>(k.teacher))[i] : (float)as_global(static_cast<const bf16_t*>(k.teacher))[i];
+}
+// whether an entry counts: a word of the vocabulary, of some probability
+__device__ __forceinline__ bool entry_counts(const HeadTop& k, int64_t i, int vocab) {
+    return label_counts(as_global(k.index)[i], vocab) && teacher_logit(k, i) != -__builtin_inff();
+}
+
+// which tokens have entries: a wavefront each
+__global__ __launch_bounds__(kThreads) void head_top_count_kernel(HeadTop k, int tokens, int vocab, int64_t* labels) {
+    const int lane = threadIdx.x & 63;
+    for (int t = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); t < tokens; t += gridDim.x * (kThreads / 64)) {
+        bool any = false;
+        for (int i = lane; i < k.top; i += 64) any |= entry_counts(k, t * k.ld + i, vocab);
+        any = __any(any);
+        if (lane == 0) as_global(labels)[t] = any ? 0 : -1;
+    }
+}
+
+// The lists of the piece's tokens, a workgroup each, of up to 256 threads: the entries are sorted by word, those of one word become one with the sum of their
+// probabilities.  `size`: the entries rounded up to a power of two, 64 at least.  write_labels: the tokens have not been looked at before (labels).
+__global__ __launch_bounds__(256) void head_top_lists_kernel(HeadDev h, int first, int size, int64_t* write_labels) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    unsigned long long* key = reinterpret_cast<unsigned long long*>(smem);      // [size]: word, place among the entries
+    float* value = reinterpret_cast<float*>(key + size);                        // [size]: the teacher's logits, as they came
+    int* word = reinterpret_cast<int*>(value + size);                           // [size]: the list
+    __shared__ float sums[4];
+    __shared__ int counts[4];
+    const HeadTop& k = h.top;
+    const int l = blockIdx.x, threads = blockDim.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, waves = threads >> 6;
+    if (!h.direct && l >= *h.count - first) return;
+    const int64_t token = h.direct ? l : h.rows[first + l];
+    float most = -__builtin_inff();
+    for (int i = threadIdx.x; i < size; i += threads) {
+        const int64_t at = token * k.ld + i;
+        const bool in = i < k.top && entry_counts(k, at, h.vocab);
+        key[i] = in ? (unsigned long long)as_global(k.index)[at] << 10 | (unsigned)i : ~0ull;
+        value[i] = in ? teacher_logit(k, at) : 0.f;
+        if (in) most = fmaxf(most, value[i]);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if (lane == 0) sums[wv] = most;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) most = fmaxf(most, sums[w]);
+    for (int len = 2; len <= size; len <<= 1)
+        for (int step = len >> 1; step > 0; step >>= 1) {
+            for (int i = threadIdx.x; i < size / 2; i += threads) {
+                const int a = 2 * i - (i & (step - 1)), b = a + step;
+                const unsigned long long x = key[a], y = key[b];
+                if ((x > y) == ((a & len) == 0)) key[a] = y, key[b] = x;
+            }
+            __syncthreads();
+        }
+    // a thread has `each` entries after each other; a word's probability is its first entry's to write
+    const int each = size / threads, from = threadIdx.x * each;
+    float mine = 0.f;
+    int words = 0;
+    for (int i = from; i < from + each; ++i)
+        if (key[i] != ~0ull) {
+            mine += expf((value[key[i] & 1023] - most) * h.inv_t);
+            words += i == 0 || (key[i - 1] >> 10) != (key[i] >> 10);
+        }
+    int up = words;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(up, d);
+        up += lane >= d ? o : 0;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
+    if (lane == 63) { counts[wv] = up; sums[wv] = mine; }
+    __syncthreads();
+    float total = 0.f;
+    int to = up - words, n = 0;
+    for (int w = 0; w < waves; ++w) {
+        total += sums[w];
+        to += w < wv ? counts[w] : 0;
+        n += counts[w];
+    }
+    const float log_total = logf(total);
+    const int64_t list = (int64_t)l * k.top;
+    for (int i = from; i < from + each; ++i)
+        if (key[i] != ~0ull && (i == 0 || (key[i - 1] >> 10) != (key[i] >> 10))) {
+            const int y = (int)(key[i] >> 10);
+            const float z = (value[key[i] & 1023] - most) * h.inv_t;
+            float e = expf(z);
+            bool several = false;
+            for (int o = i + 1; o < size && (int64_t)(key[o] >> 10) == y; ++o) {
+                e += expf((value[key[o] & 1023] - most) * h.inv_t);
+                several = true;
+            }
+            word[to] = y;
+            as_global(k.word)[list + to] = y;
+            as_global(k.q)[list + to] = e / total;
+            as_global(k.log_q)[list + to] = (several ? logf(e) : z) - log_total;
+            ++to;
+        }
+    __syncthreads();
+    for (int tile = threadIdx.x; tile <= h.tiles; tile += threads) {
+        const int64_t bound = (int64_t)tile * h.tile_width;
+        int low = 0, high = n;
+        while (low < high) {
+            const int mid = (low + high) >> 1;
+            if (word[mid] < bound) low = mid + 1; else high = mid;
+        }
+        as_global(k.start)[(int64_t)l * (h.tiles + 1) + tile] = (unsigned short)low;
+    }
+    if (write_labels && threadIdx.x == 0) as_global(write_labels)[token] = n > 0 ? 0 : -1;
+}
+
 // ---- logits of a piece: statistics per tile, exponentials --------------------------------------------------------------
 
-template <TileShape SHAPE, int KEEP>
+// The logits of the teacher's words in this tile: to their lists, and out of the accumulators.  A lane seeks the word among its own columns.
+template <class T>
+__device__ __forceinline__ void take_listed(T& tile, const HeadDev& h, int p0, int l0, int nl, int at_p) {
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j) {
+        const int l = l0 + tile.row(j);
+        int e = 0, end = 0;
+        if (l < nl) {
+            const PSGD_GLOBAL unsigned short* start = as_global(h.top.start) + (int64_t)l * (h.tiles + 1) + at_p;
+            e = start[0], end = start[1];
+        }
+        const int64_t list = (int64_t)l * h.top.top;
+        for (; __any(e < end); ++e) {
+            const int y = e < end ? as_global(h.top.word)[list + e] - p0 - tile.col(0, 0) : -1;
+            const bool found = y >= 0 && y < 32 * T::FP && (y & 4) == 0;
+            if (!__any(found)) continue;
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const bool here = y == 32 * i + 8 * (v >> 2) + (v & 3);
+                    x = here ? tile.acc[i][j][v] : x;
+                    tile.acc[i][j][v] = here ? -__builtin_inff() : tile.acc[i][j][v];
+                }
+            if (found) as_global(h.top.logit)[list + e] = x;
+        }
+    }
+}
+
+// TOP: a teacher's entries in the place of labels
+template <TileShape SHAPE, int KEEP, bool TOP>
 __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_kernel(TileArgs t, HeadDev h) {
     extern __shared__ __align__(16) unsigned char smem[];
     using T = Tile<true, true, SHAPE>;
@@ -179,7 +341,8 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
     const int p0 = at.p * T::BP, l0 = at.l * BL;
     T tile;
     tile.template run<true>(t, p0, l0, nl, t.K, 0, 1, (PSGD_TLDS unsigned char*)smem);
-    constexpr float kLog2e = 1.4426950408889634f;
+    if constexpr (TOP) take_listed(tile, h, p0, l0, nl, at.p);
+    const float log2e = TOP ? 1.4426950408889634f * h.inv_t : 1.4426950408889634f;
     // the wave's maximum per row, over its columns; a tile has at least one column
     float* red = reinterpret_cast<float*>(smem);        // [WP][BL]
     __syncthreads();
@@ -205,8 +368,8 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
         const float base = m == -__builtin_inff() ? 0.f : m;
         // The label's element, if it is this lane's (of eight columns next to each other a lane has the first or the last four), is left out of
         // the sum.  Few tiles have it: the search for it stands apart, and only reads.
-        const int y = l < nl ? label_of(h, t.first, l) - p0 - tile.col(0, 0) : -1;
-        const bool found = y >= 0 && y < 32 * T::FP && (y & 4) == 0, any = __any(found);
+        const int y = !TOP && l < nl ? label_of(h, t.first, l) - p0 - tile.col(0, 0) : -1;
+        const bool found = !TOP && y >= 0 && y < 32 * T::FP && (y & 4) == 0, any = !TOP && __any(found);
         float at_label = 0.f, s = 0.f;
         if (any) {
 #pragma unroll
@@ -219,7 +382,7 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
         for (int i = 0; i < T::FP; ++i)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const float e = __builtin_amdgcn_exp2f((tile.acc[i][j][v] - base) * kLog2e);
+                const float e = __builtin_amdgcn_exp2f((tile.acc[i][j][v] - base) * log2e);
                 s += e;
                 tile.acc[i][j][v] = e;
             }
@@ -264,14 +427,14 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
 
 // ---- the row's sum, the loss, and D ------------------------------------------------------------------------------------
 
-// Largest logit of row l and the sum of exp(logit - it) over all columns but the label's, by all threads of the block
+// Largest logit of row l and the sum of exp(logit - it) (over the temperature) over all columns but the label's or the list's, by all threads of the block
 struct RowSum { float most, others; };
 __device__ __forceinline__ RowSum row_sum(const HeadDev& h, int l, float* shared) {
     const float2* st = h.stats + (int64_t)l * h.tiles;
     float m = -__builtin_inff(), s = 0.f;
     auto join = [&](float mo, float so) {
         const float n = fmaxf(m, mo);
-        if (n != -__builtin_inff()) s = s * expf(m - n) + so * expf(mo - n);
+        if (n != -__builtin_inff()) s = s * expf((m - n) * h.inv_t) + so * expf((mo - n) * h.inv_t);
         else s += so;
         m = n;
     };
@@ -383,6 +546,129 @@ __global__ __launch_bounds__(kThreads) void head_rows_kernel(HeadDev h, int firs
     }
 }
 
+// exp(u) - 1 - u and exp(u) - 1 of small u by their series, without the digits that the differences lose
+constexpr float kSmallU = 0.25f;        // (the next term: 2 u^6 / 40320 of the sum, 1.2e-8)
+__device__ __forceinline__ float exp_rest(float u) {
+    return u * u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f);
+}
+
+// The same against a teacher: with q its probabilities, p the head's and u = log p - log q,
+//   loss = sum_v q log(q / p) = sum over the list of (p - q - q u = q (e^u - 1 - u)) + sum over the others of p,
+// of whose terms none is negative;  D = c (p - q), p - q = q (e^u - 1).  The others' D comes of their exponentials, the list's is written over it.
+template <int KEEP, int PL>
+__global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int first, int most_rows, int span) {
+    __shared__ float shared[8];
+    const int l = blockIdx.x;
+    if (l >= (h.direct ? most_rows : min(most_rows, *h.count - first))) return;
+    const int token = h.direct ? first + l : h.rows[first + l], n = h.top.start[(int64_t)l * (h.tiles + 1) + h.tiles];
+    const int begin = blockIdx.y * span, end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
+    float scale = 1.f;
+    if (KEEP != KEEP_NONE && h.direct && (h.weight || (l == 0 && blockIdx.y == 0))) {
+        const bool write = l == 0 && blockIdx.y == 0;
+        scale = direct_scale(h, shared, write);
+        if (write && threadIdx.x == 0) h.scale[0] = scale * h.inv_t;
+    }
+    if (n == 0) {
+        if (blockIdx.y == 0 && threadIdx.x == 0) h.loss[token] = 0.f;
+        if constexpr (KEEP != KEEP_NONE)
+            for (int v = begin + 8 * threadIdx.x; v < end; v += 8 * kThreads)
+#pragma unroll
+                for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL uintx4*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = uintx4{0u, 0u, 0u, 0u};
+        return;
+    }
+    uintx4 e[KEEP == KEEP_F32 ? 2 : 1];
+    auto fetch = [&](int v) {
+        if constexpr (KEEP == KEEP_F16) {
+            e[0] = __builtin_nontemporal_load(reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global((_Float16*)h.e) + l * h.ldv + v));
+        } else if constexpr (KEEP == KEEP_F32) {
+            const PSGD_GLOBAL uintx4* p = reinterpret_cast<const PSGD_GLOBAL uintx4*>(as_global((float*)h.e) + l * h.ldv + v);
+            e[0] = __builtin_nontemporal_load(p), e[1] = __builtin_nontemporal_load(p + 1);
+        }
+    };
+    const int start = begin + 8 * threadIdx.x;
+    if (KEEP != KEEP_NONE && start < end) fetch(start);
+    const RowSum r = row_sum(h, l, shared);
+    // the list's own maximum and sum, and then the row's
+    const int64_t list = (int64_t)l * h.top.top;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    auto all = [&](float x, auto join) {        // of all threads
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) x = join(x, __shfl_xor(x, d));
+        __syncthreads();
+        if (lane == 0) shared[wv] = x;
+        __syncthreads();
+        x = shared[0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) x = join(x, shared[w]);
+        return x;
+    };
+    auto larger = [](float a, float b) { return fmaxf(a, b); };
+    auto plus = [](float a, float b) { return a + b; };
+    float most = r.most;
+    for (int i = threadIdx.x; i < n; i += kThreads) most = fmaxf(most, h.top.logit[list + i]);
+    most = all(most, larger);
+    float sum = 0.f;
+    for (int i = threadIdx.x; i < n; i += kThreads) sum += expf((h.top.logit[list + i] - most) * h.inv_t);
+    const float others = r.others == 0.f ? 0.f : r.others * expf((r.most - most) * h.inv_t), total = all(sum, plus) + others;
+    const float log_total = logf(total);
+    struct Word { float p, q, u; bool small; };
+    auto listed = [&](int i) {
+        Word w;
+        const float z = (h.top.logit[list + i] - most) * h.inv_t;
+        w.q = h.top.q[list + i];
+        w.p = expf(z) / total;
+        w.u = z - log_total - h.top.log_q[list + i];
+        w.small = fabsf(w.u) <= kSmallU;
+        return w;
+    };
+    if (blockIdx.y == 0) {
+        float loss = 0.f;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const Word w = listed(i);
+            // (a probability that is 0 in 32 bits has a logarithm all the same, or none)
+            loss += w.small ? w.q * exp_rest(w.u) : w.q == 0.f ? w.p : w.p - w.q - w.q * w.u;
+        }
+        loss = all(loss, plus);
+        if (threadIdx.x == 0) h.loss[token] = loss + others / total;
+    }
+    if constexpr (KEEP == KEEP_NONE) return;
+    const float weight = h.weight ? h.weight[token] / (h.direct ? scale : h.scale[1]) : 1.f, c = weight / total;
+    for (int v = start; v < end; v += 8 * kThreads) {
+        const float in_tile = h.stats[(int64_t)l * h.tiles + v / h.tile_width].x;
+        const float f = expf((in_tile - most) * h.inv_t) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
+        float x[8];
+        if constexpr (KEEP == KEEP_F16) {
+            const halfx8 q = __builtin_bit_cast(halfx8, e[0]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = (float)q[u] * f;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = __uint_as_float(e[KEEP == KEEP_F32 ? u >> 2 : 0][u & 3]) * f;
+        }
+        if (v + 8 * kThreads < end) fetch(v + 8 * kThreads);
+        bf16x8 out[PL];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            bf16_t q[PL];
+            split_planes<PL>(x[u], q);
+#pragma unroll
+            for (int k = 0; k < PL; ++k) out[k][u] = q[k];
+        }
+#pragma unroll
+        for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL bf16x8*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = out[k];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const int v = h.top.word[list + i];
+        if (v < begin || v >= end) continue;
+        const Word w = listed(i);
+        bf16_t q[PL];
+        split_planes<PL>((w.small ? w.q * (w.u + exp_rest(w.u)) : w.p - w.q) * weight, q);
+#pragma unroll
+        for (int k = 0; k < PL; ++k) as_global(h.D)[k * h.d_plane + l * h.ldv + v] = q[k];
+    }
+}
+
 // fp32 sums of all pieces to bf16
 __global__ __launch_bounds__(kThreads) void head_round_kernel(const float* sum, int64_t rows, int cols, int64_t lds, bf16_t* out, int64_t ld, int accumulate) {
     const int quads = (cols + 3) / 4;
@@ -410,6 +696,7 @@ constexpr int64_t kMaxPiece = (int64_t)1 << 23, kMaxPieceLogits = (int64_t)1 << 
 struct HeadPlan {
     size_t bytes = 0;
     size_t count, scale, rows, label, counts, xc, wc, stats, at_label, e, D, part, dw_part, sum;
+    size_t entries, word, q, log_q, logit, start;        // of a teacher
     int64_t ldc, ldv;
     int piece, pieces, tiles, x_planes, d_planes, keep;
     TilePlan logits, dx, dw;
@@ -418,7 +705,8 @@ struct HeadPlan {
     bool copy_w, direct, pair;
 };
 
-static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
+// top: entries of a teacher per token, 0 with labels
+static HeadPlan head_plan(const psgd_head_desc& s, bool gradients, int64_t top) {
     HeadPlan p = {};
     const bool f32 = s.dtype == PSGD_F32;
     p.ldc = up8(s.d);
@@ -432,7 +720,8 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.dw_pairs = !f32 && p.d_planes == 3 ? kPairsL3 : kPairs1, p.n_dw_pairs = !f32 ? p.d_planes : 1;
     // tokens per piece (statistics: 8 bytes for each tile of 128 words; tiles of 64 are not taken for so many tokens, but where all words are in one)
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
-    const size_t row = !gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes);
+    const size_t row = (!gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes)) +
+                       (top ? 16 * top + s.vocab / 128 * 2 + 8 : 0);
     const int64_t launch = std::min(kMaxPiece, std::max<int64_t>(1, kMaxPieceLogits / s.vocab));
     const int64_t most = std::min(std::min(tokens, launch), s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256));
     p.pieces = (int)((tokens + most - 1) / most);
@@ -447,14 +736,21 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients) {
     p.tiles = (int)((s.vocab + tile_p(p.logits.shape) - 1) / tile_p(p.logits.shape));
     auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += up256(bytes); return at; };
     p.count = take(4);
-    p.scale = take(4);
+    p.scale = take(8);
     p.rows = take((size_t)tokens * 4);
     p.label = take((size_t)tokens * 4);
     p.counts = take((size_t)(tokens + 63) / 64 * 8);
     p.xc = p.direct && !gradients ? 0 : take((size_t)tokens * p.ldc * 2 * p.x_planes);      // (direct: where dX takes X's place)
     p.wc = p.copy_w ? take((size_t)s.vocab * p.ldc * 2) : 0;
     p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
-    p.at_label = take((size_t)p.piece * 4);
+    if (top) {
+        p.entries = take((size_t)tokens * 8);
+        p.word = take((size_t)p.piece * top * 4), p.q = take((size_t)p.piece * top * 4), p.log_q = take((size_t)p.piece * top * 4);
+        p.logit = take((size_t)p.piece * top * 4);
+        p.start = take((size_t)p.piece * (p.tiles + 1) * 2);
+    } else {
+        p.at_label = take((size_t)p.piece * 4);
+    }
     if (gradients) {
         const size_t elems = (size_t)p.piece * p.ldv;
         p.e = take(elems * (p.keep == KEEP_F16 ? 2 : 4));
@@ -482,11 +778,11 @@ static int head_shape(const psgd_head_desc* s) {
     return PSGD_OK;
 }
 
-template <TileShape SHAPE, int KEEP>
+template <TileShape SHAPE, int KEEP, bool TOP>
 static hipError_t launch_logits_as(const TileArgs& t, const HeadDev& h, hipStream_t st) {
     const int64_t blocks = h.tiles * (int64_t)((t.L.extent + tile_l(SHAPE) - 1) / tile_l(SHAPE));
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    auto kfn = head_logits_kernel<SHAPE, KEEP>;
+    auto kfn = head_logits_kernel<SHAPE, KEEP, TOP>;
     constexpr int lds = Tile<true, true, SHAPE>::LDS_BYTES;
     if (lds > 48 * 1024) {
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -495,61 +791,101 @@ static hipError_t launch_logits_as(const TileArgs& t, const HeadDev& h, hipStrea
     hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(kTileThreads), lds, st, t, h);
     return hipGetLastError();
 }
+template <TileShape SHAPE, int KEEP>
+static hipError_t launch_logits_for(const TileArgs& t, const HeadDev& h, hipStream_t st) {
+    return h.top.top ? launch_logits_as<SHAPE, KEEP, true>(t, h, st) : launch_logits_as<SHAPE, KEEP, false>(t, h, st);
+}
 template <TileShape SHAPE>
 static hipError_t launch_logits_shape(const TileArgs& t, const HeadDev& h, hipStream_t st) {
-    if (h.keep == KEEP_NONE) return launch_logits_as<SHAPE, KEEP_NONE>(t, h, st);
-    if (h.keep == KEEP_F16) return launch_logits_as<SHAPE, KEEP_F16>(t, h, st);
-    return launch_logits_as<SHAPE, KEEP_F32>(t, h, st);
+    if (h.keep == KEEP_NONE) return launch_logits_for<SHAPE, KEEP_NONE>(t, h, st);
+    if constexpr (!tile_is_split(SHAPE))
+        if (h.keep == KEEP_F16) return launch_logits_for<SHAPE, KEEP_F16>(t, h, st);
+    return launch_logits_for<SHAPE, KEEP_F32>(t, h, st);
 }
 static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, TileShape shape, hipStream_t st) {
     if (shape == TILE_256) return launch_logits_shape<TILE_256>(t, h, st);
     if (shape == TILE_128) return launch_logits_shape<TILE_128>(t, h, st);
     if (shape == TILE_MANY) return launch_logits_shape<TILE_MANY>(t, h, st);
-    if (shape == TILE_SPLIT) return h.keep == KEEP_NONE ? launch_logits_as<TILE_SPLIT, KEEP_NONE>(t, h, st) : launch_logits_as<TILE_SPLIT, KEEP_F32>(t, h, st);
-    if (shape == TILE_SPLIT_THIN) return h.keep == KEEP_NONE ? launch_logits_as<TILE_SPLIT_THIN, KEEP_NONE>(t, h, st) : launch_logits_as<TILE_SPLIT_THIN, KEEP_F32>(t, h, st);
+    if (shape == TILE_SPLIT) return launch_logits_shape<TILE_SPLIT>(t, h, st);
+    if (shape == TILE_SPLIT_THIN) return launch_logits_shape<TILE_SPLIT_THIN>(t, h, st);
     return launch_logits_shape<TILE_THIN>(t, h, st);
 }
 
+template <int KEEP, int PL>
+static hipError_t launch_rows_as(const HeadDev& h, int first, int rows, int span, dim3 grid, hipStream_t st) {
+    if (h.top.top) hipLaunchKernelGGL((head_top_rows_kernel<KEEP, PL>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    else hipLaunchKernelGGL((head_rows_kernel<KEEP, PL>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    return hipGetLastError();
+}
 static hipError_t launch_rows(const HeadDev& h, int first, int rows, hipStream_t st) {
-    if (h.keep == KEEP_NONE) {
-        hipLaunchKernelGGL((head_rows_kernel<KEEP_NONE, 1>), dim3(rows), dim3(kThreads), 0, st, h, first, rows, 0);
-        return hipGetLastError();
-    }
+    if (h.keep == KEEP_NONE) return launch_rows_as<KEEP_NONE, 1>(h, first, rows, 0, dim3(rows), st);
     // parts of the vocabulary, so that a few rows fill the card as well
     int64_t parts = std::max<int64_t>(1, std::min<int64_t>((h.ldv + 8 * kThreads - 1) / (8 * kThreads), 2048 / std::max(1, rows)));
     const int span = (int)(((h.ldv + parts - 1) / parts + 7) / 8 * 8);
     parts = (h.ldv + span - 1) / span;
     const dim3 grid(rows, (unsigned)parts);
-    if (h.keep == KEEP_F16) hipLaunchKernelGGL((head_rows_kernel<KEEP_F16, 1>), grid, dim3(kThreads), 0, st, h, first, rows, span);
-    else hipLaunchKernelGGL((head_rows_kernel<KEEP_F32, 3>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    return h.keep == KEEP_F16 ? launch_rows_as<KEEP_F16, 1>(h, first, rows, span, grid, st) : launch_rows_as<KEEP_F32, 3>(h, first, rows, span, grid, st);
+}
+
+// A teacher's entries, in the place of labels.
+struct HeadTeacher {
+    const int64_t* index;
+    const void* logits;
+    int dtype;
+    int64_t ld, top;
+    float temperature;
+};
+static int teacher_shape(int64_t top) { return top < 1 || top > kMaxTop ? PSGD_E_SHAPE : PSGD_OK; }
+
+static hipError_t launch_lists(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
+    int size = 64;
+    while (size < h.top.top) size *= 2;
+    hipLaunchKernelGGL(head_top_lists_kernel, dim3(rows), dim3(std::min(size, 256)), (size_t)size * 16, st, h, first, size, write_labels);
     return hipGetLastError();
 }
 
-static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
+static int head_run(const psgd_head_desc* s, const HeadTeacher* teacher, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
                     const float* weight, float* loss, void* dx, void* dw, int accumulate) {
     if (int rc = head_shape(s)) return rc;
-    if (!workspace || !w || (gradients && !dw) || (s->tokens != 0 && (!x || !labels || !loss || (gradients && !dx)))) return PSGD_E_INVALID_ARG;
+    if (teacher) {
+        const float inv = 1.f / teacher->temperature;
+        if (bad_dtype(teacher->dtype) || !(teacher->temperature > 0.f && inv > 0.f && inv < __builtin_inff())) return PSGD_E_INVALID_ARG;
+        if (s->tokens != 0 && (!teacher->index || !teacher->logits)) return PSGD_E_INVALID_ARG;
+        if (int rc = teacher_shape(teacher->top)) return rc;
+        if (teacher->ld > kMaxLd) return PSGD_E_SHAPE;
+        if (teacher->ld < teacher->top || misaligned(teacher->index) || misaligned(teacher->logits)) return PSGD_E_ALIGN;
+    }
+    if (!workspace || !w || (gradients && !dw) || (s->tokens != 0 && (!x || (!labels && !teacher) || !loss || (gradients && !dx)))) return PSGD_E_INVALID_ARG;
     const int64_t ldx = s->ldx ? s->ldx : s->d, ldw = s->ldw ? s->ldw : s->d, lddx = s->lddx ? s->lddx : s->d, lddw = s->lddw ? s->lddw : s->d;
     if (ldx > kMaxLd || ldw > kMaxLd || lddx > kMaxLd || lddw > kMaxLd) return PSGD_E_SHAPE;
     if (bad_ld(ldx, s->d) || bad_ld(ldw, s->d) || misaligned(x) || misaligned(w) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
     if (gradients && (bad_ld(lddx, s->d) || bad_ld(lddw, s->d) || misaligned(dx) || misaligned(dw))) return PSGD_E_ALIGN;
     const int64_t size = s->dtype == PSGD_F32 ? 4 : 2, g_size = s->grad_dtype == PSGD_F32 ? 4 : 2;
     const bool in_place = gradients && x && x == dx && (ldx == lddx || s->tokens == 1);
-    const RowArea in[] = {{x, s->tokens, ldx * size, s->d * size}, {w, s->vocab, ldw * size, s->d * size}, {labels, 1, 0, s->tokens * 8},
+    const int64_t t_size = teacher && teacher->dtype == PSGD_BF16 ? 2 : 4, t_ld = teacher ? teacher->ld : 0, top = teacher ? teacher->top : 0;
+    const RowArea in[] = {{teacher ? teacher->index : nullptr, s->tokens, t_ld * 8, top * 8}, {teacher ? teacher->logits : nullptr, s->tokens, t_ld * t_size, top * t_size},
+                          {x, s->tokens, ldx * size, s->d * size}, {w, s->vocab, ldw * size, s->d * size}, {labels, 1, 0, s->tokens * 8},
                            {weight, 1, 0, s->tokens * 4}};
     const RowArea out[] = {{dx, s->tokens, lddx * size, s->d * size}, {dw, s->vocab, lddw * g_size, s->d * g_size}, {loss, 1, 0, s->tokens * 4}};
     for (const RowArea& o : out)
         for (const RowArea& i : in)
-            if (overlap(o, i) && !(in_place && &o == out && &i == in)) return PSGD_E_INVALID_ARG;
+            if (overlap(o, i) && !(in_place && &o == out && &i == in + 2)) return PSGD_E_INVALID_ARG;
     if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return PSGD_E_INVALID_ARG;
-    const HeadPlan p = head_plan(*s, gradients);
+    const HeadPlan p = head_plan(*s, gradients, top);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     forget_errors();
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const bool f32 = s->dtype == PSGD_F32;
 
     HeadDev h = {};
-    h.labels = labels, h.weight = weight, h.loss = loss;
+    int64_t* entries = reinterpret_cast<int64_t*>(ws + p.entries);
+    h.labels = teacher ? entries : labels, h.weight = weight, h.loss = loss;
+    h.inv_t = 1.f;
+    if (teacher) {
+        h.inv_t = 1.f / teacher->temperature;
+        h.top = {teacher->index, teacher->logits, teacher->dtype, (int)top, teacher->ld, reinterpret_cast<int*>(ws + p.word), reinterpret_cast<float*>(ws + p.q),
+                 reinterpret_cast<float*>(ws + p.log_q), reinterpret_cast<float*>(ws + p.logit), reinterpret_cast<unsigned short*>(ws + p.start)};
+    }
     h.tokens = (int)s->tokens, h.d = (int)s->d, h.vocab = (int)s->vocab;
     h.count = reinterpret_cast<int*>(ws + p.count);
     h.scale = reinterpret_cast<float*>(ws + p.scale);
@@ -570,6 +906,11 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
     // at most 1024 blocks, each of which reads the labels before its own, and a row per wave at least (2048 x 4096 x 512, loss: 48 us with four, 45 with one)
     const int per = std::max(4, (int)((s->tokens + 1023) / 1024));
     const dim3 blocks((unsigned)std::max<int64_t>(1, (s->tokens + per - 1) / per));
+    if (teacher && !h.direct && s->tokens > 0) {
+        const int64_t groups = (s->tokens + kThreads / 64 - 1) / (kThreads / 64);
+        hipLaunchKernelGGL(head_top_count_kernel, dim3((unsigned)std::min<int64_t>(groups, 1 << 16)), dim3(kThreads), 0, st, h.top, h.tokens, h.vocab, entries);
+        if (hipGetLastError() != hipSuccess) return PSGD_E_HIP;
+    }
     if (h.direct) {}
     else if (f32) hipLaunchKernelGGL(head_gather_kernel<float>, blocks, dim3(kGatherThreads), 0, st, h, per, (const float*)x, ldx, xc, p.ldc, p.x_planes, (float*)dx, lddx);
     else hipLaunchKernelGGL(head_gather_kernel<bf16_t>, blocks, dim3(kGatherThreads), 0, st, h, per, (const bf16_t*)x, ldx, xc, p.ldc, p.x_planes, (bf16_t*)dx, lddx);
@@ -595,6 +936,7 @@ static int head_run(const psgd_head_desc* s, bool gradients, void* workspace, vo
             t.L = tokens;
             t.K = (int)(f32 ? s->d : p.ldc);
             t.pairs = kPairs1, t.n_pairs = 1;
+            if (teacher && launch_lists(h, first, rows, h.direct ? entries : nullptr, st) != hipSuccess) return PSGD_E_HIP;
             if (launch_logits(t, h, p.logits.shape, st) != hipSuccess || launch_rows(h, first, rows, st) != hipSuccess) return PSGD_E_HIP;
         }
         if (!gradients) continue;
@@ -639,16 +981,33 @@ using namespace psgd;
 extern "C" {
 
 size_t psgd_head_workspace_bytes(const psgd_head_desc* desc, int gradients) {
-    return head_shape(desc) ? 0 : head_plan(*desc, gradients != 0).bytes;
+    return head_shape(desc) ? 0 : head_plan(*desc, gradients != 0, 0).bytes;
 }
 
 int psgd_head_loss(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels, float* loss) {
-    return head_run(desc, false, workspace, stream, x, w, labels, nullptr, loss, nullptr, nullptr, 0);
+    return head_run(desc, nullptr, false, workspace, stream, x, w, labels, nullptr, loss, nullptr, nullptr, 0);
 }
 
 int psgd_head_loss_grad(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
                         const float* weight, float* loss, void* dx, void* dw, int accumulate) {
-    return head_run(desc, true, workspace, stream, x, w, labels, weight, loss, dx, dw, accumulate);
+    return head_run(desc, nullptr, true, workspace, stream, x, w, labels, weight, loss, dx, dw, accumulate);
+}
+
+size_t psgd_head_distill_workspace_bytes(const psgd_head_desc* desc, int64_t top, int gradients) {
+    return head_shape(desc) || teacher_shape(top) ? 0 : head_plan(*desc, gradients != 0, top).bytes;
+}
+
+int psgd_head_distill(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, int64_t top, const int64_t* index,
+                      const void* teacher, int teacher_dtype, int64_t ld_top, float temperature, float* loss) {
+    const HeadTeacher t = {index, teacher, teacher_dtype, ld_top, top, temperature};
+    return head_run(desc, &t, false, workspace, stream, x, w, nullptr, nullptr, loss, nullptr, nullptr, 0);
+}
+
+int psgd_head_distill_grad(const psgd_head_desc* desc, void* workspace, void* stream, const void* x, const void* w, int64_t top, const int64_t* index,
+                           const void* teacher, int teacher_dtype, int64_t ld_top, float temperature, const float* weight, float* loss, void* dx, void* dw,
+                           int accumulate) {
+    const HeadTeacher t = {index, teacher, teacher_dtype, ld_top, top, temperature};
+    return head_run(desc, &t, true, workspace, stream, x, w, nullptr, weight, loss, dx, dw, accumulate);
 }
 
 }  // extern "C"

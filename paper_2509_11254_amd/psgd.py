@@ -26,6 +26,7 @@ EXPORTS = [
     "psgd_strerror", "psgd_destroy", "psgd_profile_enable", "psgd_profile_select", "psgd_profile_read",
     "psgd_head_workspace_bytes", "psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore",
     "psgd_act_glu", "psgd_act_glu_backward", "psgd_act_wgrad_workspace_bytes", "psgd_act_wgrad",
+    "psgd_head_distill_workspace_bytes", "psgd_head_distill", "psgd_head_distill_grad",
     "psgd_norm", "psgd_norm_backward_workspace_bytes", "psgd_norm_backward", "psgd_expert_sort_workspace_bytes", "psgd_expert_sort",
     "psgd_expert_rows", "psgd_expert_combine", "psgd_expert_combine_backward",
 ]
@@ -136,6 +137,10 @@ def load_library() -> C.CDLL:
     lib.psgd_act_wgrad_workspace_bytes.argtypes = [l, l, l, i]
     lib.psgd_act_wgrad_workspace_bytes.restype = C.c_size_t
     lib.psgd_act_wgrad.argtypes = [vp, vp, l, l, l, vp, i, l, vp, l, vp, vp, i, l, i]
+    lib.psgd_head_distill_workspace_bytes.argtypes = [hd, l, i]
+    lib.psgd_head_distill_workspace_bytes.restype = C.c_size_t
+    lib.psgd_head_distill.argtypes = [hd, vp, vp, vp, vp, l, vp, vp, i, l, C.c_float, vp]
+    lib.psgd_head_distill_grad.argtypes = [hd, vp, vp, vp, vp, l, vp, vp, i, l, C.c_float, vp, vp, vp, vp, i]
     lib.psgd_norm.argtypes = [vp, l, l, i, vp, vp, l, vp, vp, i, C.c_float, vp, vp, l, vp]
     lib.psgd_norm_backward_workspace_bytes.argtypes = [l, l, i]
     lib.psgd_norm_backward_workspace_bytes.restype = C.c_size_t
@@ -147,7 +152,7 @@ def load_library() -> C.CDLL:
     lib.psgd_expert_combine.argtypes = [vp, l, l, l, i, vp, l, vp, vp, vp, l]
     lib.psgd_expert_combine_backward.argtypes = [vp, l, l, l, i, vp, l, vp, l, vp, vp, vp, l, vp]
     for name in ("psgd_head_loss", "psgd_head_loss_grad", "psgd_act_store", "psgd_act_restore", "psgd_act_glu",
-                 "psgd_act_glu_backward", "psgd_act_wgrad", "psgd_norm", "psgd_norm_backward", "psgd_expert_sort",
+                 "psgd_act_glu_backward", "psgd_act_wgrad", "psgd_head_distill", "psgd_head_distill_grad", "psgd_norm", "psgd_norm_backward", "psgd_expert_sort",
                  "psgd_expert_rows", "psgd_expert_combine", "psgd_expert_combine_backward"):
         getattr(lib, name).restype = C.c_int
     lib.psgd_destroy.argtypes = [vp]
@@ -387,6 +392,10 @@ def _work_area(n_bytes: int, device):
     return buf, (buf.data_ptr() + 255) // 256 * 256
 
 
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
 class HeadLoss:
     """Softmax cross entropy of X W^T against labels without logits in memory, and its gradients: psgd_head_loss and
     psgd_head_loss_grad with a torch-allocated workspace, for one set of sizes and types.
@@ -435,6 +444,72 @@ class HeadLoss:
         _check(self.lib, None, self.lib.psgd_head_loss_grad(
             C.byref(self.desc), self._ws_ptr, _stream_for(stream, self.workspace, X, W, labels, loss, dX, dW, weight), X.data_ptr(),
             W.data_ptr(), labels.data_ptr(), weight.data_ptr() if weight is not None else None, loss.data_ptr(), dX.data_ptr(), dW.data_ptr(), 1 if accumulate else 0))
+
+
+def _entries(name: str, t, tokens: int, top: int, types) -> int:
+    """Checks tokens x top entries on the GPU, those of a token adjacent; how far apart tokens are."""
+    strides = t.stride()
+    if t.shape != (tokens, top) or t.dtype not in types or not t.is_cuda or (top > 1 and strides[1] != 1):
+        raise ValueError("%s: %d x %d adjacent entries of %s on the GPU expected, got %s with strides %s of %s on %s"
+                         % (name, tokens, top, types, tuple(t.shape), strides, t.dtype, t.device))
+    ld = strides[0] if tokens > 1 else top
+    if ld < top:
+        raise ValueError("%s: rows that lie over each other (%d elements apart, %d entries)" % (name, ld, top))
+    return ld
+
+
+class HeadDistill:
+    """Divergence of the head's probabilities softmax(X W^T / temperature) from a teacher's, of which the `top` largest logits are known,
+    without logits in memory, and its gradients: psgd_head_distill and psgd_head_distill_grad with a torch-allocated workspace, for one
+    set of sizes and types.
+
+    index (tokens x top int64) and teacher (its logits, float32 or bfloat16) have the same strides.  Entries whose index lies outside
+    [0, vocab) do not count, nor does a token without entries.  grad=False and streams: as for HeadLoss.
+    """
+
+    def __init__(self, tokens: int, d: int, vocab: int, top: int, dtype: int = PSGD_BF16, grad_dtype: Optional[int] = None, *,
+                 grad: bool = True, piece_tokens: int = 0, device: str = "cuda"):
+        self.lib = load_library()
+        self.desc = HeadDesc(int(tokens), int(d), int(vocab), 0, 0, 0, 0, int(dtype),
+                             int(dtype if grad_dtype is None else grad_dtype), int(piece_tokens))
+        self.top, self.grad = int(top), bool(grad)
+        sizes = [int(self.lib.psgd_head_distill_workspace_bytes(C.byref(self.desc), self.top, g)) for g in ([0, 1] if grad else [0])]
+        if min(sizes) == 0:
+            raise PsgdError(PSGD_E_INVALID_ARG, "sizes or types of the head")
+        self.workspace_bytes = max(sizes)
+        self.workspace, self._ws_ptr = _work_area(self.workspace_bytes, device)
+
+    def _inputs(self, X, W, index, teacher, loss):
+        import torch
+        d = self.desc
+        d.ldx, d.ldw = _matrix("X", X, d.tokens, d.d, d.dtype), _matrix("W", W, d.vocab, d.d, d.dtype)
+        ld = _entries("index", index, d.tokens, self.top, (torch.int64,))
+        _same("strides of index and teacher", ld, _entries("teacher", teacher, d.tokens, self.top, (torch.float32, torch.bfloat16)))
+        _vector("loss", loss, d.tokens, torch.float32)
+        return ld
+
+    def loss(self, X, W, index, teacher, loss, temperature: float = 1.0, stream=None) -> None:
+        """loss[t] <- sum_v q_tv log(q_tv / p_tv), 0 for tokens that do not count."""
+        ld = self._inputs(X, W, index, teacher, loss)
+        _check(self.lib, None, self.lib.psgd_head_distill(
+            C.byref(self.desc), self._ws_ptr, _stream_for(stream, self.workspace, X, W, index, teacher, loss), X.data_ptr(), W.data_ptr(), self.top,
+            index.data_ptr(), teacher.data_ptr(), _dtype_code(teacher), ld, float(temperature), loss.data_ptr()))
+
+    def loss_grad(self, X, W, index, teacher, loss, dX, dW, temperature: float = 1.0, weight=None, accumulate: bool = False, stream=None) -> None:
+        """loss as above; dX <- gradient of sum_t weight[t] loss[t] (weight None: the mean over the tokens that count), and
+        dW <- (accumulate: +=) its gradient.  dX may be X itself; otherwise results overlap nothing."""
+        import torch
+        if not self.grad:
+            raise ValueError("this HeadDistill has no workspace for gradients (grad=False)")
+        ld = self._inputs(X, W, index, teacher, loss)
+        d = self.desc
+        d.lddx, d.lddw = _matrix("dX", dX, d.tokens, d.d, d.dtype), _matrix("dW", dW, d.vocab, d.d, d.grad_dtype)
+        if weight is not None:
+            _vector("weight", weight, d.tokens, torch.float32)
+        _check(self.lib, None, self.lib.psgd_head_distill_grad(
+            C.byref(self.desc), self._ws_ptr, _stream_for(stream, self.workspace, X, W, index, teacher, loss, dX, dW, weight), X.data_ptr(), W.data_ptr(),
+            self.top, index.data_ptr(), teacher.data_ptr(), _dtype_code(teacher), ld, float(temperature), _ptr(weight), loss.data_ptr(), dX.data_ptr(),
+            dW.data_ptr(), 1 if accumulate else 0))
 
 
 class Act8:
@@ -536,10 +611,6 @@ class WeightGrad:
         _check(self.lib, None, self.lib.psgd_act_wgrad(
             self._ws_ptr, _stream_for(stream, self.workspace, dY, G, kept.codes, kept.scales), tokens, out_features, in_features, dY.data_ptr(), self.dtype, ldy,
             kept.codes.data_ptr(), kept.ldc, kept.scales.data_ptr(), G.data_ptr(), self.grad_dtype, ldg, 1 if accumulate else 0))
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
 
 
 def norm(X, weight, bias, Y, stats=None, eps: float = 1e-5, add=None, total=None, stream=None) -> None:

@@ -1,8 +1,11 @@
-"""Host-side checks of the norms' and the experts' entry points that need no GPU: refusals (nothing is enqueued), workspace sizes, the binding."""
+"""Host-side checks of the norms', the experts' and the distillation's entry points that need no GPU: refusals (nothing is enqueued), workspace sizes, the binding."""
+import ctypes as C
+
 import pytest
 import torch
 
 from paper_2509_11254_amd import psgd
+from test_train_host import head
 from test_train_binding import OnGpu, OnStream, matrix
 
 F32, BF16 = psgd.PSGD_F32, psgd.PSGD_BF16
@@ -130,8 +133,55 @@ def test_rows_without_tokens(lib):
     assert combine_backward(lib, tokens=0, dy=None, ys=None, place=None, weight=None, dys=None, dweight=None) == OK
 
 
+def distill(lib, desc=None, grad=True, **change):
+    a = dict(workspace=M, stream=None, x=M, w=2 * M, top=12, index=4 * M, teacher=5 * M, t_dtype=F32, ld=16, temperature=2.0, weight=6 * M, loss=7 * M, dx=8 * M, dw=9 * M,
+             accumulate=0)
+    assert not set(change) - set(a)
+    a.update(change)
+    if not grad:
+        for k in ("weight", "dx", "dw", "accumulate"):
+            a.pop(k)
+    return (lib.psgd_head_distill_grad if grad else lib.psgd_head_distill)(C.byref(desc or head()), *a.values())
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(top=0), SHAPE), (dict(top=1025, ld=1032), SHAPE), (dict(ld=BIG), SHAPE), (dict(ld=11), ALIGN), (dict(index=M + 8), ALIGN), (dict(teacher=M + 4), ALIGN),
+    (dict(index=None), INVALID), (dict(teacher=None), INVALID), (dict(t_dtype=2), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
+    (dict(temperature=float("nan")), INVALID), (dict(temperature=float("inf")), INVALID), (dict(temperature=1e-42), INVALID), (dict(x=None), INVALID),
+    (dict(loss=None), INVALID), (dict(workspace=M + 16), ALIGN),
+    # 100 tokens: 99 rows of 16 entries and 12 more
+    (dict(loss=4 * M + 99 * 128 + 80), INVALID), (dict(loss=5 * M + 99 * 64 + 32), INVALID)])
+def test_distillation_refuses(lib, change, want):
+    assert distill(lib, **change) == want
+    assert distill(lib, grad=False, **change) == want
+    if "top" in change:
+        assert lib.psgd_head_distill_workspace_bytes(C.byref(head()), change["top"], 1) == 0
+
+
+def test_distillation_refuses_as_the_head(lib):
+    for change, want in ((dict(dtype=2), INVALID), (dict(d=0), SHAPE), (dict(tokens=-1), SHAPE), (dict(piece_tokens=-1), INVALID), (dict(ldx=60), ALIGN)):
+        assert distill(lib, head(**change)) == want
+    for k in ("dx", "dw"):
+        assert distill(lib, **{k: None}) == INVALID
+        assert distill(lib, **{k: 4 * M + 128}) == INVALID and distill(lib, **{k: 5 * M + 64}) == INVALID
+    assert distill(lib, dx=M, desc=head(ldx=72)) == INVALID
+    assert lib.psgd_head_distill_workspace_bytes(None, 5, 0) == 0
+
+
+def test_distillation_workspace_is_bounded(lib):
+    """Pieces of the tokens: lists and statistics exist for one piece at a time."""
+    def size(tokens, top, grad, **change):
+        return lib.psgd_head_distill_workspace_bytes(C.byref(head(tokens=tokens, vocab=64000, **change)), top, grad)
+
+    assert 0 < size(1 << 14, 1024, 1, grad_dtype=BF16) < 1.3 * 2 ** 30 and size(1 << 18, 1024, 1, grad_dtype=BF16) < 1.4 * 2 ** 30
+    assert size(1 << 22, 1024, 0) < 2.5 * 2 ** 30
+    assert size(1 << 14, 64, 1, piece_tokens=256) < 2 ** 28 and size(0, 64, 1) > 0
+    assert size(1000, 64, 1, piece_tokens=(1 << 63) - 1) == size(1000, 64, 1, piece_tokens=1000)
+
+
 def test_binding_refuses_sizes():
-    for make in (lambda: psgd.NormGrad(10, 16385), lambda: psgd.NormGrad(10, 10, 3), lambda: psgd.NormGrad(10, 10, F32, 7), lambda: psgd.ExpertSort(4, 0, 3),
+    for make in (lambda: psgd.HeadDistill(10, 64, 100, 0), lambda: psgd.HeadDistill(10, 64, 100, 1025), lambda: psgd.HeadDistill(10, 0, 100, 5),
+                 lambda: psgd.NormGrad(10, 16385), lambda: psgd.NormGrad(10, 10, 3), lambda: psgd.NormGrad(10, 10, F32, 7), lambda: psgd.ExpertSort(4, 0, 3),
                  lambda: psgd.ExpertSort(4, 2, 2000)):
         with pytest.raises(psgd.PsgdError):
             make()
@@ -157,7 +207,12 @@ def calls():
     t, s, e, d = 6, 2, 5, 40
     m, v = (lambda r, c=d: lambda dev: matrix(r, c, device=dev)), (lambda n, dtype=torch.float32, shape=None: lambda dev: vec(n, dtype, dev, shape))
     o, w = (lambda dev: expert_order(t, s, e, dev)), v(0, shape=(t, s))
+    plan = on(psgd.HeadDistill(t, d, 24, 5, F32, device="cpu"))
+    entries = [v(0, torch.int64, (t, 5)), v(0, shape=(t, 5))]
     return {
+        "distill": (lambda plan, x, w, i, k, l, stream: plan.loss(x, w, i, k, l, stream=stream), [plan, m(t), m(24), *entries, v(t)]),
+        "distill_grad": (lambda plan, x, w, i, k, l, dx, dw, c, stream: plan.loss_grad(x, w, i, k, l, dx, dw, weight=c, stream=stream),
+                         [plan, m(t), m(24), *entries, v(t), m(t), m(24), v(t)]),
         "norm": (lambda x, w, b, y, st, add, total, stream: psgd.norm(x, w, b, y, st, add=add, total=total, stream=stream),
                  [m(t), v(d), v(d), m(t), v(0, shape=(t, 2)), m(t), m(t)]),
         "norm_grad": (lambda plan, dy, x, w, st, dx, dw, db, past, stream: plan.run(dy, x, w, st, dx, dw, db, dtotal=past, stream=stream),
@@ -187,7 +242,7 @@ def test_tensors_of_another_device(monkeypatch, name):
     monkeypatch.setattr(psgd, "_check", stop)
     lib = psgd.load_library()
     for f in psgd.EXPORTS:
-        if f.startswith(("psgd_norm", "psgd_expert")) and not f.endswith("_bytes"):
+        if f.startswith(("psgd_norm", "psgd_expert", "psgd_head_distill")) and not f.endswith("_bytes"):
             monkeypatch.setattr(lib, f, lambda *a: 0)
     for stream, device in ((None, 0), (OnStream(0), 0), (OnStream(1), 1)):
         with pytest.raises(Enqueued):
@@ -199,7 +254,19 @@ def test_tensors_of_another_device(monkeypatch, name):
 
 def test_binding_refuses_tensors():
     m, w, st = (lambda r, c=40, dtype=torch.float32: matrix(r, c, dtype)), vec(40), vec(0, shape=(6, 2))
+    plan = psgd.HeadDistill(6, 40, 24, 5, F32, device="cpu")
+
+    def entries(index=(6, 5), teacher=(6, 5), index_type=torch.int64, teacher_type=torch.float32):
+        return (vec(0, index_type, 0, index) if isinstance(index, tuple) else OnGpu(index)), vec(0, teacher_type, 0, teacher)
+
     bad = [
+        lambda: plan.loss(m(6), m(24), *entries(index=(6, 4)), vec(6)), lambda: plan.loss(m(6), m(24), *entries(teacher=(5, 5)), vec(6)),
+        lambda: plan.loss(m(6), m(24), *entries(index_type=torch.int32), vec(6)), lambda: plan.loss(m(6), m(24), *entries(teacher_type=torch.float16), vec(6)),
+        lambda: plan.loss(m(6), m(24), *entries(index=torch.empty((6, 8), dtype=torch.int64)[:, :5]), vec(6)),
+        lambda: plan.loss(m(6), m(24), *entries(index=torch.empty((1, 5), dtype=torch.int64).expand(6, 5)), vec(6)),
+        lambda: plan.loss(m(6), m(24), *entries(index=torch.empty((6, 10), dtype=torch.int64)[:, ::2]), vec(6)),
+        lambda: plan.loss(m(6), m(24), *entries(), vec(5)), lambda: plan.loss(m(6), m(25), *entries(), vec(6)),
+        lambda: psgd.HeadDistill(6, 40, 24, 5, F32, grad=False, device="cpu").loss_grad(m(6), m(24), *entries(), vec(6), m(6), m(24)),
         lambda: psgd.norm(m(6), w, None, m(5)), lambda: psgd.norm(m(6), w, None, m(6, dtype=torch.bfloat16)), lambda: psgd.norm(m(6), vec(39), None, m(6)),
         lambda: psgd.norm(m(6), w, vec(40, torch.bfloat16), m(6)), lambda: psgd.norm(m(6), w, None, m(6), vec(12)), lambda: psgd.norm(m(6), w, None, m(6), add=m(6)),
         lambda: psgd.norm(m(6), w, None, m(6), total=m(6)), lambda: psgd.norm(m(6), w, None, m(6), add=matrix(6, 41), total=m(6)),
