@@ -28,17 +28,22 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 enum HeadKeep { KEEP_NONE = 0, KEEP_F16 = 1, KEEP_F32 = 2 };
 constexpr float kHalfScale = 32768.f;
 
-// A teacher's entries in the place of labels.  Per token of the piece a list of the words that its entries name, ascending, each once.
+// A teacher's entries in the place of labels.  Per token of the piece a list of the words that its entries name, ascending, each once.  The logits kernel
+// looks for them by 8 or 32 tokens (a group) and a range of words (a bucket: a tile's, or several tiles' where there are more than kBuckets): there they lie together, in no order.
 struct HeadTop {
     const int64_t* index;
     const void* teacher;
     int dtype, top;
     int64_t ld;
     // in the workspace
-    int* word;           // [token of the piece][top]
+    int *word, *place;   // [token of the piece][top]: the word, and its place among its group's
     float *q, *log_q;    // the teacher's probability of the word
-    float* logit;        // its logit
-    unsigned short* start;      // [token of the piece][tiles + 1]: the first of the list that is in a tile, and at the end their number
+    unsigned* flat;      // [group][its tokens * top]: word * 32 + token of the group
+    float* logit;        // and its logit
+    int* start;          // [group][buckets + 1]: the first place of each bucket
+    int* words;          // [token of the piece]: how many
+    int buckets, shift;  // word >> shift: its bucket
+    int group;           // tokens of a group
 };
 
 struct HeadDev {
@@ -63,6 +68,7 @@ struct HeadDev {
     int direct;          // X is taken where it is: the tokens of the piece are all tokens
 };
 
+__host__ __device__ constexpr int up4(int x) { return (x + 3) & ~3; }
 __device__ inline bool label_counts(int64_t label, int vocab) { return label >= 0 && label < vocab; }
 // label of token l of the piece from `first` on; -1: it does not count
 __device__ __forceinline__ int label_of(const HeadDev& h, int first, int l) {
@@ -186,6 +192,12 @@ __global__ __launch_bounds__(kGatherThreads) void head_gather_kernel(HeadDev h, 
 
 constexpr int kMaxTop = 1024;
 
+// what the wavefront's lanes have put into LDS, its other lanes find there
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float teacher_logit(const HeadTop& k, int64_t i) {
     return k.dtype == PSGD_F32 ? as_global(static_cast<const float*>(k.teacher))[i] : (float)as_global(static_cast<const bf16_t*>(k.teacher))[i];
 }
@@ -205,127 +217,226 @@ __global__ __launch_bounds__(kThreads) void head_top_count_kernel(HeadTop k, int
     }
 }
 
-// The lists of the piece's tokens, a workgroup each, of up to 256 threads: the entries are sorted by word, those of one word become one with the sum of their
-// probabilities.  `size`: the entries rounded up to a power of two, 64 at least.  write_labels: the tokens have not been looked at before (labels).
-__global__ __launch_bounds__(256) void head_top_lists_kernel(HeadDev h, int first, int size, int64_t* write_labels) {
+// The lists of the piece's tokens, a group to a workgroup, whose wavefronts take a token after another, with up to U entries to a lane.  Entries get
+// their place by the number of smaller ones (word, then place among the token's entries); those of one word become one with the sum of
+// their probabilities.  Then the group's words are counted by bucket, and put there.
+// write_labels: the tokens have not been looked at before (labels).
+// Few tokens: groups of 8, so that more compute units have one (200 tokens of 100 entries: 16.4 us with groups of 32, 8.0 so).
+constexpr int group_tokens(TileShape s) { return s == TILE_256 ? 32 : 8; }
+constexpr int kBuckets = 4096;
+template <int U, int GROUP> constexpr int kListWaves = U > 8 || GROUP < 16 ? 8 : 16;        // (12 bytes of LDS for each entry of a wavefront's token)
+template <int U, int GROUP>
+__global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_kernel(HeadDev h, int first, int rows, int64_t* write_labels) {
+    constexpr int SIZE = 64 * U, WAVES = kListWaves<U, GROUP>, THREADS = 64 * WAVES, EACH = GROUP / WAVES, AHEAD = U > 4 ? 1 : EACH;      // tokens whose loads are sent off first
     extern __shared__ __align__(16) unsigned char smem[];
-    unsigned long long* key = reinterpret_cast<unsigned long long*>(smem);      // [size]: word, place among the entries
-    float* value = reinterpret_cast<float*>(key + size);                        // [size]: the teacher's logits, as they came
-    int* word = reinterpret_cast<int*>(value + size);                           // [size]: the list
-    __shared__ float sums[4];
-    __shared__ int counts[4];
     const HeadTop& k = h.top;
-    const int l = blockIdx.x, threads = blockDim.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, waves = threads >> 6;
-    if (!h.direct && l >= *h.count - first) return;
-    const int64_t token = h.direct ? l : h.rows[first + l];
-    float most = -__builtin_inff();
-    for (int i = threadIdx.x; i < size; i += threads) {
-        const int64_t at = token * k.ld + i;
-        const bool in = i < k.top && entry_counts(k, at, h.vocab);
-        key[i] = in ? (unsigned long long)as_global(k.index)[at] << 10 | (unsigned)i : ~0ull;
-        value[i] = in ? teacher_logit(k, at) : 0.f;
-        if (in) most = fmaxf(most, value[i]);
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    if (lane == 0) sums[wv] = most;
+    const int threads = THREADS, waves = WAVES, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int* count = reinterpret_cast<int*>(smem);                                              // [buckets]
+    unsigned* key = reinterpret_cast<unsigned*>(smem) + up4(k.buckets) + 3 * SIZE * wv;    // [SIZE] of this wavefront: word, place among the entries
+    unsigned* sorted = key + SIZE;                                                          // the same in their order
+    float* z = reinterpret_cast<float*>(key + 2 * SIZE);                                    // logits less the largest, over the temperature
+    __shared__ int sums[16], listed[GROUP];
+    const int group0 = blockIdx.x * GROUP, end = min(rows, h.direct ? rows : *h.count - first);
+    if (group0 >= end) return;
+    for (int b = threadIdx.x; b < k.buckets; b += threads) count[b] = 0;
     __syncthreads();
-    for (int w = 0; w < waves; ++w) most = fmaxf(most, sums[w]);
-    for (int len = 2; len <= size; len <<= 1)
-        for (int step = len >> 1; step > 0; step >>= 1) {
-            for (int i = threadIdx.x; i < size / 2; i += threads) {
-                const int a = 2 * i - (i & (step - 1)), b = a + step;
-                const unsigned long long x = key[a], y = key[b];
-                if ((x > y) == ((a & len) == 0)) key[a] = y, key[b] = x;
+#pragma unroll 1
+    for (int r0 = 0; r0 < EACH; r0 += AHEAD) {
+        int64_t token[AHEAD], y[AHEAD][U];
+        float v[AHEAD][U];
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) {
+            const int l = group0 + wv + (r0 + r) * WAVES;
+            token[r] = l >= end ? -1 : h.direct ? l : h.rows[first + l];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = lane + 64 * u;
+                const bool in = token[r] >= 0 && i < k.top;
+                y[r][u] = in ? as_global(k.index)[token[r] * k.ld + i] : -1;
+                v[r][u] = in ? teacher_logit(k, token[r] * k.ld + i) : 0.f;
             }
-            __syncthreads();
         }
-    // a thread has `each` entries after each other; a word's probability is its first entry's to write
-    const int each = size / threads, from = threadIdx.x * each;
-    float mine = 0.f;
-    int words = 0;
-    for (int i = from; i < from + each; ++i)
-        if (key[i] != ~0ull) {
-            mine += expf((value[key[i] & 1023] - most) * h.inv_t);
-            words += i == 0 || (key[i - 1] >> 10) != (key[i] >> 10);
-        }
-    int up = words;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(up, d);
-        up += lane >= d ? o : 0;
-    }
+        for (int r = 0; r < AHEAD; ++r) {
+            if (token[r] < 0) continue;
+            const int l = group0 + wv + (r0 + r) * WAVES;
+            const int64_t list = (int64_t)l * k.top;
+            float most = -__builtin_inff();
+            int n = 0, rank[U];
+            unsigned mine[U];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
-    if (lane == 63) { counts[wv] = up; sums[wv] = mine; }
-    __syncthreads();
-    float total = 0.f;
-    int to = up - words, n = 0;
-    for (int w = 0; w < waves; ++w) {
-        total += sums[w];
-        to += w < wv ? counts[w] : 0;
-        n += counts[w];
-    }
-    const float log_total = logf(total);
-    const int64_t list = (int64_t)l * k.top;
-    for (int i = from; i < from + each; ++i)
-        if (key[i] != ~0ull && (i == 0 || (key[i - 1] >> 10) != (key[i] >> 10))) {
-            const int y = (int)(key[i] >> 10);
-            const float z = (value[key[i] & 1023] - most) * h.inv_t;
-            float e = expf(z);
-            bool several = false;
-            for (int o = i + 1; o < size && (int64_t)(key[o] >> 10) == y; ++o) {
-                e += expf((value[key[o] & 1023] - most) * h.inv_t);
-                several = true;
+            for (int u = 0; u < U; ++u) {
+                const bool in = label_counts(y[r][u], h.vocab) && v[r][u] != -__builtin_inff();
+                key[lane + 64 * u] = mine[u] = in ? (unsigned)y[r][u] << 10 | (unsigned)(lane + 64 * u) : ~0u;
+                most = in ? fmaxf(most, v[r][u]) : most;
+                n += __popcll(__ballot(in));
+                rank[u] = 0;
             }
-            word[to] = y;
-            as_global(k.word)[list + to] = y;
-            as_global(k.q)[list + to] = e / total;
-            as_global(k.log_q)[list + to] = (several ? logf(e) : z) - log_total;
-            ++to;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+            wave_sync();
+#pragma unroll 2
+            for (int j = 0; j < k.top; j += 4) {
+                const uintx4 other = *reinterpret_cast<const uintx4*>(key + j);
+#pragma unroll
+                for (int o = 0; o < 4; ++o)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) rank[u] += other[o] < mine[u] ? 1 : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (rank[u] < n) {          // (what does not count is behind all that does)
+                    sorted[rank[u]] = mine[u];
+                    z[rank[u]] = (v[r][u] - most) * h.inv_t;
+                }
+            wave_sync();
+            float total = 0.f;
+            for (int i = lane; i < n; i += 64) total += expf(z[i]);
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+            const float log_total = logf(total);
+            int to = 0;
+            for (int i0 = 0; i0 < n; i0 += 64) {
+                const int i = i0 + lane;
+                const unsigned word = i < n ? sorted[i] >> 10 : 0u;
+                const bool leads = i < n && (i == 0 || sorted[i - 1] >> 10 != word);
+                const unsigned long long leaders = __ballot(leads);
+                if (leads) {
+                    float e = expf(z[i]), log_e = z[i];
+                    int o = i + 1;
+                    for (; o < n && sorted[o] >> 10 == word; ++o) e += expf(z[o]);
+                    if (o > i + 1) log_e = logf(e);
+                    const int64_t at = list + to + __popcll(leaders & ((1ull << lane) - 1));
+                    as_global(k.word)[at] = (int)word;
+                    as_global(k.q)[at] = e / total;
+                    as_global(k.log_q)[at] = log_e - log_total;
+                    atomicAdd(&count[word >> k.shift], 1);
+                }
+                to += __popcll(leaders);
+            }
+            if (lane == 0) {
+                listed[l - group0] = to;
+                as_global(k.words)[l] = to;
+                if (write_labels) as_global(write_labels)[token[r]] = to > 0 ? 0 : -1;
+            }
+            wave_sync();
         }
-    __syncthreads();
-    for (int tile = threadIdx.x; tile <= h.tiles; tile += threads) {
-        const int64_t bound = (int64_t)tile * h.tile_width;
-        int low = 0, high = n;
-        while (low < high) {
-            const int mid = (low + high) >> 1;
-            if (word[mid] < bound) low = mid + 1; else high = mid;
-        }
-        as_global(k.start)[(int64_t)l * (h.tiles + 1) + tile] = (unsigned short)low;
     }
-    if (write_labels && threadIdx.x == 0) as_global(write_labels)[token] = n > 0 ? 0 : -1;
+    __syncthreads();
+    // first places of the buckets
+    PSGD_GLOBAL int* start = as_global(k.start) + (int64_t)blockIdx.x * (k.buckets + 1);
+    int before = 0;
+    for (int b0 = 0; b0 < k.buckets; b0 += threads) {
+        const int b = b0 + threadIdx.x, mine = b < k.buckets ? count[b] : 0;
+        int up = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(up, d);
+            up += lane >= d ? o : 0;
+        }
+        if (lane == 63) sums[wv] = up;
+        __syncthreads();
+        int at = before + up - mine;
+        for (int w = 0; w < waves; ++w) {
+            at += w < wv ? sums[w] : 0;
+            before += sums[w];
+        }
+        if (b < k.buckets) { count[b] = at; start[b] = at; }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) start[k.buckets] = before;
+    const int64_t base = (int64_t)group0 * k.top;
+    for (int l = group0 + wv; l < min(group0 + GROUP, end); l += waves) {
+        const int n = listed[l - group0];
+        for (int i = lane; i < n; i += 64) {
+            const int64_t at = (int64_t)l * k.top + i;
+            const int y = as_global(k.word)[at], place = atomicAdd(&count[y >> k.shift], 1);
+            as_global(k.flat)[base + place] = (unsigned)y << 5 | (unsigned)(l - group0);
+            as_global(k.place)[at] = place;
+        }
+    }
 }
 
 // ---- logits of a piece: statistics per tile, exponentials --------------------------------------------------------------
 
-// The logits of the teacher's words in this tile: to their lists, and out of the accumulators.  A lane seeks the word among its own columns.
-template <class T>
-__device__ __forceinline__ void take_listed(T& tile, const HeadDev& h, int p0, int l0, int nl, int at_p) {
+// The logits of the teacher's words in this tile: to their places, and out of the accumulators (minus infinity there).  32 rows at a time, through LDS, where any lane can
+// look for any word, each wavefront in a place of its own.  (8192 x 4096 x 64000, 64 entries: 40 us of 3430 more than without a teacher; one word of a row after the
+// other, sought among a lane's accumulators, took 365.  200 x 1024 x 10007, 100 entries, a quarter of them in one tile: 5 us of 23; 30 of 48.)
+// Where they are is asked before the product.
+template <class T, TileShape SHAPE> struct TileListed {
+    static constexpr int GROUP = group_tokens(SHAPE), SUBS = 32 / GROUP;
+    int from[T::FL][SUBS], to[T::FL][SUBS];
+};
+template <class T, TileShape SHAPE>
+__device__ __forceinline__ void where_listed(TileListed<T, SHAPE>& w, const HeadTop& k, int p0, int l0, int nl) {
+    constexpr int GROUP = group_tokens(SHAPE);
+    const int wl = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / T::WP;
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j)
+#pragma unroll
+        for (int s = 0; s < 32 / GROUP; ++s) {
+            const int row0 = l0 + (wl * T::FL + j) * 32 + s * GROUP;
+            const PSGD_GLOBAL int* start = as_global(k.start) + (int64_t)(row0 / GROUP) * (k.buckets + 1) + (p0 >> k.shift);
+            w.from[j][s] = row0 < nl ? start[0] : 0, w.to[j][s] = row0 < nl ? start[1] : 0;
+        }
+}
+template <class T, TileShape SHAPE>
+__device__ __forceinline__ void take_listed(T& tile, const HeadTop& k, const TileListed<T, SHAPE>& w, int p0, int l0, PSGD_TLDS unsigned char* lds) {
+    constexpr int COLS = 32 * T::FP, LD = COLS + 4, GROUP = group_tokens(SHAPE), SUBS = 32 / GROUP, AHEAD = 4;
+    const int lane = tile.lane;
+    auto base = [&](int j, int s) { return (int64_t)(l0 + (tile.wl * T::FL + j) * 32 + s * GROUP) * k.top; };
+    unsigned first[T::FL][SUBS];
+#pragma unroll
+    for (int j = 0; j < T::FL; ++j)
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) first[j][s] = w.from[j][s] + lane < w.to[j][s] ? as_global(k.flat)[base(j, s) + w.from[j][s] + lane] : 0u;
+    __syncthreads();        // (the chunks' reads are done)
+    PSGD_TLDS float* mine = reinterpret_cast<PSGD_TLDS float*>(lds) + (tile.wl * T::WP + tile.wp) * 32 * LD;
 #pragma unroll
     for (int j = 0; j < T::FL; ++j) {
-        const int l = l0 + tile.row(j);
-        int e = 0, end = 0;
-        if (l < nl) {
-            const PSGD_GLOBAL unsigned short* start = as_global(h.top.start) + (int64_t)l * (h.tiles + 1) + at_p;
-            e = start[0], end = start[1];
-        }
-        const int64_t list = (int64_t)l * h.top.top;
-        for (; __any(e < end); ++e) {
-            const int y = e < end ? as_global(h.top.word)[list + e] - p0 - tile.col(0, 0) : -1;
-            const bool found = y >= 0 && y < 32 * T::FP && (y & 4) == 0;
-            if (!__any(found)) continue;
-            float x = 0.f;
+        int n = 0;
 #pragma unroll
-            for (int i = 0; i < T::FP; ++i)
+        for (int s = 0; s < SUBS; ++s) n += w.to[j][s] - w.from[j][s];
+        if (n == 0) continue;
+        PSGD_TLDS float* own = mine + (lane & 31) * LD + 4 * (lane >> 5);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const bool here = y == 32 * i + 8 * (v >> 2) + (v & 3);
-                    x = here ? tile.acc[i][j][v] : x;
-                    tile.acc[i][j][v] = here ? -__builtin_inff() : tile.acc[i][j][v];
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<PSGD_TLDS floatx4*>(own + 32 * i + 8 * q) =
+                    floatx4{tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1], tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3]};
+        wave_sync();
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int64_t at = base(j, s);
+            const int to = w.to[j][s];
+            auto take = [&](int i, unsigned e) {
+                const int col = (int)(e >> 5) - p0 - tile.wp * COLS;
+                if (i < to && col >= 0 && col < COLS) {
+                    PSGD_TLDS float* x = mine + (s * GROUP + (e & 31)) * LD + col;
+                    as_global(k.logit)[at + i] = *x;
+                    *x = -__builtin_inff();
                 }
-            if (found) as_global(h.top.logit)[list + e] = x;
+            };
+            take(w.from[j][s] + lane, first[j][s]);
+            for (int i0 = w.from[j][s] + 64; i0 < to; i0 += 64 * AHEAD) {
+                unsigned e[AHEAD];
+#pragma unroll
+                for (int r = 0; r < AHEAD; ++r) e[r] = i0 + 64 * r + lane < to ? as_global(k.flat)[at + i0 + 64 * r + lane] : 0u;
+#pragma unroll
+                for (int r = 0; r < AHEAD; ++r) take(i0 + 64 * r + lane, e[r]);
+            }
         }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < T::FP; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const floatx4 x = *reinterpret_cast<const PSGD_TLDS floatx4*>(own + 32 * i + 8 * q);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) tile.acc[i][j][4 * q + u] = x[u];
+            }
+        wave_sync();
     }
 }
 
@@ -340,8 +451,10 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
     if (at.split < 0) return;
     const int p0 = at.p * T::BP, l0 = at.l * BL;
     T tile;
+    TileListed<T, SHAPE> listed;
+    if constexpr (TOP) where_listed(listed, h.top, p0, l0, nl);
     tile.template run<true>(t, p0, l0, nl, t.K, 0, 1, (PSGD_TLDS unsigned char*)smem);
-    if constexpr (TOP) take_listed(tile, h, p0, l0, nl, at.p);
+    if constexpr (TOP) take_listed(tile, h.top, listed, p0, l0, (PSGD_TLDS unsigned char*)smem);
     const float log2e = TOP ? 1.4426950408889634f * h.inv_t : 1.4426950408889634f;
     // the wave's maximum per row, over its columns; a tile has at least one column
     float* red = reinterpret_cast<float*>(smem);        // [WP][BL]
@@ -427,14 +540,14 @@ __global__ __launch_bounds__(kTileThreads, tile_share(SHAPE)) void head_logits_k
 
 // ---- the row's sum, the loss, and D ------------------------------------------------------------------------------------
 
-// Largest logit of row l and the sum of exp(logit - it) (over the temperature) over all columns but the label's or the list's, by all threads of the block
+// Largest logit of row l and the sum of exp(logit - it) over all columns but the label's, by all threads of the block
 struct RowSum { float most, others; };
 __device__ __forceinline__ RowSum row_sum(const HeadDev& h, int l, float* shared) {
     const float2* st = h.stats + (int64_t)l * h.tiles;
     float m = -__builtin_inff(), s = 0.f;
     auto join = [&](float mo, float so) {
         const float n = fmaxf(m, mo);
-        if (n != -__builtin_inff()) s = s * expf((m - n) * h.inv_t) + so * expf((mo - n) * h.inv_t);
+        if (n != -__builtin_inff()) s = s * expf(m - n) + so * expf(mo - n);
         else s += so;
         m = n;
     };
@@ -557,10 +670,11 @@ __device__ __forceinline__ float exp_rest(float u) {
 // of whose terms none is negative;  D = c (p - q), p - q = q (e^u - 1).  The others' D comes of their exponentials, the list's is written over it.
 template <int KEEP, int PL>
 __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int first, int most_rows, int span) {
-    __shared__ float shared[8];
-    const int l = blockIdx.x;
+    __shared__ float shared[4];
+    const HeadTop& k = h.top;
+    const int l = blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     if (l >= (h.direct ? most_rows : min(most_rows, *h.count - first))) return;
-    const int token = h.direct ? first + l : h.rows[first + l], n = h.top.start[(int64_t)l * (h.tiles + 1) + h.tiles];
+    const int token = h.direct ? first + l : h.rows[first + l], n = as_global(k.words)[l];
     const int begin = blockIdx.y * span, end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
     float scale = 1.f;
     if (KEEP != KEEP_NONE && h.direct && (h.weight || (l == 0 && blockIdx.y == 0))) {
@@ -573,7 +687,7 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
         if constexpr (KEEP != KEEP_NONE)
             for (int v = begin + 8 * threadIdx.x; v < end; v += 8 * kThreads)
 #pragma unroll
-                for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL uintx4*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = uintx4{0u, 0u, 0u, 0u};
+                for (int p = 0; p < PL; ++p) *reinterpret_cast<PSGD_GLOBAL uintx4*>(as_global(h.D) + p * h.d_plane + l * h.ldv + v) = uintx4{0u, 0u, 0u, 0u};
         return;
     }
     uintx4 e[KEEP == KEEP_F32 ? 2 : 1];
@@ -587,85 +701,104 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
     };
     const int start = begin + 8 * threadIdx.x;
     if (KEEP != KEEP_NONE && start < end) fetch(start);
-    const RowSum r = row_sum(h, l, shared);
-    // the list's own maximum and sum, and then the row's
-    const int64_t list = (int64_t)l * h.top.top;
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    auto all = [&](float x, auto join) {        // of all threads
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) x = join(x, __shfl_xor(x, d));
-        __syncthreads();
-        if (lane == 0) shared[wv] = x;
-        __syncthreads();
-        x = shared[0];
-#pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) x = join(x, shared[w]);
-        return x;
-    };
-    auto larger = [](float a, float b) { return fmaxf(a, b); };
-    auto plus = [](float a, float b) { return a + b; };
-    float most = r.most;
-    for (int i = threadIdx.x; i < n; i += kThreads) most = fmaxf(most, h.top.logit[list + i]);
-    most = all(most, larger);
-    float sum = 0.f;
-    for (int i = threadIdx.x; i < n; i += kThreads) sum += expf((h.top.logit[list + i] - most) * h.inv_t);
-    const float others = r.others == 0.f ? 0.f : r.others * expf((r.most - most) * h.inv_t), total = all(sum, plus) + others;
-    const float log_total = logf(total);
-    struct Word { float p, q, u; bool small; };
-    auto listed = [&](int i) {
-        Word w;
-        const float z = (h.top.logit[list + i] - most) * h.inv_t;
-        w.q = h.top.q[list + i];
-        w.p = expf(z) / total;
-        w.u = z - log_total - h.top.log_q[list + i];
-        w.small = fabsf(w.u) <= kSmallU;
+    // (Each wavefront does all this for itself, for the list is short, and the statistics come from the caches: no wavefront waits for another's.)
+    struct Word { float logit, q, log_q; int word; };
+    const int64_t base = (int64_t)(l / k.group) * k.group * k.top;
+    auto load_word = [&](int i) {
+        Word w = {-__builtin_inff(), 0.f, 0.f, -1};
+        const int64_t at = (int64_t)l * k.top + i;
+        if (i < n) w = {as_global(k.logit)[base + as_global(k.place)[at]], as_global(k.q)[at], as_global(k.log_q)[at], as_global(k.word)[at]};
         return w;
     };
-    if (blockIdx.y == 0) {
-        float loss = 0.f;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const Word w = listed(i);
-            // (a probability that is 0 in 32 bits has a logarithm all the same, or none)
-            loss += w.small ? w.q * exp_rest(w.u) : w.q == 0.f ? w.p : w.p - w.q - w.q * w.u;
+    const Word w0 = load_word(lane);
+    // the largest logit, and the sums of exp(logit - it) of the list and of the others
+    const float inv_t = h.inv_t;
+    float most = -__builtin_inff(), mine = 0.f, others = 0.f;
+    auto join = [&](float m, float s, float o) {
+        const float both = fmaxf(most, m);
+        if (both != -__builtin_inff()) {
+            const float f = expf((most - both) * inv_t), g = expf((m - both) * inv_t);
+            mine = mine * f + s * g, others = others * f + o * g;
+        } else {
+            mine += s, others += o;
         }
-        loss = all(loss, plus);
-        if (threadIdx.x == 0) h.loss[token] = loss + others / total;
+        most = both;
+    };
+    const float2* st = h.stats + (int64_t)l * h.tiles;
+    for (int i = lane; i < h.tiles; i += 64) join(st[i].x, 0.f, st[i].y);
+    if (w0.word >= 0) join(w0.logit, 1.f, 0.f);
+    for (int i = lane + 64; i < n; i += 64) join(load_word(i).logit, 1.f, 0.f);
+    const float lane_most = most;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if (lane_most != most) {
+        const float f = expf((lane_most - most) * inv_t);
+        mine *= f, others *= f;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d), others += __shfl_xor(others, d);
+    const float total = mine + others, log_total = logf(total), weight = h.weight ? h.weight[token] / (h.direct ? scale : h.scale[1]) : 1.f;
+    struct Off { float p, u; bool small; };
+    auto off = [&](const Word& w) {
+        const float z = (w.logit - most) * inv_t, u = z - log_total - w.log_q;
+        return Off{expf(z) / total, u, fabsf(u) <= kSmallU};
+    };
+    if (blockIdx.y == 0 && wv == 0) {
+        float loss = 0.f;
+        for (int i = lane; i < n; i += 64) {
+            const Word w = i < 64 ? w0 : load_word(i);
+            const Off o = off(w);
+            // (a probability that is 0 in 32 bits has a logarithm all the same, or none)
+            loss += o.small ? w.q * exp_rest(o.u) : w.q == 0.f ? o.p : o.p - w.q - w.q * o.u;
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+        if (lane == 0) h.loss[token] = loss + others / total;
     }
     if constexpr (KEEP == KEEP_NONE) return;
-    const float weight = h.weight ? h.weight[token] / (h.direct ? scale : h.scale[1]) : 1.f, c = weight / total;
-    for (int v = start; v < end; v += 8 * kThreads) {
-        const float in_tile = h.stats[(int64_t)l * h.tiles + v / h.tile_width].x;
-        const float f = expf((in_tile - most) * h.inv_t) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
-        float x[8];
-        if constexpr (KEEP == KEEP_F16) {
-            const halfx8 q = __builtin_bit_cast(halfx8, e[0]);
+    // a word's D, of all its planes
+    auto put = [&](const Word& w) {
+        const Off o = off(w);
+        bf16_t plane[PL];
+        split_planes<PL>((o.small ? w.q * (o.u + exp_rest(o.u)) : o.p - w.q) * weight, plane);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = (float)q[u] * f;
-        } else {
+        for (int p = 0; p < PL; ++p) as_global(h.D)[p * h.d_plane + l * h.ldv + w.word] = plane[p];
+    };
+    const float c = weight / total;
+    for (int v0 = begin + 512 * wv; v0 < end; v0 += 8 * kThreads) {
+        const int v = v0 + 8 * lane;
+        if (v < end) {
+            const float f = expf((st[v / h.tile_width].x - most) * inv_t) * c * (KEEP == KEEP_F16 ? 1.f / kHalfScale : 1.f);
+            float x[8];
+            if constexpr (KEEP == KEEP_F16) {
+                const halfx8 y = __builtin_bit_cast(halfx8, e[0]);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = __uint_as_float(e[KEEP == KEEP_F32 ? u >> 2 : 0][u & 3]) * f;
+                for (int u = 0; u < 8; ++u) x[u] = (float)y[u] * f;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = __uint_as_float(e[KEEP == KEEP_F32 ? u >> 2 : 0][u & 3]) * f;
+            }
+            if (v + 8 * kThreads < end) fetch(v + 8 * kThreads);
+            bf16x8 out[PL];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                bf16_t plane[PL];
+                split_planes<PL>(x[u], plane);
+#pragma unroll
+                for (int p = 0; p < PL; ++p) out[p][u] = plane[p];
+            }
+#pragma unroll
+            for (int p = 0; p < PL; ++p) *reinterpret_cast<PSGD_GLOBAL bf16x8*>(as_global(h.D) + p * h.d_plane + l * h.ldv + v) = out[p];
         }
-        if (v + 8 * kThreads < end) fetch(v + 8 * kThreads);
-        bf16x8 out[PL];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            bf16_t q[PL];
-            split_planes<PL>(x[u], q);
-#pragma unroll
-            for (int k = 0; k < PL; ++k) out[k][u] = q[k];
-        }
-#pragma unroll
-        for (int k = 0; k < PL; ++k) *reinterpret_cast<PSGD_GLOBAL bf16x8*>(as_global(h.D) + k * h.d_plane + l * h.ldv + v) = out[k];
+        // the list's, as soon as their places are written (later, they would be parts of lines that have left the caches), by the same wavefront: its stores
+        // come in their order
+        wave_sync();
+        if (w0.word >= v0 && w0.word < min(v0 + 512, end)) put(w0);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int v = h.top.word[list + i];
-        if (v < begin || v >= end) continue;
-        const Word w = listed(i);
-        bf16_t q[PL];
-        split_planes<PL>((w.small ? w.q * (w.u + exp_rest(w.u)) : w.p - w.q) * weight, q);
-#pragma unroll
-        for (int k = 0; k < PL; ++k) as_global(h.D)[k * h.d_plane + l * h.ldv + v] = q[k];
+    wave_sync();
+    for (int i = lane + 64; i < n; i += 64) {
+        const Word w = load_word(i);
+        if (w.word >= begin && w.word < end && ((w.word - begin) / 512) % (kThreads / 64) == wv) put(w);
     }
 }
 
@@ -696,13 +829,14 @@ constexpr int64_t kMaxPiece = (int64_t)1 << 23, kMaxPieceLogits = (int64_t)1 << 
 struct HeadPlan {
     size_t bytes = 0;
     size_t count, scale, rows, label, counts, xc, wc, stats, at_label, e, D, part, dw_part, sum;
-    size_t entries, word, q, log_q, logit, start;        // of a teacher
+    size_t entries, word, place, q, log_q, flat, logit, start, words;        // of a teacher
     int64_t ldc, ldv;
     int piece, pieces, tiles, x_planes, d_planes, keep;
     TilePlan logits, dx, dw;
     unsigned dw_pairs;
     int n_dw_pairs;
     bool copy_w, direct, pair;
+    int shift, buckets, group;     // of a teacher's words
 };
 
 // top: entries of a teacher per token, 0 with labels
@@ -721,7 +855,7 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients, int64_t top) 
     // tokens per piece (statistics: 8 bytes for each tile of 128 words; tiles of 64 are not taken for so many tokens, but where all words are in one)
     const int64_t tokens = std::max<int64_t>(1, s.tokens);
     const size_t row = (!gradients ? s.vocab / 128 * sizeof(float2) + 64 : (size_t)p.ldv * (p.keep == KEEP_F16 ? 2 : 4 + 2 * p.d_planes)) +
-                       (top ? 16 * top + s.vocab / 128 * 2 + 8 : 0);
+                       (top ? 24 * top + s.vocab / 256 + 8 : 0);
     const int64_t launch = std::min(kMaxPiece, std::max<int64_t>(1, kMaxPieceLogits / s.vocab));
     const int64_t most = std::min(std::min(tokens, launch), s.piece_tokens > 0 ? s.piece_tokens : std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256));
     p.pieces = (int)((tokens + most - 1) / most);
@@ -745,9 +879,14 @@ static HeadPlan head_plan(const psgd_head_desc& s, bool gradients, int64_t top) 
     p.stats = take((size_t)p.piece * p.tiles * sizeof(float2));
     if (top) {
         p.entries = take((size_t)tokens * 8);
-        p.word = take((size_t)p.piece * top * 4), p.q = take((size_t)p.piece * top * 4), p.log_q = take((size_t)p.piece * top * 4);
-        p.logit = take((size_t)p.piece * top * 4);
-        p.start = take((size_t)p.piece * (p.tiles + 1) * 2);
+        p.group = group_tokens(p.logits.shape);
+        const size_t groups = (p.piece + p.group - 1) / p.group, list = groups * p.group * top * 4;
+        p.word = take(list), p.place = take(list), p.q = take(list), p.log_q = take(list), p.flat = take(list), p.logit = take(list);
+        for (int width = tile_p(p.logits.shape); width > 1; width /= 2) ++p.shift;
+        while (((s.vocab - 1) >> p.shift) >= kBuckets) ++p.shift;
+        p.buckets = (int)((s.vocab - 1) >> p.shift) + 1;
+        p.start = take(groups * (p.buckets + 1) * 4);
+        p.words = take((size_t)p.piece * 4);
     } else {
         p.at_label = take((size_t)p.piece * 4);
     }
@@ -837,11 +976,26 @@ struct HeadTeacher {
 };
 static int teacher_shape(int64_t top) { return top < 1 || top > kMaxTop ? PSGD_E_SHAPE : PSGD_OK; }
 
-static hipError_t launch_lists(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
-    int size = 64;
-    while (size < h.top.top) size *= 2;
-    hipLaunchKernelGGL(head_top_lists_kernel, dim3(rows), dim3(std::min(size, 256)), (size_t)size * 16, st, h, first, size, write_labels);
+template <int U, int GROUP>
+static hipError_t launch_lists_as(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
+    auto kfn = head_top_lists_kernel<U, GROUP>;
+    constexpr int waves = kListWaves<U, GROUP>;
+    const int lds = up4(h.top.buckets) * 4 + waves * U * 64 * 12;
+    if (lds > 48 * 1024) {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kfn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kfn, dim3((rows + GROUP - 1) / GROUP), dim3(64 * waves), lds, st, h, first, rows, write_labels);
     return hipGetLastError();
+}
+template <int U>
+static hipError_t launch_lists_for(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
+    return h.top.group == 32 ? launch_lists_as<U, 32>(h, first, rows, write_labels, st) : launch_lists_as<U, 8>(h, first, rows, write_labels, st);
+}
+static hipError_t launch_lists(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
+    const int top = h.top.top;
+    return top <= 64 ? launch_lists_for<1>(h, first, rows, write_labels, st) : top <= 128 ? launch_lists_for<2>(h, first, rows, write_labels, st)
+         : top <= 256 ? launch_lists_for<4>(h, first, rows, write_labels, st) : launch_lists_for<16>(h, first, rows, write_labels, st);
 }
 
 static int head_run(const psgd_head_desc* s, const HeadTeacher* teacher, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,
@@ -883,8 +1037,12 @@ static int head_run(const psgd_head_desc* s, const HeadTeacher* teacher, bool gr
     h.inv_t = 1.f;
     if (teacher) {
         h.inv_t = 1.f / teacher->temperature;
-        h.top = {teacher->index, teacher->logits, teacher->dtype, (int)top, teacher->ld, reinterpret_cast<int*>(ws + p.word), reinterpret_cast<float*>(ws + p.q),
-                 reinterpret_cast<float*>(ws + p.log_q), reinterpret_cast<float*>(ws + p.logit), reinterpret_cast<unsigned short*>(ws + p.start)};
+        h.top = {teacher->index, teacher->logits, teacher->dtype, (int)top, teacher->ld};
+        h.top.word = reinterpret_cast<int*>(ws + p.word), h.top.place = reinterpret_cast<int*>(ws + p.place);
+        h.top.q = reinterpret_cast<float*>(ws + p.q), h.top.log_q = reinterpret_cast<float*>(ws + p.log_q);
+        h.top.flat = reinterpret_cast<unsigned*>(ws + p.flat), h.top.logit = reinterpret_cast<float*>(ws + p.logit);
+        h.top.start = reinterpret_cast<int*>(ws + p.start), h.top.words = reinterpret_cast<int*>(ws + p.words);
+        h.top.buckets = p.buckets, h.top.shift = p.shift, h.top.group = p.group;
     }
     h.tokens = (int)s->tokens, h.d = (int)s->d, h.vocab = (int)s->vocab;
     h.count = reinterpret_cast<int*>(ws + p.count);
