@@ -4,7 +4,7 @@
 //   u = (s - mean) r,  y = u w + b
 //   g = dy w,  ds = r (g - sum_c g / n - u sum_c(g u) / n) (+ the gradient that comes past the norm),  dw = sum_rows dy u,  db = sum_rows dy
 //
-// A row is in the registers of one wavefront, of four or of sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
+// A row is in the registers of one wavefront or of four to sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
 // first mean is subtracted, and corrected by what is left of the mean in that: a row far from zero loses nothing to it.
 //
 // Backward, a workgroup goes through rows that are the grid apart and keeps its columns' sums of dy u and dy in registers, in fp32; it
@@ -43,6 +43,10 @@ struct NormGradDev {
     const floatx2* stats;
     float* part;                    // nullable; [workgroup][2][ldp]: sums of dy u and of dy
     int64_t ldp;
+    // where the rows are few: workgroups from `row_blocks` on add up columns
+    int row_blocks;
+    void *dw, *db;
+    int g_dtype, accumulate;
 };
 
 // N columns of a vector that ends at `cols`; `otherwise` where there is no vector, zeros beyond cols
@@ -81,7 +85,7 @@ __device__ __forceinline__ void load_param(const NormParam& p, int col, int cols
 }
 
 // Threads of a workgroup: WAVES to a row, and where that is one, four rows at a time.
-template <int WAVES> constexpr int kNormThreads = WAVES == 16 ? 1024 : 256;
+template <int WAVES> constexpr int kNormThreads = WAVES == 1 ? 256 : 64 * WAVES;
 template <int WAVES> constexpr int kNormRows = WAVES == 1 ? 4 : 1;
 
 // sums over a row's lanes; `shared`: two sets of [K][WAVES], used in turn, so that one barrier is enough
@@ -127,19 +131,24 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
         load_param<N>(a.w, col, a.cols, 1.f, w[i]);
         load_param<N>(a.b, col, a.cols, 0.f, b[i]);
     }
-    for (int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group; row < a.rows; row += (int64_t)gridDim.x * kNormRows<WAVES>) {
-        uintx4 raw[PIECES], raw_add[PIECES];
-        ActPlace p[PIECES];
-        float v[PIECES][N];
+    const int64_t step = (int64_t)gridDim.x * kNormRows<WAVES>;
+    uintx4 raw[PIECES], raw_add[PIECES];
+    ActPlace p[PIECES];
+    auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
             raw[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_in, p[i]);
             if constexpr (ADD) raw_add[i] = load_raw<STREAM>(static_cast<const T*>(a.add), a.ld_in, p[i]);
         }
-        float sum[1] = {0.f};
+    };
+    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group;
+    if (row < a.rows) fetch(row);
+    for (; row < a.rows; row += step) {
+        float v[PIECES][N], sum[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
+            p[i].row = row;
             clear_beyond<T>(raw[i], p[i], a.cols);
             widen<T>(raw[i], v[i]);
             if constexpr (ADD) {
@@ -153,6 +162,9 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
 #pragma unroll
             for (int u = 0; u < N; ++u) sum[0] += v[i][u];
         }
+        if (row + step < a.rows) fetch(row + step);     // (the next row is on its way while this one is added up)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) p[i].row = row;
         row_sums<WAVES>(sum, shared, turn);
         const float first = rounded_product(sum[0], inv_n);
         float rest[2] = {0.f, 0.f};
@@ -184,9 +196,66 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
     }
 }
 
+__device__ __forceinline__ void put_sum(void* out, int dtype, int accumulate, int c, float s) {
+    if (dtype == PSGD_F32) {
+        PSGD_GLOBAL float* to = as_global(static_cast<float*>(out)) + c;
+        *to = accumulate ? *to + s : s;
+    } else {
+        PSGD_GLOBAL bf16_t* to = as_global(static_cast<bf16_t*>(out)) + c;
+        *to = (bf16_t)(accumulate ? (float)*to + s : s);
+    }
+}
+
+// dw and db of four pieces of columns, all rows: a lane has a piece of every 16th row of its wavefront's
+template <class T, int THREADS>
+__device__ __forceinline__ void norm_columns(const NormGradDev& a, int block) {
+    constexpr int N = kPiece<T>, W = THREADS / 64;
+    __shared__ float joined[W][4][2 * N];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    ActPlace p;
+    p.col = N * (4 * block + (lane & 3)), p.in = p.col < a.cols;
+    float s[2 * N];
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) s[k] = 0.f;
+#pragma unroll 4
+    for (int row = 16 * wv + (lane >> 2); row < (int)a.rows; row += 16 * W) {
+        p.row = row;
+        const uintx4 raw_x = load_raw<false>(static_cast<const T*>(a.x), a.ld_x, p), raw_dy = load_raw<false>(static_cast<const T*>(a.dy), a.ld_dy, p);
+        const floatx2 st = as_global(a.stats)[row];
+        float u[N], g[N];
+        widen<T>(raw_x, u);
+        widen<T>(raw_dy, g);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            s[k] = fmaf(g[k], (u[k] - st[0]) * st[1], s[k]);
+            s[N + k] += g[k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) {
+#pragma unroll
+        for (int d = 32; d >= 4; d >>= 1) s[k] += __shfl_xor(s[k], d);
+        if (lane < 4) joined[wv][lane][k] = s[k];
+    }
+    __syncthreads();
+    if (threadIdx.x < 8 * N) {
+        const int piece = threadIdx.x & 3, k = threadIdx.x >> 2, c = N * (4 * block + piece) + (k < N ? k : k - N);
+        float sum = joined[0][piece][k];
+#pragma unroll
+        for (int w = 1; w < W; ++w) sum += joined[w][piece][k];
+        void* out = k < N ? a.dw : a.db;
+        if (out && c < a.cols) put_sum(out, a.g_dtype, a.accumulate, c, sum);
+    }
+}
+
 template <class T, int WAVES, int PIECES, bool PAST, bool STREAM>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(NormGradDev a) {
     constexpr int N = kPiece<T>;
+    if constexpr (!STREAM)
+        if ((int)blockIdx.x >= a.row_blocks) {
+            norm_columns<T, kNormThreads<WAVES>>(a, blockIdx.x - a.row_blocks);
+            return;
+        }
     __shared__ float shared[4 * WAVES];
     int turn = 0;
     const int at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, group = WAVES == 1 ? threadIdx.x >> 6 : 0;
@@ -198,9 +267,11 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
 #pragma unroll
         for (int u = 0; u < N; ++u) dw[i][u] = db[i][u] = 0.f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group; row < a.rows; row += (int64_t)gridDim.x * kNormRows<WAVES>) {
-        uintx4 raw_x[PIECES], raw_dy[PIECES], raw_past[PIECES];
-        ActPlace p[PIECES];
+    const int64_t step = (int64_t)a.row_blocks * kNormRows<WAVES>;
+    uintx4 raw_x[PIECES], raw_dy[PIECES], raw_past[PIECES];
+    floatx2 stats = {0.f, 0.f};
+    ActPlace p[PIECES];
+    auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
@@ -208,7 +279,13 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
             raw_dy[i] = load_raw<STREAM>(static_cast<const T*>(a.dy), a.ld_dy, p[i]);
             if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_dx, p[i]);
         }
-        const floatx2 st = as_global(a.stats)[row];
+        stats = as_global(a.stats)[row];
+    };
+    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group;
+    if (row < a.rows) fetch(row);
+    for (; row < a.rows; row += step) {
+        const floatx2 st = stats;
+        uintx4 past[PIECES];
         float u[PIECES][N], g[PIECES][N], sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -227,12 +304,16 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
                 sums[1] = fmaf(g[i][k], u[i][k], sums[1]);
             }
         }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) past[i] = raw_past[i];
+        if (row + step < a.rows) fetch(row + step);     // (the next row is on its way while this one is added up)
         row_sums<WAVES>(sums, shared, turn);
         const float c1 = sums[0] * inv_n, c2 = sums[1] * inv_n;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             float o[N];
-            if constexpr (PAST) widen<T>(raw_past[i], o);
+            p[i].row = row;
+            if constexpr (PAST) widen<T>(past[i], o);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const float d = st.y * (g[i][k] - fmaf(u[i][k], c2, c1));
@@ -291,35 +372,36 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int64
     if (slice == 0 && c < cols) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) s += shared[i][threadIdx.x];
-        if (dtype == PSGD_F32) {
-            PSGD_GLOBAL float* to = as_global(static_cast<float*>(out)) + c;
-            *to = accumulate ? *to + s : s;
-        } else {
-            PSGD_GLOBAL bf16_t* to = as_global(static_cast<bf16_t*>(out)) + c;
-            *to = (bf16_t)(accumulate ? (float)*to + s : s);
-        }
+        put_sum(out, dtype, accumulate, c, s);
     }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
 
-// wavefronts to a row and pieces to a lane: as few of the former as have the row in four pieces each (in two of several wavefronts)
+// Wavefronts to a row and pieces to a lane.  One wavefront needs no barrier, and has a row of up to four pieces to a lane; wider rows have four wavefronts
+// or eight with as few pieces as do (16384 x 4096 with addend, in us, of (4, 2), (8, 1), (2, 4), each with its best grid: forward 90.0, 90.7, 92.9, backward 95.8, 90.8,
+// 98.9; 8192 x 8192 of (4, 4), (8, 2), (16, 1): 93.8, 91.2, 106.4, 96.2, 93.3, 93.2; 8192 x 11008 without one of (8, 3), (16, 2): 65.9, 95.4, 99.0, 167;
+// 16384 x 2048 of (1, 4), (2, 2), (4, 1): 46.2, 46.6, 47.2, 54.0, 54.7, 52.2).
 struct NormShape { int waves, pieces; };
-static NormShape norm_variant(int64_t cols, int dtype) {
-    const int64_t n = (cols + (dtype == PSGD_F32 ? 3 : 7)) / (dtype == PSGD_F32 ? 4 : 8);
-    if (n <= 64) return {1, 1};
-    if (n <= 128) return {1, 2};
-    if (n <= 256) return {1, 4};
-    if (n <= 512) return {4, 2};
-    if (n <= 1024) return {4, 4};
-    return {16, n <= 2048 ? 2 : 4};
+static NormShape norm_variant(int64_t cols, int dtype, bool backward) {
+    const int n = (int)((cols + (dtype == PSGD_F32 ? 3 : 7)) / (dtype == PSGD_F32 ? 4 : 8));
+    if (n <= 256) return {1, (n + 63) / 64};
+    if (n <= 512) return backward ? NormShape{8, 1} : NormShape{4, 2};
+    if (n <= 2048) return {8, (n + 511) / 512};
+    return {16, (n + 1023) / 1024};
 }
-constexpr int kNormBlocks = 2048;           // forward
-constexpr int kNormGradBlocks = 1024;       // backward: each has its sums written and read
+// Workgroups.  Forward, rows in flight: too many streams of addresses cost as much as too few loads (16384 x 4096, 512, 1024 and 2048 workgroups: with addend 90.0, 98.2 and
+// 100.5 us, without 60.1, 47.1, 51.0).  Backward, one to a compute unit, or two of one wavefront to a row: each has its columns' sums written and read (16384 x 4096 with 256, 512 and
+// 1024: 90.8, 98.4 and 102.8 us).
 static int norm_blocks(int64_t rows, const NormShape& v, int most) {
     const int per = v.waves == 1 ? 4 : 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, v.waves == 16 ? most / 4 : most));
+    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, most));
 }
+static int forward_blocks(const NormShape& v, bool add) { return add || v.waves >= 8 ? 512 : 1024; }
+static int backward_blocks(const NormShape& v) { return v.waves == 1 && v.pieces < 4 ? 512 : 256; }
+// Few rows: the sums of columns are made beside the rows, in one launch, from another reading of them.  (1000 x 515 in fp32 5.7 us, with sums of workgroups and a
+// second launch 9.0; 1024 x 4096 in bf16 13.9, 14.6; 1024 x 8192 28.0, 19.5; and what the host takes for a launch, 3 us of 12.5.)
+constexpr int64_t kNormFewRows = 1024, kNormFewBytes = 9 << 20;
 // From this many bytes in a call on activations have the non-temporal hint (as those of act.hip).
 constexpr int64_t kNormStream = 96 << 20;
 
@@ -332,29 +414,38 @@ static bool bad_place(const RowArea& out, const RowArea& in) {
 }
 
 // launch(waves, pieces) with constants
-template <class T, class F>
+template <class T, bool BACKWARD, class F>
 static hipError_t norm_dispatch(const NormShape& v, F launch) {
-    if (v.waves == 1) return v.pieces == 1 ? launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
-                           : v.pieces == 2 ? launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{})
-                                           : launch(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-    if (v.waves == 4) return v.pieces == 2 ? launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{})
-                                           : launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
-    if constexpr (sizeof(T) == 4)
-        if (v.pieces == 4) return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
-    return launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+#define PSGD_SHAPE(W, P) if (v.waves == W && v.pieces == P) return launch(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
+    PSGD_SHAPE(1, 1);
+    PSGD_SHAPE(1, 2);
+    PSGD_SHAPE(1, 3);
+    PSGD_SHAPE(1, 4);
+    if constexpr (BACKWARD) { PSGD_SHAPE(8, 1); }
+    else { PSGD_SHAPE(4, 2); }
+    PSGD_SHAPE(8, 2);
+    PSGD_SHAPE(8, 3);
+    PSGD_SHAPE(8, 4);
+    if constexpr (sizeof(T) == 4) {
+        PSGD_SHAPE(16, 3);
+        PSGD_SHAPE(16, 4);
+    }
+#undef PSGD_SHAPE
+    return hipErrorInvalidValue;
 }
 
 template <class T, bool ADD, bool STREAM>
 static hipError_t launch_norm_as(const NormDev& a, const NormShape& v, hipStream_t st) {
-    const int blocks = norm_blocks(a.rows, v, kNormBlocks);
-    return norm_dispatch<T>(v, [&](auto waves, auto pieces) {
+    const int blocks = norm_blocks(a.rows, v, forward_blocks(v, ADD));
+    return norm_dispatch<T, false>(v, [&](auto waves, auto pieces) {
         hipLaunchKernelGGL((norm_kernel<T, waves.value, pieces.value, ADD, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
         return hipGetLastError();
     });
 }
 template <class T, bool PAST, bool STREAM>
-static hipError_t launch_backward_as(const NormGradDev& a, const NormShape& v, int blocks, hipStream_t st) {
-    return norm_dispatch<T>(v, [&](auto waves, auto pieces) {
+static hipError_t launch_backward_as(const NormGradDev& a, const NormShape& v, hipStream_t st) {
+    const int per = 4 * kPiece<T>, blocks = a.row_blocks + (a.dw || a.db ? (a.cols + per - 1) / per : 0);
+    return norm_dispatch<T, true>(v, [&](auto waves, auto pieces) {
         hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, PAST, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
         return hipGetLastError();
     });
@@ -388,7 +479,7 @@ int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x
             if (overlap(out[i], out[j])) return PSGD_E_INVALID_ARG;
     }
     const NormDev a = {rows, (int)cols, eps, x, add, ld_in, total, y, ld_out, {weight, w_dtype}, {bias, w_dtype}, reinterpret_cast<floatx2*>(stats)};
-    const NormShape v = norm_variant(cols, dtype);
+    const NormShape v = norm_variant(cols, dtype, false);
     const bool stream_it = rows * cols * size * (add ? 4 : 2) >= kNormStream;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     forget_errors();
@@ -402,7 +493,7 @@ int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x
 
 size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype) {
     if (bad_dtype(dtype) || norm_shape(rows, cols)) return 0;
-    return up256((size_t)norm_blocks(rows, norm_variant(cols, dtype), kNormGradBlocks) * 2 * up8(cols) * sizeof(float));
+    return up256((size_t)norm_blocks(rows, norm_variant(cols, dtype, true), backward_blocks(norm_variant(cols, dtype, true))) * 2 * up8(cols) * sizeof(float));
 }
 
 int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols, int dtype, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
@@ -427,22 +518,25 @@ int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols
     }
     if (rows == 0 && (!sums || accumulate)) return PSGD_OK;
     NormGradDev a = {rows, (int)cols, dy, x, dtotal, ld_dy, ld_x, ld_dx, dx, {weight, w_dtype}, reinterpret_cast<const floatx2*>(stats),
-                     sums ? static_cast<float*>(workspace) : nullptr, up8(cols)};
-    const NormShape v = norm_variant(cols, dtype);
-    const int blocks = norm_blocks(rows, v, kNormGradBlocks);
-    const bool stream_it = rows * cols * size * (dtotal ? 4 : 3) >= kNormStream;
+                     nullptr, up8(cols)};
+    const NormShape v = norm_variant(cols, dtype, true);
+    const bool few = rows <= kNormFewRows && rows * cols * size <= kNormFewBytes && dx != dy && dx != x;       // (where dx takes their place, the columns would find some rows written)
+    if (sums && few) a.dw = dweight, a.db = dbias, a.g_dtype = g_dtype, a.accumulate = accumulate != 0;
+    else if (sums) a.part = static_cast<float*>(workspace);
+    a.row_blocks = norm_blocks(rows, v, few ? (int)kNormFewRows : backward_blocks(v));
+    const bool stream_it = !few && rows * cols * size * (dtotal ? 4 : 3) >= kNormStream;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     forget_errors();
     if (rows != 0) {
         hipError_t e;
-#define PSGD_NORM(T, PAST) (stream_it ? launch_backward_as<T, PAST, true>(a, v, blocks, st) : launch_backward_as<T, PAST, false>(a, v, blocks, st))
+#define PSGD_NORM(T, PAST) (stream_it ? launch_backward_as<T, PAST, true>(a, v, st) : launch_backward_as<T, PAST, false>(a, v, st))
         if (dtype == PSGD_F32) e = dtotal ? PSGD_NORM(float, true) : PSGD_NORM(float, false);
         else e = dtotal ? PSGD_NORM(bf16_t, true) : PSGD_NORM(bf16_t, false);
 #undef PSGD_NORM
         if (e != hipSuccess) return PSGD_E_HIP;
     }
-    if (!sums) return PSGD_OK;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 63) / 64), 2), dim3(1024), 0, st, a.part, a.ldp, rows ? blocks : 0, (int)cols, dweight, dbias,
+    if (!sums || (few && rows)) return PSGD_OK;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 63) / 64), 2), dim3(1024), 0, st, a.part, a.ldp, rows ? a.row_blocks : 0, (int)cols, dweight, dbias,
                        g_dtype, accumulate != 0);
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }

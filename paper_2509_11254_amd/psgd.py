@@ -344,13 +344,18 @@ def copy_bytes(dst, src, n_bytes: int, stream=None) -> None:
 
 # ---- the training step around the compressor ---------------------------------------------------------------------------
 
+_dtype_codes: dict = {}
+
+
 def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return PSGD_F32
-    if t.dtype == torch.bfloat16:
-        return PSGD_BF16
-    raise ValueError("float32 or bfloat16 expected, got %s" % t.dtype)
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        import torch
+        _dtype_codes.update({torch.float32: PSGD_F32, torch.bfloat16: PSGD_BF16})
+        code = _dtype_codes.get(t.dtype)
+        if code is None:
+            raise ValueError("float32 or bfloat16 expected, got %s" % t.dtype)
+    return code
 
 
 def _matrix(name: str, t, rows: int, cols: int, dtype: Optional[int] = None) -> int:
@@ -365,7 +370,8 @@ def _matrix(name: str, t, rows: int, cols: int, dtype: Optional[int] = None) -> 
     ld = strides[0] if rows > 1 else (cols + 7) // 8 * 8
     if ld < cols:
         raise ValueError("%s: rows that lie over each other (%d elements apart, %d columns)" % (name, ld, cols))
-    if rows and t.storage_offset() + (rows - 1) * ld + (cols + 7) // 8 * 8 > t.untyped_storage().nbytes() // t.element_size():
+    # (a row of whole eights ends there itself; calls on small matrices take as long as these questions)
+    if cols & 7 and rows and t.storage_offset() + (rows - 1) * ld + (cols + 7) // 8 * 8 > t.untyped_storage().nbytes() // t.element_size():
         raise ValueError("%s: the last row ends before the next multiple of 8 columns, up to which rows may be read" % name)
     return ld
 
@@ -381,7 +387,7 @@ def _stream_for(stream, *tensors) -> int:
 
 
 def _vector(name: str, t, n: int, dtype):
-    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_cuda or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s: %d contiguous elements of %s on the GPU expected" % (name, n, dtype))
     return t
 
@@ -616,31 +622,35 @@ class WeightGrad:
 def norm(X, weight, bias, Y, stats=None, eps: float = 1e-5, add=None, total=None, stream=None) -> None:
     """psgd_norm: Y <- layer norm of the rows of X, or with add of total <- X + add (rounded to the type), times weight plus bias
     (one type; None: 1 and 0).  stats (rows x 2, float32): what NormGrad needs.  total or Y may be X or add itself."""
-    import torch
     lib = load_library()
     _same("presence of add and of total", add is None, total is None)
-    rows, cols, dt = int(X.shape[0]), int(X.shape[1]), _dtype_code(X)
+    (rows, cols), dt = X.shape, _dtype_code(X)
     ld_in, ld_out = _matrix("X", X, rows, cols), _matrix("Y", Y, rows, cols, dt)
     if add is not None:
         _same("leading dimensions of X and add", ld_in, _matrix("add", add, rows, cols, dt))
         _same("leading dimensions of Y and total", ld_out, _matrix("total", total, rows, cols, dt))
-    if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or not stats.is_contiguous() or not stats.is_cuda):
-        raise ValueError("stats: a contiguous %d x 2 float32 matrix on the GPU expected" % rows)
-    w_dt = _params(cols, weight=weight, bias=bias)
+    if stats is not None:
+        _pairs(stats, rows)
+    w_dt = _params(cols, weight, bias)
     _check(lib, None, lib.psgd_norm(_stream_for(stream, X, weight, bias, Y, stats, add, total), rows, cols, dt, X.data_ptr(), _ptr(add), ld_in,
                                     _ptr(weight), _ptr(bias), w_dt, float(eps), _ptr(total), Y.data_ptr(), ld_out, _ptr(stats)))
 
 
-def _params(cols: int, **vectors) -> int:
-    """Checks vectors of one type, each of which may be None; their type."""
+def _pairs(stats, rows: int) -> None:
+    if _dtype_code(stats) != PSGD_F32 or stats.shape != (rows, 2) or not stats.is_contiguous() or not stats.is_cuda:
+        raise ValueError("stats: a contiguous %d x 2 float32 matrix on the GPU expected" % rows)
+
+
+def _params(cols: int, a, b) -> int:
+    """Checks two vectors of one type, each of which may be None; their type."""
     code = None
-    for name, t in vectors.items():
-        if t is None:
-            continue
-        if code is not None and _dtype_code(t) != code:
-            raise ValueError("%s: wrong element type %s" % (name, t.dtype))
-        code = _dtype_code(t)
-        _vector(name, t, cols, t.dtype)
+    for t in (a, b):
+        if t is not None:
+            if t.shape != (cols,) or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("%d contiguous elements on the GPU expected, got %s on %s" % (cols, tuple(t.shape), t.device))
+            if code is not None and _dtype_code(t) != code:
+                raise ValueError("element types of a weight and a bias: one expected")
+            code = _dtype_code(t)
     return PSGD_F32 if code is None else code
 
 
@@ -662,18 +672,16 @@ class NormGrad:
     def run(self, dY, X, weight, stats, dX, dweight=None, dbias=None, dtotal=None, accumulate: bool = False, stream=None) -> None:
         """X: what was normalised (norm's total, where there was one); dtotal: the gradient that reaches it past the norm.
         dX <- its gradient; dweight, dbias <- (accumulate: +=) theirs, each of which may be None.  dX may be dY, X or dtotal itself."""
-        import torch
         rows, cols = self.shape
         ld_dy, ld_x, ld_dx = (_matrix("dY", dY, rows, cols, self.dtype), _matrix("X", X, rows, cols, self.dtype),
                               _matrix("dX", dX, rows, cols, self.dtype))
         if dtotal is not None:
             _same("leading dimensions of dX and dtotal", ld_dx, _matrix("dtotal", dtotal, rows, cols, self.dtype))
-        if stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or not stats.is_contiguous() or not stats.is_cuda:
-            raise ValueError("stats: a contiguous %d x 2 float32 matrix on the GPU expected" % rows)
-        if weight is not None:
-            _same("element types of weight", _params(cols, weight=weight), self.w_dtype)
-        if dweight is not None or dbias is not None:
-            _same("element types of dweight and dbias", _params(cols, dweight=dweight, dbias=dbias), self.grad_dtype)
+        _pairs(stats, rows)
+        if weight is not None and _params(cols, weight, None) != self.w_dtype:
+            raise ValueError("weight: wrong element type %s" % weight.dtype)
+        if (dweight is not None or dbias is not None) and _params(cols, dweight, dbias) != self.grad_dtype:
+            raise ValueError("dweight, dbias: wrong element type")
         _check(self.lib, None, self.lib.psgd_norm_backward(
             self._ws_ptr, _stream_for(stream, self.workspace, dY, X, weight, stats, dX, dweight, dbias, dtotal), rows, cols, self.dtype, dY.data_ptr(),
             ld_dy, X.data_ptr(), ld_x, _ptr(weight), self.w_dtype, stats.data_ptr(), _ptr(dtotal), dX.data_ptr(), ld_dx, _ptr(dweight), _ptr(dbias),
@@ -694,9 +702,6 @@ class ExpertOrder:
         _vector("order", order, self.tokens * self.slots, torch.int32)
         _vector("offsets", offsets, self.experts + 1, torch.int32)
         self.place, self.order, self.offsets = place, order, offsets
-
-    def _tensors(self):
-        return (self.place, self.order, self.offsets)
 
 
 def expert_order_empty(tokens: int, slots: int, experts: int, device: str = "cuda") -> ExpertOrder:
@@ -722,16 +727,15 @@ class ExpertSort:
         """order <- the tokens sorted by choice (tokens x slots int64; outside [0, experts): the choice does not count)."""
         import torch
         _same("sizes of the order", (order.tokens, order.slots, order.experts), self.shape)
-        if choice.dtype != torch.int64 or tuple(choice.shape) != self.shape[:2] or not choice.is_contiguous() or not choice.is_cuda:
+        if choice.dtype != torch.int64 or choice.shape != self.shape[:2] or not choice.is_contiguous() or not choice.is_cuda:
             raise ValueError("choice: a contiguous %d x %d int64 matrix on the GPU expected" % self.shape[:2])
         _check(self.lib, None, self.lib.psgd_expert_sort(
-            self._ws_ptr, _stream_for(stream, self.workspace, choice, *order._tensors()), *self.shape, choice.data_ptr(), order.place.data_ptr(),
+            self._ws_ptr, _stream_for(stream, self.workspace, choice, order.place, order.order, order.offsets), *self.shape, choice.data_ptr(), order.place.data_ptr(),
             order.order.data_ptr(), order.offsets.data_ptr()))
 
 
 def _choice_weights(name: str, t, order: ExpertOrder):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (order.tokens, order.slots) or not t.is_contiguous() or not t.is_cuda):
+    if t is not None and (_dtype_code(t) != PSGD_F32 or t.shape != (order.tokens, order.slots) or not t.is_contiguous() or not t.is_cuda):
         raise ValueError("%s: a contiguous %d x %d float32 matrix on the GPU expected" % (name, order.tokens, order.slots))
 
 
@@ -739,19 +743,19 @@ def expert_rows(X, order: ExpertOrder, Xs, stream=None) -> None:
     """psgd_expert_rows: row place[t, s] of Xs (tokens * slots rows) <- row t of X; rows behind the last stay as they are.
     The gradient of X is expert_combine of the gradient of Xs."""
     lib = load_library()
-    cols, dt = int(X.shape[1]), _dtype_code(X)
+    cols, dt = X.shape[1], _dtype_code(X)
     ld, ld_s = _matrix("X", X, order.tokens, cols), _matrix("Xs", Xs, order.tokens * order.slots, cols, dt)
-    _check(lib, None, lib.psgd_expert_rows(_stream_for(stream, X, Xs, *order._tensors()), order.tokens, order.slots, cols, dt, X.data_ptr(), ld,
+    _check(lib, None, lib.psgd_expert_rows(_stream_for(stream, X, Xs, order.place), order.tokens, order.slots, cols, dt, X.data_ptr(), ld,
                                            order.place.data_ptr(), Xs.data_ptr(), ld_s))
 
 
 def expert_combine(Ys, order: ExpertOrder, Y, weight=None, stream=None) -> None:
     """psgd_expert_combine: row t of Y <- the sum of its choices' rows of Ys times weight[t, s] (None: 1)."""
     lib = load_library()
-    cols, dt = int(Y.shape[1]), _dtype_code(Y)
+    cols, dt = Y.shape[1], _dtype_code(Y)
     ld_s, ld = _matrix("Ys", Ys, order.tokens * order.slots, cols, dt), _matrix("Y", Y, order.tokens, cols)
     _choice_weights("weight", weight, order)
-    _check(lib, None, lib.psgd_expert_combine(_stream_for(stream, Ys, Y, weight, *order._tensors()), order.tokens, order.slots, cols, dt, Ys.data_ptr(),
+    _check(lib, None, lib.psgd_expert_combine(_stream_for(stream, Ys, Y, weight, order.place), order.tokens, order.slots, cols, dt, Ys.data_ptr(),
                                               ld_s, order.place.data_ptr(), _ptr(weight), Y.data_ptr(), ld))
 
 
@@ -759,7 +763,7 @@ def expert_combine_backward(dY, Ys, order: ExpertOrder, dYs, weight=None, dweigh
     """psgd_expert_combine_backward: row place[t, s] of dYs <- weight[t, s] times row t of dY, rows behind the last stay as they are;
     dweight[t, s] <- dY[t] . Ys[place[t, s]], 0 where there is no row (dweight None: Ys may be None).  dYs may be Ys itself."""
     lib = load_library()
-    cols, dt, rows = int(dY.shape[1]), _dtype_code(dY), order.tokens * order.slots
+    cols, dt, rows = dY.shape[1], _dtype_code(dY), order.tokens * order.slots
     ld, ld_ds = _matrix("dY", dY, order.tokens, cols), _matrix("dYs", dYs, rows, cols, dt)
     ld_s = _matrix("Ys", Ys, rows, cols, dt) if Ys is not None else 0
     if dweight is not None and Ys is None:
@@ -767,5 +771,5 @@ def expert_combine_backward(dY, Ys, order: ExpertOrder, dYs, weight=None, dweigh
     _choice_weights("weight", weight, order)
     _choice_weights("dweight", dweight, order)
     _check(lib, None, lib.psgd_expert_combine_backward(
-        _stream_for(stream, dY, Ys, dYs, weight, dweight, *order._tensors()), order.tokens, order.slots, cols, dt, dY.data_ptr(), ld, _ptr(Ys), ld_s,
+        _stream_for(stream, dY, Ys, dYs, weight, dweight, order.place), order.tokens, order.slots, cols, dt, dY.data_ptr(), ld, _ptr(Ys), ld_s,
         order.place.data_ptr(), _ptr(weight), dYs.data_ptr(), ld_ds, _ptr(dweight)))
