@@ -140,6 +140,8 @@ __device__ __forceinline__ int row_of(const RowsDev& a, int64_t i) {
     return __builtin_amdgcn_readfirstlane((unsigned)p < (unsigned)a.n ? p : -1);
 }
 
+// (A wavefront to a token, with two, four or eight of its rows at a time, reads dY once, which comes from the caches here, and is slower: gradients of 16384 tokens of eight
+// rows of 2048 in bf16 200 us so, 5.7 TB/s, and 226 to 233 us; 8192 tokens of two rows of 4096 53, and 60 to 63.  Nor does a smaller grid gain anything: 212 to 217 us.)
 // a wavefront to each choice: X[t] to its row (SCALE: times its weight, and the dot product with Ys' row)
 template <class T, bool SCALE, bool DOT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_rows_kernel(RowsDev a) {
