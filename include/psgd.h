@@ -341,7 +341,7 @@ int psgd_head_loss_grad(const psgd_head_desc *desc, void *workspace, void *strea
  * An entry counts whose index lies in [0, vocab) and whose logit is not -infinity; what the others hold is not looked at.  The order of entries does not matter; a word that
  * is named by several has their probabilities added up.  A token without entries that count does not count (as one whose label lies
  * outside the vocabulary).  top: at most 1024.  Weights, pieces, types, overlaps, accumulation and errors as above; INVALID_ARG as well where
- * temperature or one over it is not a positive number. */
+ * the temperature lies outside [1e-30, 1e30]. */
 size_t psgd_head_distill_workspace_bytes(const psgd_head_desc *desc, int64_t top, int gradients);
 int psgd_head_distill(const psgd_head_desc *desc, void *workspace, void *stream, const void *x, const void *w, int64_t top,
                       const int64_t *index, const void *teacher, int teacher_dtype, int64_t ld_top, float temperature,
@@ -383,7 +383,7 @@ int psgd_act_wgrad(void *workspace, void *stream, int64_t tokens, int64_t out_fe
 /* Layer normalisation of the rows of s = x, or with add (total and add are there both or neither) s = x + add, rounded to the type and written to total:
  *   mean = sum_c s / cols, var = sum_c (s - mean)^2 / cols, r = 1 / sqrt(var + eps);  y = (s - mean) r weight + bias.
  * weight, bias: cols elements of w_dtype, or NULL (1 and 0).  stats, nullable: rows x 2 fp32, mean and r, for the backward pass.  total and y have ld_out, x and add
- * ld_in; total or y may take the place of x or add (the same pointer and leading dimension).  Statistics and sums are fp32 (squares beyond 3.4e38 are not held).
+ * ld_in; total or y may take the place of x or add (the same pointer and leading dimension).  Statistics and sums are fp32 (squares beyond 3.4e38 are not held, nor without eps those below 1e-38).
  * cols: at most 16384.  rows may be 0.  Errors: INVALID_ARG (null pointer, bad enum, eps negative or not finite, an overlap), SHAPE, ALIGN, HIP. */
 int psgd_norm(void *stream, int64_t rows, int64_t cols, int dtype, const void *x, const void *add /* nullable */, int64_t ld_in,
               const void *weight /* nullable */, const void *bias /* nullable */, int w_dtype, float eps, void *total /* nullable */,

@@ -974,6 +974,7 @@ struct HeadTeacher {
     int64_t ld, top;
     float temperature;
 };
+constexpr float kMinTemperature = 1e-30f;       // (what is multiplied by one over it stays in range)
 static int teacher_shape(int64_t top) { return top < 1 || top > kMaxTop ? PSGD_E_SHAPE : PSGD_OK; }
 
 template <int U, int GROUP>
@@ -1002,8 +1003,7 @@ static int head_run(const psgd_head_desc* s, const HeadTeacher* teacher, bool gr
                     const float* weight, float* loss, void* dx, void* dw, int accumulate) {
     if (int rc = head_shape(s)) return rc;
     if (teacher) {
-        const float inv = 1.f / teacher->temperature;
-        if (bad_dtype(teacher->dtype) || !(teacher->temperature > 0.f && inv > 0.f && inv < __builtin_inff())) return PSGD_E_INVALID_ARG;
+        if (bad_dtype(teacher->dtype) || !(teacher->temperature >= kMinTemperature && teacher->temperature <= 1.f / kMinTemperature)) return PSGD_E_INVALID_ARG;
         if (s->tokens != 0 && (!teacher->index || !teacher->logits)) return PSGD_E_INVALID_ARG;
         if (int rc = teacher_shape(teacher->top)) return rc;
         if (teacher->ld > kMaxLd) return PSGD_E_SHAPE;

@@ -133,6 +133,36 @@ def test_words_that_several_entries_name(dtype, tokens):
     run(tokens, 72, 50, 100, dtype, "f32", distinct=False)
 
 
+@pytest.mark.parametrize("tokens,dtype,vocab", [(5, "bf16", 700001), (3, "f32", 300001), (300, "bf16", 560000)])
+def test_more_tiles_than_ranges_of_words(tokens, dtype, vocab):
+    """Vocabularies of more tiles than the lists have ranges for: several tiles look through the same entries."""
+    d, top = 8, 40
+    x, w, index, teacher = inputs(tokens, d, vocab, top, DT[dtype], 21, distinct=False, masked=0.0)
+    index[0, :6], teacher[0, :6] = torch.tensor([0, vocab - 1, 127, 128, 255, 256]), torch.arange(6.0)
+    loss, dx, dw = torch.empty(tokens, device="cuda"), torch.empty_like(x), torch.empty((vocab, d), dtype=DT[dtype], device="cuda")
+    psgd.HeadDistill(tokens, d, vocab, top, CODE[dtype]).loss_grad(x, w, index, teacher, loss, dx, dw)
+    rows = list(range(0, tokens, 97)) if tokens > 100 else list(range(tokens))
+    check(x[rows], w, index[rows], teacher[rows], 1.0, loss[rows], None, None, None)
+    if tokens < 100:
+        check(x, w, index, teacher, 1.0, loss, dx, dw, None)
+
+
+def test_extreme_temperatures():
+    """At 1e-30 the largest logit has all probability, on both sides; at 1e30 all words have the same, and the entries the same among them."""
+    tokens, d, vocab, top = 20, 64, 500, 6
+    x, w, index, teacher = inputs(tokens, d, vocab, top, torch.float32, 22, masked=0.0, ragged=0.0)
+    teacher = torch.randn((tokens, top), device="cuda")
+    best = index.gather(1, teacher.argmax(1, keepdim=True))[:, 0]
+    x = torch.nan_to_num(x)
+    x[:10] = 30 * w[best[:10]]                # these know the teacher's word
+    plan, loss = psgd.HeadDistill(tokens, d, vocab, top, psgd.PSGD_F32, grad=False), torch.empty(tokens, device="cuda")
+    plan.loss(padded(x, torch.float32, 8)[0], w, index, teacher, loss, temperature=1e-30)
+    knows = (x.double() @ w.double().t()).argmax(1) == best
+    assert (loss[knows] == 0).all() and (loss[~knows] > 1).all() and knows[:10].all() and not knows.all()
+    plan.loss(padded(x, torch.float32, 8)[0], w, index, teacher, loss, temperature=1e30)
+    assert (loss - math.log(vocab / top)).abs().max() < 2.0 ** -20 * 10
+
+
 def test_entries_in_another_order():
     """The same bits, whatever the order of a token's entries."""
     tokens, d, vocab, top = 90, 72, 800, 50

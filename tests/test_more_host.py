@@ -147,7 +147,7 @@ def distill(lib, desc=None, grad=True, **change):
 @pytest.mark.parametrize("change,want", [
     (dict(top=0), SHAPE), (dict(top=1025, ld=1032), SHAPE), (dict(ld=BIG), SHAPE), (dict(ld=11), ALIGN), (dict(index=M + 8), ALIGN), (dict(teacher=M + 4), ALIGN),
     (dict(index=None), INVALID), (dict(teacher=None), INVALID), (dict(t_dtype=2), INVALID), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
-    (dict(temperature=float("nan")), INVALID), (dict(temperature=float("inf")), INVALID), (dict(temperature=1e-42), INVALID), (dict(x=None), INVALID),
+    (dict(temperature=float("nan")), INVALID), (dict(temperature=float("inf")), INVALID), (dict(temperature=1e-42), INVALID), (dict(temperature=1e-31), INVALID), (dict(temperature=1e31), INVALID), (dict(x=None), INVALID),
     (dict(loss=None), INVALID), (dict(workspace=M + 16), ALIGN),
     # 100 tokens: 99 rows of 16 entries and 12 more
     (dict(loss=4 * M + 99 * 128 + 80), INVALID), (dict(loss=5 * M + 99 * 64 + 32), INVALID)])
