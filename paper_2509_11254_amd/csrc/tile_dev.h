@@ -319,10 +319,10 @@ struct Tile {
     }
 
     // acc = the tile at (p0, l0), part `split` of n_split of the contraction over K steps; nl: rows of C there are.  MINUS_INF: what lies beyond P's
-    // extent comes out as -inf, where sums begin that only get zeros added
+    // extent comes out as -inf, where sums begin that only get zeros added.  turn: the chunk a ring begins with, where there is one pair of planes and one part
     template <bool MINUS_INF = false, bool CODES = false>
     __device__ void run(const TileArgs& t, int p0, int l0, int nl, int K, int split, int n_split, PSGD_TLDS unsigned char* lds,
-                        const TileCodes& codes = {}) {
+                        const TileCodes& codes = {}, int turn = 0) {
         lane = threadIdx.x & 63;
         const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wp = wv % WP;
@@ -355,7 +355,7 @@ struct Tile {
             else if constexpr (SPLIT) run_split(t, p0, l0, K, n0, n, wv, sp, sl, fp, fl, lds);
             else if constexpr (CODES) run_codes(t, codes, p0, l0, K, n0, n, per, wv, sl, fp, fl, lds);
             else if constexpr (STAGES == 1) run_single(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
-            else run_ring(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds);
+            else run_ring(t, p0, l0, K, n0, n, per, wv, sp, sl, fp, fl, lds, turn);
         }
     }
 
@@ -385,8 +385,8 @@ struct Tile {
     // unit the loads' latency is what counts).  Fragments, barrier and what lies past the end as in run_full.
     __device__ __forceinline__ void run_ring(const TileArgs& t, int p0, int l0, int K, int n0, int n, int per, int wv, const SideP& sp,
                                              const SideL& sl, const TileFragment<PKC, BP, BK>& fp, const TileFragment<LKC, BL, BK>& fl,
-                                             PSGD_TLDS unsigned char* lds) {
-        int left = n, pair = n0 / per, kc = n0 - pair * per, into = 0, from = 0;     // of the next chunk to load
+                                             PSGD_TLDS unsigned char* lds, int turn) {
+        int left = n, pair = n0 / per, kc = n0 - pair * per + turn, into = 0, from = 0;     // of the next chunk to load
         typename SideP::Source from_p;
         typename SideL::Source from_l;
         auto next = [&]() {         // its place
