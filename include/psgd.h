@@ -297,7 +297,7 @@ int psgd_profile_read(psgd_ctx *ctx, double *total_ms, int *count, int n_tags);
 /* ---- the training step around the compressor: the output head's loss, 8-bit activations, weight gradients, norms, experts ----
  *
  * The calls below have no context.  Matrices are row-major device memory with a leading dimension in elements, a multiple of 8 (codes:
- * of 16) that is at least the columns and, of the matrices that are multiplied, at most 2^22; bases are 16-byte aligned.  Unless a call says otherwise, what is written overlaps nothing else.  Elements beyond the columns are never taken as data nor written,
+ * of 16) that is at least the columns and, of the matrices that are multiplied, normalised or laid out by expert, at most 2^22; bases are 16-byte aligned.  Unless a call says otherwise, what is written overlaps nothing else.  Elements beyond the columns are never taken as data nor written,
  * up to the next multiple of 8 they may be read, so the last row's are part of the buffer as well.  Work is enqueued on `stream`, nothing is kept from one call to the next, and a
  * workspace (256-byte aligned, of the bytes that the call's _workspace_bytes function gives; 0 = the arguments are refused) holds nothing between calls.  Calls
  * that may run at the same time, on streams that do not wait for each other, have a workspace each.  The calls launch kernels only and
@@ -382,21 +382,21 @@ int psgd_act_wgrad(void *workspace, void *stream, int64_t tokens, int64_t out_fe
 
 /* Layer normalisation of the rows of s = x, or with add (total and add are there both or neither) s = x + add, rounded to the type and written to total:
  *   mean = sum_c s / cols, var = sum_c (s - mean)^2 / cols, r = 1 / sqrt(var + eps);  y = (s - mean) r weight + bias.
- * weight, bias: cols elements of w_dtype, or NULL (1 and 0).  stats, nullable: rows x 2 fp32, mean and r, for the backward pass.  total and y have ld_out, x and add
- * ld_in; total or y may take the place of x or add (the same pointer and leading dimension).  Statistics and sums are fp32 (squares beyond 3.4e38 are not held, nor without eps those below 1e-38).
+ * weight, bias: cols elements of w_dtype, or NULL (1 and 0).  stats, nullable: rows x 2 fp32, mean and r, for the backward pass.
+ * total or y may take the place of x or add (the same pointer and leading dimension).  Statistics and sums are fp32 (squares beyond 3.4e38 are not held, nor without eps those below 1e-38).
  * cols: at most 16384.  rows may be 0.  Errors: INVALID_ARG (null pointer, bad enum, eps negative or not finite, an overlap), SHAPE, ALIGN, HIP. */
-int psgd_norm(void *stream, int64_t rows, int64_t cols, int dtype, const void *x, const void *add /* nullable */, int64_t ld_in,
-              const void *weight /* nullable */, const void *bias /* nullable */, int w_dtype, float eps, void *total /* nullable */,
-              void *y, int64_t ld_out, float *stats /* nullable */);
+int psgd_norm(void *stream, int64_t rows, int64_t cols, int dtype, const void *x, int64_t ld_x, const void *add /* nullable */,
+              int64_t ld_add, const void *weight /* nullable */, const void *bias /* nullable */, int w_dtype, float eps,
+              void *total /* nullable */, int64_t ld_total, void *y, int64_t ld_y, float *stats /* nullable */);
 /* With u = (x - mean) r and g = dy weight:  dx = r (g - mean_c g - u mean_c(g u)) + dtotal;  dweight = sum_rows dy u, dbias = sum_rows dy,
  * written or, with accumulate != 0, added to.  x: what was normalised (total, where there was one); stats: psgd_norm's; dtotal: the gradient that reaches
- * it past the norm (ld_dx), or NULL.  dx may take the place of dy, x or dtotal.  dweight, dbias: cols elements of g_dtype, each nullable;
+ * it past the norm, or NULL.  dx may take the place of dy, x or dtotal.  dweight, dbias: cols elements of g_dtype, each nullable;
  * without either the workspace may be NULL. */
 size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype);
 int psgd_norm_backward(void *workspace, void *stream, int64_t rows, int64_t cols, int dtype, const void *dy, int64_t ld_dy,
                        const void *x, int64_t ld_x, const void *weight /* nullable */, int w_dtype, const float *stats,
-                       const void *dtotal /* nullable */, void *dx, int64_t ld_dx, void *dweight /* nullable */,
-                       void *dbias /* nullable */, int g_dtype, int accumulate);
+                       const void *dtotal /* nullable */, int64_t ld_dtotal, void *dx, int64_t ld_dx,
+                       void *dweight /* nullable */, void *dbias /* nullable */, int g_dtype, int accumulate);
 
 /* Tokens sorted by the experts they chose, `slots` choices each (choice: tokens x slots; outside [0, experts): the choice does not count).
  * Rows are counted through the experts in their order, within an expert through the choices in theirs (token by token):

@@ -27,9 +27,9 @@ struct NormDev {
     int cols;
     float eps;
     const void *x, *add;
-    int64_t ld_in;
+    int64_t ld_x, ld_add;
     void *total, *y;
-    int64_t ld_out;
+    int64_t ld_total, ld_y;
     NormParam w, b;
     floatx2* stats;
 };
@@ -37,7 +37,7 @@ struct NormGradDev {
     int64_t rows;
     int cols;
     const void *dy, *x, *past;      // past: the gradient that comes past the norm
-    int64_t ld_dy, ld_x, ld_dx;
+    int64_t ld_dy, ld_x, ld_past, ld_dx;
     void* dx;
     NormParam w;
     const floatx2* stats;
@@ -138,8 +138,8 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
-            raw[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_in, p[i]);
-            if constexpr (ADD) raw_add[i] = load_raw<STREAM>(static_cast<const T*>(a.add), a.ld_in, p[i]);
+            raw[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_x, p[i]);
+            if constexpr (ADD) raw_add[i] = load_raw<STREAM>(static_cast<const T*>(a.add), a.ld_add, p[i]);
         }
     };
     int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group;
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
                 widen<T>(raw_add[i], o);
 #pragma unroll
                 for (int u = 0; u < N; ++u) v[i][u] = (float)(T)(v[i][u] + o[u]);       // (what is normalised is what is kept)
-                store_piece<STREAM>(static_cast<T*>(a.total), a.ld_out, p[i], a.cols, v[i]);
+                store_piece<STREAM>(static_cast<T*>(a.total), a.ld_total, p[i], a.cols, v[i]);
             }
 #pragma unroll
             for (int u = 0; u < N; ++u) sum[0] += v[i][u];
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
         for (int i = 0; i < PIECES; ++i) {
 #pragma unroll
             for (int u = 0; u < N; ++u) v[i][u] = fmaf((v[i][u] - more) * r, w[i][u], b[i][u]);
-            store_piece<STREAM>(static_cast<T*>(a.y), a.ld_out, p[i], a.cols, v[i]);
+            store_piece<STREAM>(static_cast<T*>(a.y), a.ld_y, p[i], a.cols, v[i]);
         }
     }
 }
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
             p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
             raw_x[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_x, p[i]);
             raw_dy[i] = load_raw<STREAM>(static_cast<const T*>(a.dy), a.ld_dy, p[i]);
-            if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_dx, p[i]);
+            if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_past, p[i]);
         }
         stats = as_global(a.stats)[row];
     };
@@ -457,19 +457,19 @@ using namespace psgd;
 
 extern "C" {
 
-int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x, const void* add, int64_t ld_in, const void* weight, const void* bias,
-              int w_dtype, float eps, void* total, void* y, int64_t ld_out, float* stats) {
+int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x, int64_t ld_x, const void* add, int64_t ld_add, const void* weight,
+              const void* bias, int w_dtype, float eps, void* total, int64_t ld_total, void* y, int64_t ld_y, float* stats) {
     if (bad_dtype(dtype) || bad_dtype(w_dtype) || !(eps >= 0.f && eps < __builtin_inff())) return PSGD_E_INVALID_ARG;
     if (rows != 0 && (!x || !y || (add == nullptr) != (total == nullptr))) return PSGD_E_INVALID_ARG;
     if (int rc = norm_shape(rows, cols)) return rc;
-    if (bad_ld(ld_in, cols) || bad_ld(ld_out, cols) || misaligned(x) || misaligned(add) || misaligned(weight) || misaligned(bias) || misaligned(total) ||
+    if (bad_ld(ld_x, cols) || bad_ld(ld_y, cols) || (add && (bad_ld(ld_add, cols) || bad_ld(ld_total, cols))) || misaligned(x) || misaligned(add) || misaligned(weight) || misaligned(bias) || misaligned(total) ||
         misaligned(y) || misaligned(stats)) return PSGD_E_ALIGN;
-    if (ld_in > kMaxLd || ld_out > kMaxLd) return PSGD_E_SHAPE;
+    if (ld_x > kMaxLd || ld_y > kMaxLd || (add && (ld_add > kMaxLd || ld_total > kMaxLd))) return PSGD_E_SHAPE;
     if (rows == 0) return PSGD_OK;
     const int64_t size = dtype == PSGD_F32 ? 4 : 2, w_size = w_dtype == PSGD_F32 ? 4 : 2;
-    const RowArea in[] = {{x, rows, ld_in * size, cols * size}, {add, rows, ld_in * size, cols * size}};
+    const RowArea in[] = {{x, rows, ld_x * size, cols * size}, {add, rows, ld_add * size, cols * size}};
     const RowArea params[] = {{weight, 1, 0, cols * w_size}, {bias, 1, 0, cols * w_size}};
-    const RowArea out[] = {{total, rows, ld_out * size, cols * size}, {y, rows, ld_out * size, cols * size}, {stats, 1, 0, rows * 8}};
+    const RowArea out[] = {{total, rows, ld_total * size, cols * size}, {y, rows, ld_y * size, cols * size}, {stats, 1, 0, rows * 8}};
     for (int i = 0; i < 3; ++i) {
         for (const RowArea& a : in)
             if (i == 2 ? overlap(out[i], a) : bad_place(out[i], a)) return PSGD_E_INVALID_ARG;
@@ -478,7 +478,7 @@ int psgd_norm(void* stream, int64_t rows, int64_t cols, int dtype, const void* x
         for (int j = 0; j < i; ++j)
             if (overlap(out[i], out[j])) return PSGD_E_INVALID_ARG;
     }
-    const NormDev a = {rows, (int)cols, eps, x, add, ld_in, total, y, ld_out, {weight, w_dtype}, {bias, w_dtype}, reinterpret_cast<floatx2*>(stats)};
+    const NormDev a = {rows, (int)cols, eps, x, add, ld_x, ld_add, total, y, ld_total, ld_y, {weight, w_dtype}, {bias, w_dtype}, reinterpret_cast<floatx2*>(stats)};
     const NormShape v = norm_variant(cols, dtype, false);
     const bool stream_it = rows * cols * size * (add ? 4 : 2) >= kNormStream;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
@@ -497,17 +497,17 @@ size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype)
 }
 
 int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols, int dtype, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
-                       const void* weight, int w_dtype, const float* stats, const void* dtotal, void* dx, int64_t ld_dx, void* dweight, void* dbias,
-                       int g_dtype, int accumulate) {
+                       const void* weight, int w_dtype, const float* stats, const void* dtotal, int64_t ld_dtotal, void* dx, int64_t ld_dx, void* dweight,
+                       void* dbias, int g_dtype, int accumulate) {
     const bool sums = dweight || dbias;
     if (bad_dtype(dtype) || bad_dtype(w_dtype) || bad_dtype(g_dtype) || (sums && !workspace)) return PSGD_E_INVALID_ARG;
     if (rows != 0 && (!dy || !x || !stats || !dx)) return PSGD_E_INVALID_ARG;
     if (int rc = norm_shape(rows, cols)) return rc;
-    if (bad_ld(ld_dy, cols) || bad_ld(ld_x, cols) || bad_ld(ld_dx, cols) || misaligned(dy) || misaligned(x) || misaligned(weight) || misaligned(stats) ||
+    if (bad_ld(ld_dy, cols) || bad_ld(ld_x, cols) || (dtotal && bad_ld(ld_dtotal, cols)) || bad_ld(ld_dx, cols) || misaligned(dy) || misaligned(x) || misaligned(weight) || misaligned(stats) ||
         misaligned(dtotal) || misaligned(dx) || misaligned(dweight) || misaligned(dbias) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PSGD_E_ALIGN;
-    if (ld_dy > kMaxLd || ld_x > kMaxLd || ld_dx > kMaxLd) return PSGD_E_SHAPE;
+    if (ld_dy > kMaxLd || ld_x > kMaxLd || (dtotal && ld_dtotal > kMaxLd) || ld_dx > kMaxLd) return PSGD_E_SHAPE;
     const int64_t size = dtype == PSGD_F32 ? 4 : 2, w_size = w_dtype == PSGD_F32 ? 4 : 2, g_size = g_dtype == PSGD_F32 ? 4 : 2;
-    const RowArea in[] = {{dy, rows, ld_dy * size, cols * size}, {x, rows, ld_x * size, cols * size}, {dtotal, rows, ld_dx * size, cols * size},
+    const RowArea in[] = {{dy, rows, ld_dy * size, cols * size}, {x, rows, ld_x * size, cols * size}, {dtotal, rows, ld_dtotal * size, cols * size},
                           {weight, 1, 0, cols * w_size}, {stats, 1, 0, rows * 8}};
     const RowArea out[] = {{dx, rows, ld_dx * size, cols * size}, {dweight, 1, 0, cols * g_size}, {dbias, 1, 0, cols * g_size}};
     for (int i = 0; i < 3; ++i) {
@@ -517,7 +517,7 @@ int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols
             if (overlap(out[i], out[j])) return PSGD_E_INVALID_ARG;
     }
     if (rows == 0 && (!sums || accumulate)) return PSGD_OK;
-    NormGradDev a = {rows, (int)cols, dy, x, dtotal, ld_dy, ld_x, ld_dx, dx, {weight, w_dtype}, reinterpret_cast<const floatx2*>(stats),
+    NormGradDev a = {rows, (int)cols, dy, x, dtotal, ld_dy, ld_x, ld_dtotal, ld_dx, dx, {weight, w_dtype}, reinterpret_cast<const floatx2*>(stats),
                      nullptr, up8(cols)};
     const NormShape v = norm_variant(cols, dtype, true);
     const bool few = rows <= kNormFewRows && rows * cols * size <= kNormFewBytes && dx != dy && dx != x;       // (where dx takes their place, the columns would find some rows written)

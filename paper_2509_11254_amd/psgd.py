@@ -141,10 +141,10 @@ def load_library() -> C.CDLL:
     lib.psgd_head_distill_workspace_bytes.restype = C.c_size_t
     lib.psgd_head_distill.argtypes = [hd, vp, vp, vp, vp, l, vp, vp, i, l, C.c_float, vp]
     lib.psgd_head_distill_grad.argtypes = [hd, vp, vp, vp, vp, l, vp, vp, i, l, C.c_float, vp, vp, vp, vp, i]
-    lib.psgd_norm.argtypes = [vp, l, l, i, vp, vp, l, vp, vp, i, C.c_float, vp, vp, l, vp]
+    lib.psgd_norm.argtypes = [vp, l, l, i, vp, l, vp, l, vp, vp, i, C.c_float, vp, l, vp, l, vp]
     lib.psgd_norm_backward_workspace_bytes.argtypes = [l, l, i]
     lib.psgd_norm_backward_workspace_bytes.restype = C.c_size_t
-    lib.psgd_norm_backward.argtypes = [vp, vp, l, l, i, vp, l, vp, l, vp, i, vp, vp, vp, l, vp, vp, i, i]
+    lib.psgd_norm_backward.argtypes = [vp, vp, l, l, i, vp, l, vp, l, vp, i, vp, vp, l, vp, l, vp, vp, i, i]
     lib.psgd_expert_sort_workspace_bytes.argtypes = [l, l, l]
     lib.psgd_expert_sort_workspace_bytes.restype = C.c_size_t
     lib.psgd_expert_sort.argtypes = [vp, vp, l, l, l, vp, vp, vp, vp]
@@ -625,15 +625,14 @@ def norm(X, weight, bias, Y, stats=None, eps: float = 1e-5, add=None, total=None
     lib = load_library()
     _same("presence of add and of total", add is None, total is None)
     (rows, cols), dt = X.shape, _dtype_code(X)
-    ld_in, ld_out = _matrix("X", X, rows, cols), _matrix("Y", Y, rows, cols, dt)
+    ld_x, ld_y, ld_add, ld_total = _matrix("X", X, rows, cols), _matrix("Y", Y, rows, cols, dt), 0, 0
     if add is not None:
-        _same("leading dimensions of X and add", ld_in, _matrix("add", add, rows, cols, dt))
-        _same("leading dimensions of Y and total", ld_out, _matrix("total", total, rows, cols, dt))
+        ld_add, ld_total = _matrix("add", add, rows, cols, dt), _matrix("total", total, rows, cols, dt)
     if stats is not None:
         _pairs(stats, rows)
     w_dt = _params(cols, weight, bias)
-    _check(lib, None, lib.psgd_norm(_stream_for(stream, X, weight, bias, Y, stats, add, total), rows, cols, dt, X.data_ptr(), _ptr(add), ld_in,
-                                    _ptr(weight), _ptr(bias), w_dt, float(eps), _ptr(total), Y.data_ptr(), ld_out, _ptr(stats)))
+    _check(lib, None, lib.psgd_norm(_stream_for(stream, X, weight, bias, Y, stats, add, total), rows, cols, dt, X.data_ptr(), ld_x, _ptr(add), ld_add,
+                                    _ptr(weight), _ptr(bias), w_dt, float(eps), _ptr(total), ld_total, Y.data_ptr(), ld_y, _ptr(stats)))
 
 
 def _pairs(stats, rows: int) -> None:
@@ -675,8 +674,7 @@ class NormGrad:
         rows, cols = self.shape
         ld_dy, ld_x, ld_dx = (_matrix("dY", dY, rows, cols, self.dtype), _matrix("X", X, rows, cols, self.dtype),
                               _matrix("dX", dX, rows, cols, self.dtype))
-        if dtotal is not None:
-            _same("leading dimensions of dX and dtotal", ld_dx, _matrix("dtotal", dtotal, rows, cols, self.dtype))
+        ld_dtotal = _matrix("dtotal", dtotal, rows, cols, self.dtype) if dtotal is not None else 0
         _pairs(stats, rows)
         if weight is not None and _params(cols, weight, None) != self.w_dtype:
             raise ValueError("weight: wrong element type %s" % weight.dtype)
@@ -684,7 +682,7 @@ class NormGrad:
             raise ValueError("dweight, dbias: wrong element type")
         _check(self.lib, None, self.lib.psgd_norm_backward(
             self._ws_ptr, _stream_for(stream, self.workspace, dY, X, weight, stats, dX, dweight, dbias, dtotal), rows, cols, self.dtype, dY.data_ptr(),
-            ld_dy, X.data_ptr(), ld_x, _ptr(weight), self.w_dtype, stats.data_ptr(), _ptr(dtotal), dX.data_ptr(), ld_dx, _ptr(dweight), _ptr(dbias),
+            ld_dy, X.data_ptr(), ld_x, _ptr(weight), self.w_dtype, stats.data_ptr(), _ptr(dtotal), ld_dtotal, dX.data_ptr(), ld_dx, _ptr(dweight), _ptr(dbias),
             self.grad_dtype, 1 if accumulate else 0))
 
 

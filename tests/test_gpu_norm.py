@@ -39,12 +39,12 @@ def vector(n, dtype, seed, scale, shift):
 
 def forward(rows, cols, dtype, wtype, *, add, affine="wb", shift=0.0, eps=1e-5, extra=8):
     x = padded(values(rows, cols, 1, shift), DT[dtype], extra)[0]
-    o = padded(values(rows, cols, 2), DT[dtype], extra)[0] if add else None
+    o = padded(values(rows, cols, 2), DT[dtype], 2 * extra)[0] if add else None
     w = vector(cols, wtype, 3, 0.3, 1.0) if "w" in affine else None
     b = vector(cols, wtype, 4, 0.3, 0.0) if "b" in affine else None
     nan = torch.full((rows, cols), float("nan"))
     y, y_buf = padded(nan, DT[dtype], 16)
-    total, total_buf = padded(nan, DT[dtype], 16) if add else (None, None)
+    total, total_buf = padded(nan, DT[dtype], 40) if add else (None, None)
     stats = torch.full((rows, 2), float("nan"), device="cuda")
     psgd.norm(x, w, b, y, stats, eps=eps, add=o, total=total)
     s = x
@@ -94,7 +94,7 @@ def test_rows_without_variance(cols):
 def backward(rows, cols, dtype, wtype, gtype, *, past=False, accumulate=False, affine="wb", which="wb", shift=0.0, place=None):
     s, w, stats = forward(rows, cols, dtype, wtype, add=False, affine=affine, shift=shift)
     dy, _ = padded(values(rows, cols, 6) * 1e-2, DT[dtype], 24)
-    beyond, _ = padded(values(rows, cols, 7) * 1e-2, DT[dtype], 16) if past else (None, None)
+    beyond, _ = padded(values(rows, cols, 7) * 1e-2, DT[dtype], 32) if past else (None, None)
     dx, dx_buf = padded(torch.full((rows, cols), float("nan")), DT[dtype], 16)
     first = {k: vector(cols, gtype, 8 + i, 1.0, 0.0) if accumulate else torch.full((cols,), float("nan"), dtype=DT[gtype], device="cuda")
              for i, k in enumerate("wb") if k in which}

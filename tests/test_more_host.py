@@ -20,15 +20,15 @@ def lib():
 
 
 def norm(lib, **change):
-    a = dict(rows=6, cols=40, dtype=F32, x=M, add=2 * M, ld_in=40, weight=3 * M, bias=4 * M, w_dtype=F32, eps=1e-5, total=5 * M, y=6 * M, ld_out=40, stats=7 * M)
+    a = dict(rows=6, cols=40, dtype=F32, x=M, ld_x=40, add=2 * M, ld_add=48, weight=3 * M, bias=4 * M, w_dtype=F32, eps=1e-5, total=5 * M, ld_total=56, y=6 * M, ld_y=40, stats=7 * M)
     assert not set(change) - set(a)
     a.update(change)
     return lib.psgd_norm(None, *a.values())
 
 
 def norm_backward(lib, **change):
-    a = dict(workspace=M, stream=None, rows=6, cols=40, dtype=F32, dy=2 * M, ld_dy=40, x=3 * M, ld_x=40, weight=4 * M, w_dtype=F32, stats=5 * M, dtotal=6 * M, dx=7 * M,
-             ld_dx=40, dweight=8 * M, dbias=9 * M, g_dtype=F32, accumulate=0)
+    a = dict(workspace=M, stream=None, rows=6, cols=40, dtype=F32, dy=2 * M, ld_dy=40, x=3 * M, ld_x=40, weight=4 * M, w_dtype=F32, stats=5 * M, dtotal=6 * M, ld_dtotal=48,
+             dx=7 * M, ld_dx=40, dweight=8 * M, dbias=9 * M, g_dtype=F32, accumulate=0)
     assert not set(change) - set(a)
     a.update(change)
     return lib.psgd_norm_backward(*a.values())
@@ -37,11 +37,11 @@ def norm_backward(lib, **change):
 @pytest.mark.parametrize("change,want", [
     (dict(dtype=2), INVALID), (dict(w_dtype=-1), INVALID), (dict(eps=-1e-9), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(add=None), INVALID), (dict(total=None), INVALID),
-    (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(cols=16385, ld_in=16392, ld_out=16392), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(ld_in=BIG), SHAPE),
-    (dict(ld_out=BIG), SHAPE), (dict(ld_in=32), ALIGN), (dict(ld_out=44), ALIGN), (dict(x=M + 8), ALIGN), (dict(add=M // 2 + 4), ALIGN), (dict(weight=M + 4), ALIGN),
+    (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(cols=16385), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(ld_x=BIG), SHAPE),
+    (dict(ld_add=BIG), SHAPE), (dict(ld_total=BIG), SHAPE), (dict(ld_y=BIG), SHAPE), (dict(ld_x=32), ALIGN), (dict(ld_add=36), ALIGN), (dict(ld_total=32), ALIGN), (dict(ld_y=44), ALIGN), (dict(x=M + 8), ALIGN), (dict(add=M // 2 + 4), ALIGN), (dict(weight=M + 4), ALIGN),
     (dict(bias=M + 8), ALIGN), (dict(total=M + 2), ALIGN), (dict(y=5 * M + 8), ALIGN), (dict(stats=M + 8), ALIGN),
     # 6 rows of 160 bytes: y begins in x's last row; over its rows by half; over the other output, over parameters and statistics
-    (dict(y=M + 5 * 160), INVALID), (dict(y=M + 80), INVALID), (dict(y=M, ld_out=48), INVALID), (dict(y=5 * M), INVALID), (dict(total=3 * M), INVALID),
+    (dict(y=M + 5 * 160), INVALID), (dict(y=M + 80), INVALID), (dict(y=M, ld_y=48), INVALID), (dict(total=2 * M), INVALID), (dict(y=5 * M), INVALID), (dict(total=3 * M), INVALID),
     (dict(y=4 * M + 144), INVALID), (dict(stats=M + 800), INVALID), (dict(stats=6 * M + 944), INVALID), (dict(stats=3 * M), INVALID)])
 def test_norm_refuses(lib, change, want):
     assert norm(lib, **change) == want
@@ -50,7 +50,7 @@ def test_norm_refuses(lib, change, want):
 @pytest.mark.parametrize("change,want", [
     (dict(dtype=2), INVALID), (dict(w_dtype=3), INVALID), (dict(g_dtype=-1), INVALID), (dict(workspace=None), INVALID), (dict(dy=None), INVALID), (dict(x=None), INVALID),
     (dict(stats=None), INVALID), (dict(dx=None), INVALID), (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(cols=16385), SHAPE), (dict(ld_dy=BIG), SHAPE),
-    (dict(ld_x=BIG), SHAPE), (dict(ld_dx=BIG), SHAPE), (dict(ld_dy=36), ALIGN), (dict(ld_x=32), ALIGN), (dict(ld_dx=44), ALIGN), (dict(workspace=M + 128), ALIGN),
+    (dict(ld_x=BIG), SHAPE), (dict(ld_dx=BIG), SHAPE), (dict(ld_dtotal=BIG), SHAPE), (dict(ld_dtotal=32), ALIGN), (dict(dx=6 * M), INVALID), (dict(ld_dy=36), ALIGN), (dict(ld_x=32), ALIGN), (dict(ld_dx=44), ALIGN), (dict(workspace=M + 128), ALIGN),
     (dict(dy=M + 8), ALIGN), (dict(x=M + 8), ALIGN), (dict(weight=M + 8), ALIGN), (dict(stats=M + 8), ALIGN), (dict(dtotal=M + 8), ALIGN), (dict(dx=M + 8), ALIGN),
     (dict(dweight=M + 8), ALIGN), (dict(dbias=M + 8), ALIGN),
     (dict(dx=2 * M + 160), INVALID), (dict(dx=3 * M, ld_dx=48), INVALID), (dict(dx=4 * M), INVALID), (dict(dx=5 * M), INVALID), (dict(dweight=2 * M + 800), INVALID),
