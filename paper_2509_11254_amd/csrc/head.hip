@@ -217,9 +217,37 @@ __global__ __launch_bounds__(kThreads) void head_top_count_kernel(HeadTop k, int
     }
 }
 
-// The lists of the piece's tokens, a group to a workgroup, whose wavefronts take a token after another, with up to U entries to a lane.  Entries get
-// their place by the number of smaller ones (word, then place among the token's entries); those of one word become one with the sum of
-// their probabilities.  Then the group's words are counted by bucket, and put there.
+// a and b of a sorting network
+__device__ __forceinline__ void in_order(unsigned& a, unsigned& b, bool up) {
+    const unsigned low = min(a, b), high = max(a, b);
+    a = up ? low : high, b = up ? high : low;
+}
+// U keys of each lane, key lane + 64 u of them all, in order: Batcher's bitonic network, whose steps of 64 and more stay in a lane
+template <int U>
+__device__ __forceinline__ void sort_keys(unsigned (&key)[U], int lane) {
+#pragma unroll
+    for (int len = 2; len <= 64 * U; len <<= 1)
+#pragma unroll
+        for (int step = len >> 1; step > 0; step >>= 1) {
+            if (step >= 64) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if ((u & (step / 64)) == 0) in_order(key[u], key[u | (step / 64)], ((64 * u) & len) == 0);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const unsigned other = (unsigned)__shfl_xor((int)key[u], step);
+                    const bool up = ((lane + 64 * u) & len) == 0, first = (lane & step) == 0;
+                    key[u] = up == first ? min(key[u], other) : max(key[u], other);
+                }
+            }
+        }
+}
+
+// The lists of the piece's tokens, a group to a workgroup, whose wavefronts take a token after another, with up to U entries to a lane.  Entries are put in
+// order (of word, then of place among the token's entries): up to 64 by the number of smaller ones, more by a sorting network (640 tokens, us of the launch, with 128,
+// 256 and 1024 entries 9.5, 18.9 and 151 by numbers of smaller ones, 8.2, 13.2 and 44.9 so).  Those of one word become one with the sum of their probabilities.  Then the
+// group's words are counted by bucket, and put there.
 // write_labels: the tokens have not been looked at before (labels).
 // Few tokens: groups of 8, so that more compute units have one (200 tokens of 100 entries: 16.4 us with groups of 32, 8.0 so).
 constexpr int group_tokens(TileShape s) { return s == TILE_256 ? 32 : 8; }
@@ -233,6 +261,7 @@ __global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_ke
     const int threads = THREADS, waves = WAVES, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     int* count = reinterpret_cast<int*>(smem);                                              // [buckets]
     unsigned* key = reinterpret_cast<unsigned*>(smem) + up4(k.buckets) + 3 * SIZE * wv;    // [SIZE] of this wavefront: word, place among the entries
+    float* value = reinterpret_cast<float*>(key);                                           // or its logits, as they came
     unsigned* sorted = key + SIZE;                                                          // the same in their order
     float* z = reinterpret_cast<float*>(key + 2 * SIZE);                                    // logits less the largest, over the temperature
     __shared__ int sums[16], listed[GROUP];
@@ -262,33 +291,42 @@ __global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_ke
             const int l = group0 + wv + (r0 + r) * WAVES;
             const int64_t list = (int64_t)l * k.top;
             float most = -__builtin_inff();
-            int n = 0, rank[U];
+            int n = 0;
             unsigned mine[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const bool in = label_counts(y[r][u], h.vocab) && v[r][u] != -__builtin_inff();
-                key[lane + 64 * u] = mine[u] = in ? (unsigned)y[r][u] << 10 | (unsigned)(lane + 64 * u) : ~0u;
+                mine[u] = in ? (unsigned)y[r][u] << 10 | (unsigned)(lane + 64 * u) : ~0u;
                 most = in ? fmaxf(most, v[r][u]) : most;
                 n += __popcll(__ballot(in));
-                rank[u] = 0;
+                if constexpr (U == 1) key[lane] = mine[u];
+                else value[lane + 64 * u] = v[r][u];
             }
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
             wave_sync();
+            // (what does not count is behind all that does)
+            if constexpr (U == 1) {
+                int rank = 0;
 #pragma unroll 2
-            for (int j = 0; j < k.top; j += 4) {
-                const uintx4 other = *reinterpret_cast<const uintx4*>(key + j);
+                for (int j = 0; j < k.top; j += 4) {
+                    const uintx4 other = *reinterpret_cast<const uintx4*>(key + j);
 #pragma unroll
-                for (int o = 0; o < 4; ++o)
-#pragma unroll
-                    for (int u = 0; u < U; ++u) rank[u] += other[o] < mine[u] ? 1 : 0;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (rank[u] < n) {          // (what does not count is behind all that does)
-                    sorted[rank[u]] = mine[u];
-                    z[rank[u]] = (v[r][u] - most) * h.inv_t;
+                    for (int o = 0; o < 4; ++o) rank += other[o] < mine[0] ? 1 : 0;
                 }
+                if (rank < n) {
+                    sorted[rank] = mine[0];
+                    z[rank] = (v[r][0] - most) * h.inv_t;
+                }
+            } else {
+                sort_keys(mine, lane);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (lane + 64 * u < n) {
+                        sorted[lane + 64 * u] = mine[u];
+                        z[lane + 64 * u] = (value[mine[u] & 1023] - most) * h.inv_t;
+                    }
+            }
             wave_sync();
             float total = 0.f;
             for (int i = lane; i < n; i += 64) total += expf(z[i]);
@@ -997,7 +1035,8 @@ static hipError_t launch_lists_for(const HeadDev& h, int first, int rows, int64_
 static hipError_t launch_lists(const HeadDev& h, int first, int rows, int64_t* write_labels, hipStream_t st) {
     const int top = h.top.top;
     return top <= 64 ? launch_lists_for<1>(h, first, rows, write_labels, st) : top <= 128 ? launch_lists_for<2>(h, first, rows, write_labels, st)
-         : top <= 256 ? launch_lists_for<4>(h, first, rows, write_labels, st) : launch_lists_for<16>(h, first, rows, write_labels, st);
+         : top <= 256 ? launch_lists_for<4>(h, first, rows, write_labels, st) : top <= 512 ? launch_lists_for<8>(h, first, rows, write_labels, st)
+         : launch_lists_for<16>(h, first, rows, write_labels, st);
 }
 
 static int head_run(const psgd_head_desc* s, const HeadTeacher* teacher, bool gradients, void* workspace, void* stream, const void* x, const void* w, const int64_t* labels,

@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 
 # (tokens, d, vocab, top): one word, all words, more entries than words, odd sizes, tile borders, several tiles and splits, the most entries
 SIZES = [(1, 8, 1, 1), (1, 1, 2, 2), (3, 64, 255, 9), (2, 515, 256, 64), (64, 72, 257, 20), (65, 64, 1000, 65), (130, 40, 512, 300), (257, 200, 1031, 7),
-         (300, 520, 33, 40), (513, 264, 300, 3), (40, 1032, 5003, 1024), (700, 136, 900, 33)]
+         (300, 520, 33, 40), (513, 264, 300, 3), (40, 1032, 5003, 1024), (700, 136, 900, 33), (45, 64, 3000, 256),
+         (33, 72, 2000, 257), (50, 64, 1500, 512), (1100, 64, 700, 513)]
 
 
 def inputs(tokens, d, vocab, top, dtype, seed, masked=0.2, ragged=0.2, extra=8, t_dtype=torch.float32, distinct=True):
