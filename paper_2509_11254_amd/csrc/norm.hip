@@ -4,7 +4,7 @@
 //   u = (s - mean) r,  y = u w + b
 //   g = dy w,  ds = r (g - sum_c g / n - u sum_c(g u) / n) (+ the gradient that comes past the norm),  dw = sum_rows dy u,  db = sum_rows dy
 //
-// A row is in the registers of one wavefront or of four to sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
+// A row is in the registers of one wavefront (several narrow ones are) or of four to sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
 // first mean is subtracted, and corrected by what is left of the mean in that: a row far from zero loses nothing to it.
 //
 // Backward, a workgroup goes through rows that are the grid apart and keeps its columns' sums of dy u and dy in registers, in fp32; it
@@ -84,17 +84,43 @@ __device__ __forceinline__ void load_param(const NormParam& p, int col, int cols
     }
 }
 
-// Threads of a workgroup: WAVES to a row, and where that is one, four rows at a time.
+// Threads of a workgroup: WAVES to a row, and where that is one, four wavefronts with a row each, or with 64 / LANES rows.
 template <int WAVES> constexpr int kNormThreads = WAVES == 1 ? 256 : 64 * WAVES;
-template <int WAVES> constexpr int kNormRows = WAVES == 1 ? 4 : 1;
+template <int WAVES, int LANES> constexpr int kNormRows = WAVES == 1 ? 256 / LANES : 1;
+
+// The sum over LANES lanes next to each other, in all of them: lane ^ 1, lane ^ 2, the other four of eight, the other eight of sixteen, the other row of two, the
+// other half.  (In registers; by way of LDS each step waits for it:
+// 60000 x 512 in bf16, forward, 27.1 us in place of 24.2.  Not in the backward pass, where two sums hide each other's waits: 8192 x 11008 121 us in place of 98.)
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    auto from = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    v += from(v, std::integral_constant<int, 0xB1>{});
+    v += from(v, std::integral_constant<int, 0x4E>{});
+    if constexpr (LANES > 4) v += from(v, std::integral_constant<int, 0x141>{});
+    if constexpr (LANES > 8) v += from(v, std::integral_constant<int, 0x140>{});
+    if constexpr (LANES > 16) {
+        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+    }
+    if constexpr (LANES > 32) {
+        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+    }
+    return v;
+}
 
 // sums over a row's lanes; `shared`: two sets of [K][WAVES], used in turn, so that one barrier is enough
-template <int WAVES, int K>
+template <int WAVES, int LANES, bool REGISTERS, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float* shared, int& turn) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+        if constexpr (REGISTERS) {
+            v[k] = lanes_sum<LANES>(v[k]);
+        } else {
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) v[k] += __shfl_xor(v[k], d);
+            for (int d = LANES / 2; d > 0; d >>= 1) v[k] += __shfl_xor(v[k], d);
+        }
+    }
     if constexpr (WAVES > 1) {
         float* to = shared + turn * 2 * WAVES;
         turn ^= 1;
@@ -117,32 +143,32 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
     return a * b;
 }
 
-template <class T, int WAVES, int PIECES, bool ADD, bool STREAM>
+template <class T, int WAVES, int PIECES, int LANES, bool ADD, bool STREAM>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
     constexpr int N = kPiece<T>;
     __shared__ float shared[4 * WAVES];
     int turn = 0;
-    const int at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, group = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int at = WAVES == 1 ? threadIdx.x % LANES : threadIdx.x, group = WAVES == 1 ? threadIdx.x / LANES : 0;
     const float inv_n = 1.f / (float)a.cols;
     float w[PIECES][N], b[PIECES][N];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int col = N * (at + 64 * WAVES * i);
+        const int col = N * (at + LANES * WAVES * i);
         load_param<N>(a.w, col, a.cols, 1.f, w[i]);
         load_param<N>(a.b, col, a.cols, 0.f, b[i]);
     }
-    const int64_t step = (int64_t)gridDim.x * kNormRows<WAVES>;
+    const int64_t step = (int64_t)gridDim.x * kNormRows<WAVES, LANES>;
     uintx4 raw[PIECES], raw_add[PIECES];
     ActPlace p[PIECES];
     auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
+            p[i].row = row, p[i].col = N * (at + LANES * WAVES * i), p[i].in = p[i].col < a.cols;
             raw[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_x, p[i]);
             if constexpr (ADD) raw_add[i] = load_raw<STREAM>(static_cast<const T*>(a.add), a.ld_add, p[i]);
         }
     };
-    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group;
+    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES, LANES> + group;
     if (row < a.rows) fetch(row);
     for (; row < a.rows; row += step) {
         float v[PIECES][N], sum[1] = {0.f};
@@ -165,7 +191,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
         if (row + step < a.rows) fetch(row + step);     // (the next row is on its way while this one is added up)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) p[i].row = row;
-        row_sums<WAVES>(sum, shared, turn);
+        row_sums<WAVES, LANES, true>(sum, shared, turn);
         const float first = rounded_product(sum[0], inv_n);
         float rest[2] = {0.f, 0.f};
 #pragma unroll
@@ -181,7 +207,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
                 rest[1] = fmaf(v[i][u], v[i][u], rest[1]);
             }
         }
-        row_sums<WAVES>(rest, shared, turn);
+        row_sums<WAVES, LANES, true>(rest, shared, turn);
         const float more = rounded_product(rest[0], inv_n);
         float var = fmaf(rest[1], inv_n, -more * more);
         var = var < 0.f ? 0.f : var;
@@ -248,7 +274,7 @@ __device__ __forceinline__ void norm_columns(const NormGradDev& a, int block) {
     }
 }
 
-template <class T, int WAVES, int PIECES, bool PAST, bool STREAM>
+template <class T, int WAVES, int PIECES, int LANES, bool PAST, bool STREAM>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(NormGradDev a) {
     constexpr int N = kPiece<T>;
     if constexpr (!STREAM)
@@ -258,30 +284,30 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
         }
     __shared__ float shared[4 * WAVES];
     int turn = 0;
-    const int at = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, group = WAVES == 1 ? threadIdx.x >> 6 : 0;
+    const int at = WAVES == 1 ? threadIdx.x % LANES : threadIdx.x, group = WAVES == 1 ? threadIdx.x / LANES : 0;
     const float inv_n = 1.f / (float)a.cols;
     float w[PIECES][N], dw[PIECES][N], db[PIECES][N];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        load_param<N>(a.w, N * (at + 64 * WAVES * i), a.cols, 1.f, w[i]);
+        load_param<N>(a.w, N * (at + LANES * WAVES * i), a.cols, 1.f, w[i]);
 #pragma unroll
         for (int u = 0; u < N; ++u) dw[i][u] = db[i][u] = 0.f;
     }
-    const int64_t step = (int64_t)a.row_blocks * kNormRows<WAVES>;
+    const int64_t step = (int64_t)a.row_blocks * kNormRows<WAVES, LANES>;
     uintx4 raw_x[PIECES], raw_dy[PIECES], raw_past[PIECES];
     floatx2 stats = {0.f, 0.f};
     ActPlace p[PIECES];
     auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            p[i].row = row, p[i].col = N * (at + 64 * WAVES * i), p[i].in = p[i].col < a.cols;
+            p[i].row = row, p[i].col = N * (at + LANES * WAVES * i), p[i].in = p[i].col < a.cols;
             raw_x[i] = load_raw<STREAM>(static_cast<const T*>(a.x), a.ld_x, p[i]);
             raw_dy[i] = load_raw<STREAM>(static_cast<const T*>(a.dy), a.ld_dy, p[i]);
             if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_past, p[i]);
         }
         stats = as_global(a.stats)[row];
     };
-    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES> + group;
+    int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES, LANES> + group;
     if (row < a.rows) fetch(row);
     for (; row < a.rows; row += step) {
         const floatx2 st = stats;
@@ -307,7 +333,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) past[i] = raw_past[i];
         if (row + step < a.rows) fetch(row + step);     // (the next row is on its way while this one is added up)
-        row_sums<WAVES>(sums, shared, turn);
+        row_sums<WAVES, LANES, false>(sums, shared, turn);
         const float c1 = sums[0] * inv_n, c2 = sums[1] * inv_n;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -323,16 +349,22 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
         }
     }
     if (!a.part) return;
-    constexpr int SPAN = 64 * WAVES * PIECES * N;
-    if constexpr (WAVES == 1) {         // the four rows' sums, in their order
+    constexpr int SPAN = LANES * WAVES * PIECES * N;
+    if constexpr (WAVES == 1) {         // the sums of a wavefront's rows, and then the four wavefronts' in their order
         __shared__ float joined[2 * SPAN];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int d = 32; d >= LANES; d >>= 1) dw[i][k] += __shfl_xor(dw[i][k], d), db[i][k] += __shfl_xor(db[i][k], d);
         for (int from = 0; from < 4; ++from) {
-            if (group == from)
+            if ((int)(threadIdx.x >> 6) == from && (threadIdx.x & 63) < LANES)
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i)
 #pragma unroll
                     for (int k = 0; k < N; ++k) {
-                        const int c = N * (at + 64 * i) + k;
+                        const int c = N * (at + LANES * i) + k;
                         joined[c] = from ? joined[c] + dw[i][k] : dw[i][k];
                         joined[SPAN + c] = from ? joined[SPAN + c] + db[i][k] : db[i][k];
                     }
@@ -347,7 +379,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
             for (int k = 0; k < N; k += 4) {
-                const int c = N * (at + 64 * WAVES * i) + k;
+                const int c = N * (at + LANES * WAVES * i) + k;
                 if (c >= a.cols) break;         // (the rows of `part` are a multiple of 8 long)
                 PSGD_GLOBAL float* to = as_global(a.part) + (int64_t)blockIdx.x * 2 * a.ldp + c;
                 *reinterpret_cast<PSGD_GLOBAL floatx4*>(to) = floatx4{dw[i][k], dw[i][k + 1], dw[i][k + 2], dw[i][k + 3]};
@@ -381,10 +413,12 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int64
 // Wavefronts to a row and pieces to a lane.  One wavefront needs no barrier, and has a row of up to four pieces to a lane; wider rows have four wavefronts
 // or eight with as few pieces as do (16384 x 4096 with addend, in us, of (4, 2), (8, 1), (2, 4), each with its best grid: forward 90.0, 90.7, 92.9, backward 95.8, 90.8,
 // 98.9; 8192 x 8192 of (4, 4), (8, 2), (16, 1): 93.8, 91.2, 106.4, 96.2, 93.3, 93.2; 8192 x 11008 without one of (8, 3), (16, 2): 65.9, 95.4, 99.0, 167;
-// 16384 x 2048 of (1, 4), (2, 2), (4, 1): 46.2, 46.6, 47.2, 54.0, 54.7, 52.2).
-struct NormShape { int waves, pieces; };
+// 16384 x 2048 of (1, 4), (2, 2), (4, 1): 46.2, 46.6, 47.2, 54.0, 54.7, 52.2).  Rows of up to 512 bytes lie beside each other in a wavefront (60000 rows in bf16, forward and
+// backward, in us, with a wavefront each and so: of 64 columns 21.7 and 32.8, 7.9 and 12.9; of 256 22.9 and 33.8, 13.0 and 23.7).
+struct NormShape { int waves, pieces, lanes = 64; };
 static NormShape norm_variant(int64_t cols, int dtype, bool backward) {
     const int n = (int)((cols + (dtype == PSGD_F32 ? 3 : 7)) / (dtype == PSGD_F32 ? 4 : 8));
+    if (n <= 32) return {1, 1, n <= 8 ? 8 : n <= 16 ? 16 : 32};
     if (n <= 256) return {1, (n + 63) / 64};
     if (n <= 512) return backward ? NormShape{8, 1} : NormShape{4, 2};
     if (n <= 2048) return {8, (n + 511) / 512};
@@ -394,7 +428,7 @@ static NormShape norm_variant(int64_t cols, int dtype, bool backward) {
 // 100.5 us, without 60.1, 47.1, 51.0).  Backward, one to a compute unit, or two of one wavefront to a row: each has its columns' sums written and read (16384 x 4096 with 256, 512 and
 // 1024: 90.8, 98.4 and 102.8 us).
 static int norm_blocks(int64_t rows, const NormShape& v, int most) {
-    const int per = v.waves == 1 ? 4 : 1;
+    const int per = v.waves == 1 ? 256 / v.lanes : 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, most));
 }
 static int forward_blocks(const NormShape& v, bool add) { return add || v.waves >= 8 ? 512 : 1024; }
@@ -413,10 +447,15 @@ static bool bad_place(const RowArea& out, const RowArea& in) {
     return overlap(out, in) && !(out.ptr == in.ptr && (out.stride == in.stride || out.rows == 1) && out.width == in.width);
 }
 
-// launch(waves, pieces) with constants
+// launch(waves, pieces, lanes) with constants
 template <class T, bool BACKWARD, class F>
 static hipError_t norm_dispatch(const NormShape& v, F launch) {
-#define PSGD_SHAPE(W, P) if (v.waves == W && v.pieces == P) return launch(std::integral_constant<int, W>{}, std::integral_constant<int, P>{})
+#define PSGD_LANES(W, P, L) \
+    if (v.waves == W && v.pieces == P && v.lanes == L) return launch(std::integral_constant<int, W>{}, std::integral_constant<int, P>{}, std::integral_constant<int, L>{})
+#define PSGD_SHAPE(W, P) PSGD_LANES(W, P, 64)
+    PSGD_LANES(1, 1, 8);
+    PSGD_LANES(1, 1, 16);
+    PSGD_LANES(1, 1, 32);
     PSGD_SHAPE(1, 1);
     PSGD_SHAPE(1, 2);
     PSGD_SHAPE(1, 3);
@@ -431,22 +470,23 @@ static hipError_t norm_dispatch(const NormShape& v, F launch) {
         PSGD_SHAPE(16, 4);
     }
 #undef PSGD_SHAPE
+#undef PSGD_LANES
     return hipErrorInvalidValue;
 }
 
 template <class T, bool ADD, bool STREAM>
 static hipError_t launch_norm_as(const NormDev& a, const NormShape& v, hipStream_t st) {
     const int blocks = norm_blocks(a.rows, v, forward_blocks(v, ADD));
-    return norm_dispatch<T, false>(v, [&](auto waves, auto pieces) {
-        hipLaunchKernelGGL((norm_kernel<T, waves.value, pieces.value, ADD, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
+    return norm_dispatch<T, false>(v, [&](auto waves, auto pieces, auto lanes) {
+        hipLaunchKernelGGL((norm_kernel<T, waves.value, pieces.value, lanes.value, ADD, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
         return hipGetLastError();
     });
 }
 template <class T, bool PAST, bool STREAM>
 static hipError_t launch_backward_as(const NormGradDev& a, const NormShape& v, hipStream_t st) {
     const int per = 4 * kPiece<T>, blocks = a.row_blocks + (a.dw || a.db ? (a.cols + per - 1) / per : 0);
-    return norm_dispatch<T, true>(v, [&](auto waves, auto pieces) {
-        hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, PAST, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
+    return norm_dispatch<T, true>(v, [&](auto waves, auto pieces, auto lanes) {
+        hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, lanes.value, PAST, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
         return hipGetLastError();
     });
 }

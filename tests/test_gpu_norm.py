@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 # one column, less than a piece, odd sizes; the borders of one, four and sixteen wavefronts to a row in either type; many rows
 SIZES = [(1, 1), (1, 8), (3, 31), (2, 33), (5, 515), (37, 64), (9, 1024), (7, 1025), (6, 2049), (4, 4096), (5, 4097), (3, 8200), (2, 16384), (1030, 40),
-         (5000, 136), (4099, 1032)]
+         (5000, 136), (4099, 1032), (1100, 64), (1501, 250), (1201, 120)]
 # A row's sums are 32 terms on a lane after each other, then 6 + 16 steps over lanes and wavefronts: an error below 64 roundings of the terms' magnitudes
 STEPS = 64 * 2.0 ** -24
 
