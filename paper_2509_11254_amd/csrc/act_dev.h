@@ -1,6 +1,8 @@
-// Activations in kernels that read and write them piece by piece (act.hip, norm.hip), and the values of 8-bit checkpoints.
+// Activations in kernels that read and write them piece by piece (act.hip, norm.hip, expert.hip, head.hip), and the values of 8-bit checkpoints.
 #pragma once
 #include "psgd_dev.h"
+
+#include <type_traits>
 
 namespace psgd {
 
@@ -56,6 +58,28 @@ __device__ __forceinline__ void store_piece(T* x, int64_t ld, const ActPlace& p,
             if (p.col + u < cols) at[u] = (T)v[u];
     }
 }
+
+// What join makes of LANES lanes next to each other, in all of them: lane ^ 1, lane ^ 2, the other four of eight, the other eight of sixteen, the other row
+// of two, the other half.  (In registers; by way of LDS each step waits for it: 60000 rows of 512 in bf16 normalised, 27.1 us in place of 24.2.)
+template <int LANES, class F>
+__device__ __forceinline__ float lanes_join(float v, F join) {
+    auto from = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    v = join(v, from(v, std::integral_constant<int, 0xB1>{}));
+    v = join(v, from(v, std::integral_constant<int, 0x4E>{}));
+    if constexpr (LANES > 4) v = join(v, from(v, std::integral_constant<int, 0x141>{}));
+    if constexpr (LANES > 8) v = join(v, from(v, std::integral_constant<int, 0x140>{}));
+    if constexpr (LANES > 16) {
+        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join(__uint_as_float(two[0]), __uint_as_float(two[1]));
+    }
+    if constexpr (LANES > 32) {
+        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join(__uint_as_float(two[0]), __uint_as_float(two[1]));
+    }
+    return v;
+}
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) { return lanes_join<LANES>(v, [](float a, float b) { return a + b; }); }
+template <int LANES> __device__ __forceinline__ float lanes_max(float v) { return lanes_join<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
 
 // four codes to a word, and their group's scale
 template <int W> struct ActCodes { unsigned w[W]; float scale; };

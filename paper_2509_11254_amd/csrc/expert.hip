@@ -149,23 +149,24 @@ struct RowsDev {
     float* dweight;         // nullable
 };
 
-constexpr int kRowWaves = kThreads / 64, kRowPieces = 4;
-
-// row of choice i; -1: none
+// row of choice i; -1: none.  LANES: those of a wavefront that ask for the same
+template <int LANES>
 __device__ __forceinline__ int row_of(const RowsDev& a, int64_t i) {
-    const int p = as_global(a.place)[i];
-    return __builtin_amdgcn_readfirstlane((unsigned)p < (unsigned)a.n ? p : -1);
+    const int p = as_global(a.place)[i], row = (unsigned)p < (unsigned)a.n ? p : -1;
+    return LANES == 64 ? __builtin_amdgcn_readfirstlane(row) : row;
 }
 
 // (A wavefront to a token, with two, four or eight of its rows at a time, reads dY once, which comes from the caches here, and is slower: gradients of 16384 tokens of eight
 // rows of 2048 in bf16 200 us so, 5.7 TB/s, and 226 to 233 us; 8192 tokens of two rows of 4096 53, and 60 to 63.  Nor does a smaller grid gain anything: 212 to 217 us.)
 // a wavefront to each choice: X[t] to its row (SCALE: times its weight, and the dot product with Ys' row)
-template <class T, bool SCALE, bool DOT, bool STREAM>
+// LANES: of a choice, 16 or 32 where a row has no more pieces; PIECES: of a lane at a time (16384 x 8 choices, rows of 64, 256 and 512 in bf16, gradients: 76, 80 and 88 us with
+// (64, 4) for all, 11, 29 and 57 so).
+template <class T, int LANES, int PIECES, bool SCALE, bool DOT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_rows_kernel(RowsDev a) {
-    constexpr int N = kPiece<T>;
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = (int64_t)blockIdx.x * kRowWaves + (threadIdx.x >> 6); i < a.n; i += (int64_t)gridDim.x * kRowWaves) {
-        const int row = row_of(a, i);
+    constexpr int N = kPiece<T>, ROWS = kThreads / LANES;
+    const int lane = threadIdx.x % LANES;
+    for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; i < a.n; i += (int64_t)gridDim.x * ROWS) {
+        const int row = row_of<LANES>(a, i);
         if (row < 0) {
             if (DOT && lane == 0) as_global(a.dweight)[i] = 0.f;
             continue;
@@ -173,18 +174,18 @@ __global__ __launch_bounds__(kThreads) void expert_rows_kernel(RowsDev a) {
         const int64_t t = (unsigned)i / (unsigned)a.slots;
         const float w = SCALE && a.weight ? as_global(a.weight)[i] : 1.f;
         float dot = 0.f;
-        for (int c0 = 0; c0 < a.cols; c0 += kRowPieces * 64 * N) {
-            uintx4 raw[kRowPieces], raw_y[kRowPieces];
-            ActPlace p[kRowPieces];
+        for (int c0 = 0; c0 < a.cols; c0 += PIECES * LANES * N) {
+            uintx4 raw[PIECES], raw_y[PIECES];
+            ActPlace p[PIECES];
 #pragma unroll
-            for (int k = 0; k < kRowPieces; ++k) {
-                p[k].row = t, p[k].col = c0 + N * (lane + 64 * k), p[k].in = p[k].col < a.cols;
+            for (int k = 0; k < PIECES; ++k) {
+                p[k].row = t, p[k].col = c0 + N * (lane + LANES * k), p[k].in = p[k].col < a.cols;
                 raw[k] = load_raw<false>(static_cast<const T*>(a.dy), a.ld_dy, p[k]);
                 p[k].row = row;
                 if constexpr (DOT) raw_y[k] = load_raw<STREAM>(static_cast<const T*>(a.in), a.ld_in, p[k]);
             }
 #pragma unroll
-            for (int k = 0; k < kRowPieces; ++k) {
+            for (int k = 0; k < PIECES; ++k) {
                 float v[N];
                 if (!SCALE && p[k].col + N <= a.cols) {         // (as it is)
                     st_act<STREAM>(reinterpret_cast<PSGD_GLOBAL uintx4*>(as_global(static_cast<T*>(a.out)) + p[k].row * a.ld_out + p[k].col), raw[k]);
@@ -208,23 +209,22 @@ __global__ __launch_bounds__(kThreads) void expert_rows_kernel(RowsDev a) {
             }
         }
         if constexpr (DOT) {
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+            dot = lanes_sum<LANES>(dot);
             if (lane == 0) as_global(a.dweight)[i] = dot;
         }
     }
 }
 
-// a wavefront to each token and 64 pieces of its columns: the sum of its rows
-template <class T, bool STREAM>
+// a wavefront to each token and 64 pieces of its columns, or 16 or 32 lanes to a token: the sum of its rows
+template <class T, int LANES, bool STREAM>
 __global__ __launch_bounds__(kThreads) void expert_combine_kernel(RowsDev a, int parts) {
-    constexpr int N = kPiece<T>, AHEAD = 4;
-    const int lane = threadIdx.x & 63;
+    constexpr int N = kPiece<T>, AHEAD = 4, ROWS = kThreads / LANES;
+    const int lane = threadIdx.x % LANES;
     const int64_t all = a.tokens * parts;
-    for (int64_t j = (int64_t)blockIdx.x * kRowWaves + (threadIdx.x >> 6); j < all; j += (int64_t)gridDim.x * kRowWaves) {
+    for (int64_t j = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; j < all; j += (int64_t)gridDim.x * ROWS) {
         const int64_t t = j / parts;
         ActPlace p;
-        p.col = N * ((int)(j - t * parts) * 64 + lane);
+        p.col = N * ((int)(j - t * parts) * LANES + lane);
         float sum[N];
 #pragma unroll
         for (int u = 0; u < N; ++u) sum[u] = 0.f;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void expert_combine_kernel(RowsDev a, int
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const int64_t i = t * a.slots + s0 + k;
-                const int row = s0 + k < a.slots ? row_of(a, i) : -1;
+                const int row = s0 + k < a.slots ? row_of<LANES>(a, i) : -1;
                 there[k] = row >= 0;
                 w[k] = there[k] && a.weight ? as_global(a.weight)[i] : 1.f;
                 p.row = row, p.in = there[k] && p.col < a.cols;
@@ -277,19 +277,27 @@ static int rows_shape(int64_t tokens, int64_t slots, int64_t cols) {
     if (tokens < 0 || slots < 1 || cols < 1 || tokens > kMaxExtent || slots > kMaxExtent || tokens * slots > kMaxExtent || cols > kMaxLd) return PSGD_E_SHAPE;
     return PSGD_OK;
 }
-static unsigned row_blocks(int64_t waves) { return (unsigned)std::min<int64_t>((waves + kRowWaves - 1) / kRowWaves, kRowBlocks); }
+static unsigned row_blocks(int64_t rows, int lanes) { return (unsigned)std::min<int64_t>((rows * lanes + kThreads - 1) / kThreads, kRowBlocks); }
+static int row_pieces(int64_t cols, int dtype) { return (int)((cols + (dtype == PSGD_F32 ? 3 : 7)) / (dtype == PSGD_F32 ? 4 : 8)); }
 static bool same_place(const RowArea& a, const RowArea& b) { return a.ptr == b.ptr && (a.stride == b.stride || a.rows == 1) && a.width == b.width; }
 
-template <bool SCALE, bool DOT>
-static int launch_rows(const RowsDev& a, int dtype, hipStream_t st) {
-    const int64_t bytes = a.n * a.cols * (dtype == PSGD_F32 ? 4 : 2) * (DOT ? 2 : 1);
-    const dim3 blocks(row_blocks(a.n));
+template <class T, bool SCALE, bool DOT>
+static int launch_rows_as(const RowsDev& a, int pieces, hipStream_t st) {
+    const bool stream_it = a.n * a.cols * (int64_t)sizeof(T) * (DOT ? 2 : 1) >= kRowStream;
     forget_errors();
-#define PSGD_ROWS(T, STREAM) hipLaunchKernelGGL((expert_rows_kernel<T, SCALE, DOT, STREAM>), blocks, dim3(kThreads), 0, st, a)
-    if (dtype == PSGD_F32) { if (bytes >= kRowStream) PSGD_ROWS(float, true); else PSGD_ROWS(float, false); }
-    else                   { if (bytes >= kRowStream) PSGD_ROWS(bf16_t, true); else PSGD_ROWS(bf16_t, false); }
+#define PSGD_ROWS(LANES, PIECES, STREAM) \
+    hipLaunchKernelGGL((expert_rows_kernel<T, LANES, PIECES, SCALE, DOT, STREAM>), dim3(row_blocks(a.n, LANES)), dim3(kThreads), 0, st, a)
+    if (pieces <= 16) { if (stream_it) PSGD_ROWS(16, 1, true); else PSGD_ROWS(16, 1, false); }
+    else if (pieces <= 32) { if (stream_it) PSGD_ROWS(32, 1, true); else PSGD_ROWS(32, 1, false); }
+    else if (pieces <= 64) { if (stream_it) PSGD_ROWS(64, 1, true); else PSGD_ROWS(64, 1, false); }
+    else { if (stream_it) PSGD_ROWS(64, 4, true); else PSGD_ROWS(64, 4, false); }
 #undef PSGD_ROWS
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
+}
+template <bool SCALE, bool DOT>
+static int launch_rows(const RowsDev& a, int dtype, hipStream_t st) {
+    const int pieces = row_pieces(a.cols, dtype);
+    return dtype == PSGD_F32 ? launch_rows_as<float, SCALE, DOT>(a, pieces, st) : launch_rows_as<bf16_t, SCALE, DOT>(a, pieces, st);
 }
 
 }  // namespace psgd
@@ -358,15 +366,17 @@ int psgd_expert_combine(void* stream, int64_t tokens, int64_t slots, int64_t col
     RowsDev a = {};
     a.tokens = tokens, a.n = n, a.slots = (int)slots, a.cols = (int)cols, a.place = place, a.weight = weight;
     a.in = ys, a.ld_in = ld_ys, a.out = y, a.ld_out = ld_y;
-    const int width = 64 * (dtype == PSGD_F32 ? kPiece<float> : kPiece<bf16_t>), parts = (int)((cols + width - 1) / width);
-    const dim3 blocks(row_blocks(tokens * parts));
+    const int pieces = row_pieces(cols, dtype), lanes = pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64, parts = (pieces + lanes - 1) / lanes;
+    const dim3 blocks(row_blocks(tokens * parts, lanes));
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const bool stream_it = n * cols * size >= kRowStream;
     forget_errors();
-#define PSGD_ROWS(T, STREAM) hipLaunchKernelGGL((expert_combine_kernel<T, STREAM>), blocks, dim3(kThreads), 0, st, a, parts)
-    if (dtype == PSGD_F32) { if (stream_it) PSGD_ROWS(float, true); else PSGD_ROWS(float, false); }
-    else                   { if (stream_it) PSGD_ROWS(bf16_t, true); else PSGD_ROWS(bf16_t, false); }
+#define PSGD_ROWS(T, LANES, STREAM) hipLaunchKernelGGL((expert_combine_kernel<T, LANES, STREAM>), blocks, dim3(kThreads), 0, st, a, parts)
+#define PSGD_ROWS_LANES(T, STREAM) do { if (lanes == 16) PSGD_ROWS(T, 16, STREAM); else if (lanes == 32) PSGD_ROWS(T, 32, STREAM); else PSGD_ROWS(T, 64, STREAM); } while (0)
+    if (dtype == PSGD_F32) { if (stream_it) PSGD_ROWS_LANES(float, true); else PSGD_ROWS_LANES(float, false); }
+    else                   { if (stream_it) PSGD_ROWS_LANES(bf16_t, true); else PSGD_ROWS_LANES(bf16_t, false); }
 #undef PSGD_ROWS
+#undef PSGD_ROWS_LANES
     return hipGetLastError() == hipSuccess ? PSGD_OK : PSGD_E_HIP;
 }
 

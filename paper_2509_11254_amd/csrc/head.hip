@@ -302,8 +302,7 @@ __global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_ke
                 if constexpr (U == 1) key[lane] = mine[u];
                 else value[lane + 64 * u] = v[r][u];
             }
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+            most = lanes_max<64>(most);
             wave_sync();
             // (what does not count is behind all that does)
             if constexpr (U == 1) {
@@ -330,8 +329,7 @@ __global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_ke
             wave_sync();
             float total = 0.f;
             for (int i = lane; i < n; i += 64) total += expf(z[i]);
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+            total = lanes_sum<64>(total);
             const float log_total = logf(total);
             int to = 0;
             for (int i0 = 0; i0 < n; i0 += 64) {
@@ -768,14 +766,12 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
     if (w0.word >= 0) join(w0.logit, 1.f, 0.f);
     for (int i = lane + 64; i < n; i += 64) join(load_word(i).logit, 1.f, 0.f);
     const float lane_most = most;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    most = lanes_max<64>(most);
     if (lane_most != most) {
         const float f = expf((lane_most - most) * inv_t);
         mine *= f, others *= f;
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d), others += __shfl_xor(others, d);
+    mine = lanes_sum<64>(mine), others = lanes_sum<64>(others);
     const float total = mine + others, log_total = logf(total), weight = h.weight ? h.weight[token] / (h.direct ? scale : h.scale[1]) : 1.f;
     struct Off { float p, u; bool small; };
     auto off = [&](const Word& w) {
@@ -790,8 +786,7 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
             // (a probability that is 0 in 32 bits has a logarithm all the same, or none)
             loss += o.small ? w.q * exp_rest(o.u) : w.q == 0.f ? o.p : o.p - w.q - w.q * o.u;
         }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+        loss = lanes_sum<64>(loss);
         if (lane == 0) h.loss[token] = loss + others / total;
     }
     if constexpr (KEEP == KEEP_NONE) return;

@@ -88,28 +88,8 @@ __device__ __forceinline__ void load_param(const NormParam& p, int col, int cols
 template <int WAVES> constexpr int kNormThreads = WAVES == 1 ? 256 : 64 * WAVES;
 template <int WAVES, int LANES> constexpr int kNormRows = WAVES == 1 ? 256 / LANES : 1;
 
-// The sum over LANES lanes next to each other, in all of them: lane ^ 1, lane ^ 2, the other four of eight, the other eight of sixteen, the other row of two, the
-// other half.  (In registers; by way of LDS each step waits for it:
-// 60000 x 512 in bf16, forward, 27.1 us in place of 24.2.  Not in the backward pass, where two sums hide each other's waits: 8192 x 11008 121 us in place of 98.)
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-    auto from = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
-    v += from(v, std::integral_constant<int, 0xB1>{});
-    v += from(v, std::integral_constant<int, 0x4E>{});
-    if constexpr (LANES > 4) v += from(v, std::integral_constant<int, 0x141>{});
-    if constexpr (LANES > 8) v += from(v, std::integral_constant<int, 0x140>{});
-    if constexpr (LANES > 16) {
-        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(two[0]) + __uint_as_float(two[1]);
-    }
-    if constexpr (LANES > 32) {
-        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(two[0]) + __uint_as_float(two[1]);
-    }
-    return v;
-}
-
 // sums over a row's lanes; `shared`: two sets of [K][WAVES], used in turn, so that one barrier is enough
+// REGISTERS: without LDS inside a wavefront.  (Not in the backward pass, where two sums hide each other's waits: 8192 x 11008 121 us in place of 98.)
 template <int WAVES, int LANES, bool REGISTERS, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float* shared, int& turn) {
 #pragma unroll

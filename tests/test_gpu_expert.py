@@ -83,7 +83,8 @@ def test_sort_no_tokens():
 
 
 # (tokens, slots, experts, cols): one piece, odd columns, several rounds of pieces
-ROWS = [(1, 1, 1, 1), (1, 8, 16, 4096), (5, 3, 2, 31), (40, 2, 8, 515), (130, 5, 4, 2056), (17, 9, 30, 5000), (1000, 4, 64, 72), (3, 2, 4, 20001)]
+ROWS = [(1, 1, 1, 1), (1, 8, 16, 4096), (5, 3, 2, 31), (40, 2, 8, 515), (130, 5, 4, 2056), (17, 9, 30, 5000), (1000, 4, 64, 72), (3, 2, 4, 20001),
+        (301, 3, 20, 64), (77, 6, 9, 128), (50, 2, 4, 131), (65, 4, 8, 512), (33, 2, 4, 257)]
 
 
 def rows_of(n, cols, dtype, seed, extra=8):
