@@ -397,7 +397,7 @@ __global__ __launch_bounds__((64 * kListWaves<U, GROUP>)) void head_top_lists_ke
 
 // The logits of the teacher's words in this tile: to their places, and out of the accumulators (minus infinity there).  32 rows at a time, through LDS, where any lane can
 // look for any word, each wavefront in a place of its own.  (8192 x 4096 x 64000, 64 entries: 40 us of 3430 more than without a teacher; one word of a row after the
-// other, sought among a lane's accumulators, took 365.  200 x 1024 x 10007, 100 entries, a quarter of them in one tile: 5 us of 23; 30 of 48.)
+// other, sought among a lane's accumulators, took 365.  200 x 1024 x 10007, 100 entries, a quarter of them in one tile: 3 us of 20; 30 of 48.)
 // Where they are is asked before the product.
 template <class T, TileShape SHAPE> struct TileListed {
     static constexpr int GROUP = group_tokens(SHAPE), SUBS = 32 / GROUP;
@@ -419,13 +419,20 @@ __device__ __forceinline__ void where_listed(TileListed<T, SHAPE>& w, const Head
 template <class T, TileShape SHAPE>
 __device__ __forceinline__ void take_listed(T& tile, const HeadTop& k, const TileListed<T, SHAPE>& w, int p0, int l0, PSGD_TLDS unsigned char* lds) {
     constexpr int COLS = 32 * T::FP, LD = COLS + 4, GROUP = group_tokens(SHAPE), SUBS = 32 / GROUP, AHEAD = 4;
+    // rounds of 64 whose loads are sent off first, where there are registers for them (a tile with a quarter of all words has four)
+    constexpr int FIRST = tile_share(SHAPE) == 1 && SHAPE != TILE_256 ? 4 : 1;
     const int lane = tile.lane;
     auto base = [&](int j, int s) { return (int64_t)(l0 + (tile.wl * T::FL + j) * 32 + s * GROUP) * k.top; };
-    unsigned first[T::FL][SUBS];
+    unsigned first[T::FL][SUBS][FIRST];
 #pragma unroll
     for (int j = 0; j < T::FL; ++j)
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) first[j][s] = w.from[j][s] + lane < w.to[j][s] ? as_global(k.flat)[base(j, s) + w.from[j][s] + lane] : 0u;
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+            for (int r = 0; r < FIRST; ++r) {
+                const int i = w.from[j][s] + 64 * r + lane;
+                first[j][s][r] = i < w.to[j][s] ? as_global(k.flat)[base(j, s) + i] : 0u;
+            }
     __syncthreads();        // (the chunks' reads are done)
     PSGD_TLDS float* mine = reinterpret_cast<PSGD_TLDS float*>(lds) + (tile.wl * T::WP + tile.wp) * 32 * LD;
 #pragma unroll
@@ -454,8 +461,9 @@ __device__ __forceinline__ void take_listed(T& tile, const HeadTop& k, const Til
                     *x = -__builtin_inff();
                 }
             };
-            take(w.from[j][s] + lane, first[j][s]);
-            for (int i0 = w.from[j][s] + 64; i0 < to; i0 += 64 * AHEAD) {
+#pragma unroll
+            for (int r = 0; r < FIRST; ++r) take(w.from[j][s] + 64 * r + lane, first[j][s][r]);
+            for (int i0 = w.from[j][s] + 64 * FIRST; i0 < to; i0 += 64 * AHEAD) {
                 unsigned e[AHEAD];
 #pragma unroll
                 for (int r = 0; r < AHEAD; ++r) e[r] = i0 + 64 * r + lane < to ? as_global(k.flat)[at + i0 + 64 * r + lane] : 0u;
@@ -705,13 +713,15 @@ __device__ __forceinline__ float exp_rest(float u) {
 // The same against a teacher: with q its probabilities, p the head's and u = log p - log q,
 //   loss = sum_v q log(q / p) = sum over the list of (p - q - q u = q (e^u - 1 - u)) + sum over the others of p,
 // of whose terms none is negative;  D = c (p - q), p - q = q (e^u - 1).  The others' D comes of their exponentials, the list's is written over it.
-template <int KEEP, int PL>
+// KEPT: rounds of 64 words of the list that a wavefront has in registers (1 for up to 64 entries: 333 x 515 x 10007, 8 entries, 8.9 us, with four 10.4; 4 for more:
+// 8192 x 464 x 1280, losses, 256 entries 30.1 us, with four 25.4)
+template <int KEEP, int PL, int KEPT>
 __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int first, int most_rows, int span) {
     __shared__ float shared[4];
     const HeadTop& k = h.top;
     const int l = blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     if (l >= (h.direct ? most_rows : min(most_rows, *h.count - first))) return;
-    const int token = h.direct ? first + l : h.rows[first + l], n = as_global(k.words)[l];
+    const int token = h.direct ? first + l : h.rows[first + l], n = __builtin_amdgcn_readfirstlane(as_global(k.words)[l]);
     const int begin = blockIdx.y * span, end = (int)min((int64_t)(blockIdx.y + 1) * span, h.ldv);
     float scale = 1.f;
     if (KEEP != KEEP_NONE && h.direct && (h.weight || (l == 0 && blockIdx.y == 0))) {
@@ -747,7 +757,18 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
         if (i < n) w = {as_global(k.logit)[base + as_global(k.place)[at]], as_global(k.q)[at], as_global(k.log_q)[at], as_global(k.word)[at]};
         return w;
     };
-    const Word w0 = load_word(lane);
+    Word kept[KEPT];
+#pragma unroll
+    for (int r = 0; r < KEPT; ++r) {
+        kept[r] = {-__builtin_inff(), 0.f, 0.f, -1};
+        if (64 * r < n) kept[r] = load_word(64 * r + lane);
+    }
+    auto for_words = [&](auto use) {
+#pragma unroll
+        for (int r = 0; r < KEPT; ++r)
+            if (64 * r < n && kept[r].word >= 0) use(kept[r]);
+        for (int i = 64 * KEPT + lane; i < n; i += 64) use(load_word(i));
+    };
     // the largest logit, and the sums of exp(logit - it) of the list and of the others
     const float inv_t = h.inv_t;
     float most = -__builtin_inff(), mine = 0.f, others = 0.f;
@@ -763,8 +784,7 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
     };
     const float2* st = h.stats + (int64_t)l * h.tiles;
     for (int i = lane; i < h.tiles; i += 64) join(st[i].x, 0.f, st[i].y);
-    if (w0.word >= 0) join(w0.logit, 1.f, 0.f);
-    for (int i = lane + 64; i < n; i += 64) join(load_word(i).logit, 1.f, 0.f);
+    for_words([&](const Word& w) { join(w.logit, 1.f, 0.f); });
     const float lane_most = most;
     most = lanes_max<64>(most);
     if (lane_most != most) {
@@ -780,12 +800,11 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
     };
     if (blockIdx.y == 0 && wv == 0) {
         float loss = 0.f;
-        for (int i = lane; i < n; i += 64) {
-            const Word w = i < 64 ? w0 : load_word(i);
+        for_words([&](const Word& w) {
             const Off o = off(w);
             // (a probability that is 0 in 32 bits has a logarithm all the same, or none)
             loss += o.small ? w.q * exp_rest(o.u) : w.q == 0.f ? o.p : o.p - w.q - w.q * o.u;
-        }
+        });
         loss = lanes_sum<64>(loss);
         if (lane == 0) h.loss[token] = loss + others / total;
     }
@@ -827,10 +846,12 @@ __global__ __launch_bounds__(kThreads) void head_top_rows_kernel(HeadDev h, int 
         // the list's, as soon as their places are written (later, they would be parts of lines that have left the caches), by the same wavefront: its stores
         // come in their order
         wave_sync();
-        if (w0.word >= v0 && w0.word < min(v0 + 512, end)) put(w0);
+#pragma unroll
+        for (int r = 0; r < KEPT; ++r)
+            if (64 * r < n && kept[r].word >= v0 && kept[r].word < min(v0 + 512, end)) put(kept[r]);
     }
     wave_sync();
-    for (int i = lane + 64; i < n; i += 64) {
+    for (int i = 64 * KEPT + lane; i < n; i += 64) {
         const Word w = load_word(i);
         if (w.word >= begin && w.word < end && ((w.word - begin) / 512) % (kThreads / 64) == wv) put(w);
     }
@@ -986,7 +1007,8 @@ static hipError_t launch_logits(const TileArgs& t, const HeadDev& h, TileShape s
 
 template <int KEEP, int PL>
 static hipError_t launch_rows_as(const HeadDev& h, int first, int rows, int span, dim3 grid, hipStream_t st) {
-    if (h.top.top) hipLaunchKernelGGL((head_top_rows_kernel<KEEP, PL>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    if (h.top.top > 64) hipLaunchKernelGGL((head_top_rows_kernel<KEEP, PL, 4>), grid, dim3(kThreads), 0, st, h, first, rows, span);
+    else if (h.top.top) hipLaunchKernelGGL((head_top_rows_kernel<KEEP, PL, 1>), grid, dim3(kThreads), 0, st, h, first, rows, span);
     else hipLaunchKernelGGL((head_rows_kernel<KEEP, PL>), grid, dim3(kThreads), 0, st, h, first, rows, span);
     return hipGetLastError();
 }
