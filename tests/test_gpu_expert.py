@@ -71,6 +71,27 @@ def test_sort_where_all_choose_one(tokens, experts):
     check_sort(sort(choice, experts), choice, experts)
 
 
+def test_sort_of_very_many():
+    """24 million choices, against torch's stable sort; and rows of the most tokens that a launch goes through more than once."""
+    tokens, slots, experts = 3000001, 8, 60
+    choice = torch.randint(-2, experts + 2, (tokens, slots), device="cuda")
+    order = sort(choice, experts)
+    flat = choice.view(-1)
+    key, want = torch.sort(torch.where((flat >= 0) & (flat < experts), flat, experts), stable=True)
+    n = int((key < experts).sum())
+    assert torch.equal(order.offsets.long(), torch.searchsorted(key, torch.arange(experts + 1, device="cuda"))) and int(order.offsets[-1]) == n
+    assert torch.equal(order.order[:n].long(), want[:n]) and (order.order[n:] == -1).all()
+    assert torch.equal(order.place.view(-1)[want[:n]].long(), torch.arange(n, device="cuda")) and (order.place.view(-1)[want[n:]] == -1).all()
+    x = torch.arange(tokens, device="cuda").float()[:, None].expand(tokens, 8).contiguous()
+    xs, y = torch.full((tokens * slots, 8), -1.0, device="cuda"), torch.empty_like(x)
+    psgd.expert_rows(x, order, xs)
+    assert torch.equal(xs[:n, 7], (want[:n] // slots).float()) and (xs[n:] == -1).all()
+    psgd.expert_combine(xs, order, y)
+    # (whole numbers below 2^24 times at most eight: exact in 32 bits or rounded once per sum)
+    there = ((choice >= 0) & (choice < experts)).sum(1)
+    assert ((y[:, 0].double() - there.double() * x[:, 0].double()).abs() <= slots * 2.0 ** -24 * 8 * tokens).all()
+
+
 def test_sort_no_tokens():
     order = psgd.expert_order_empty(0, 2, 5)
     order.offsets.fill_(9)

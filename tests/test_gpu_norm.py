@@ -198,6 +198,15 @@ def test_in_place():
     assert torch.equal(x2, total) and torch.equal(o2, y)
 
 
+def test_y_in_the_place_of_x():
+    for rows, cols, dtype in ((50, 1000, torch.bfloat16), (7, 16384, torch.float32), (999, 64, torch.bfloat16)):
+        x = padded(values(rows, cols, 1), dtype)[0]
+        y, here = torch.empty_like(x), x.clone()
+        psgd.norm(x, None, None, y)
+        psgd.norm(here, None, None, here)
+        assert torch.equal(here, y)
+
+
 def test_no_rows():
     e = torch.empty((0, 40), device="cuda")
     w, stats = torch.ones(40, device="cuda"), torch.empty((0, 2), device="cuda")
