@@ -123,6 +123,25 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
     return a * b;
 }
 
+// `otherwise` in the place of a piece's elements beyond cols (of bf16 twice)
+template <class T>
+__device__ __forceinline__ void fill_beyond(uintx4& w, const ActPlace& p, int cols, unsigned otherwise) {
+    if (p.col + kPiece<T> > cols) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if constexpr (sizeof(T) == 4) {
+                w[u] = p.col + u < cols ? w[u] : otherwise;
+            } else {
+                const unsigned in = (p.col + 2 * u < cols ? 0xffffu : 0u) | (p.col + 2 * u + 1 < cols ? 0xffff0000u : 0u);
+                w[u] = (w[u] & in) | (otherwise & ~in);
+            }
+        }
+    }
+}
+// Whether the mean of a row may leave 32 bits when it is multiplied by r.
+constexpr float kNormFar = 2.f;
+__device__ __forceinline__ bool far_from_zero(const floatx2& st) { return fabsf(st.x) * st.y > kNormFar; }
+
 template <class T, int WAVES, int PIECES, int LANES, bool ADD, bool STREAM>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
     constexpr int N = kPiece<T>;
@@ -278,6 +297,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
     floatx2 stats = {0.f, 0.f};
     ActPlace p[PIECES];
     auto fetch = [&](int64_t row) {
+        stats = as_global(a.stats)[row];        // (asked about first)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             p[i].row = row, p[i].col = N * (at + LANES * WAVES * i), p[i].in = p[i].col < a.cols;
@@ -285,7 +305,6 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
             raw_dy[i] = load_raw<STREAM>(static_cast<const T*>(a.dy), a.ld_dy, p[i]);
             if constexpr (PAST) raw_past[i] = load_raw<STREAM>(static_cast<const T*>(a.past), a.ld_past, p[i]);
         }
-        stats = as_global(a.stats)[row];
     };
     int64_t row = (int64_t)blockIdx.x * kNormRows<WAVES, LANES> + group;
     if (row < a.rows) fetch(row);
@@ -293,13 +312,18 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
         const floatx2 st = stats;
         uintx4 past[PIECES];
         float u[PIECES][N], g[PIECES][N], sums[2] = {0.f, 0.f};
+        unsigned beyond = 0;        // (beyond the columns g is 0, and u finite where the row's elements are)
+        if (far_from_zero(st)) {
+            const PSGD_GLOBAL T* first = as_global(static_cast<const T*>(a.x)) + row * a.ld_x;
+            if constexpr (sizeof(T) == 4) beyond = *reinterpret_cast<const PSGD_GLOBAL unsigned*>(first);
+            else beyond = *reinterpret_cast<const PSGD_GLOBAL unsigned short*>(first) * 0x10001u;
+        }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            clear_beyond<T>(raw_x[i], p[i], a.cols);
+            fill_beyond<T>(raw_x[i], p[i], a.cols, beyond);
             clear_beyond<T>(raw_dy[i], p[i], a.cols);
             widen<T>(raw_x[i], u[i]);
             widen<T>(raw_dy[i], g[i]);
-            // (beyond the columns g is 0; u is not, but finite where the row's are)
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 u[i][k] = (u[i][k] - st.x) * st.y;
