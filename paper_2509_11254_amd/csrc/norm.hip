@@ -5,7 +5,8 @@
 //   g = dy w,  ds = r (g - sum_c g / n - u sum_c(g u) / n) (+ the gradient that comes past the norm),  dw = sum_rows dy u,  db = sum_rows dy
 //
 // A row is in the registers of one wavefront (several narrow ones are) or of four to sixteen, 16 bytes to a lane and piece; it is read once.  The variance is taken of what is left when a
-// first mean is subtracted, and corrected by what is left of the mean in that: a row far from zero loses nothing to it.
+// first mean is subtracted, and corrected by what is left of the mean in that: a row far from zero loses nothing to it.  The backward pass is given the sum of both, rounded:
+// of rows far from zero it takes the mean of its u's and subtracts that as well.
 //
 // Backward, a workgroup goes through rows that are the grid apart and keeps its columns' sums of dy u and dy in registers, in fp32; it
 // writes them once at its end, and a second launch adds up the workgroups' sums in their order.
@@ -123,6 +124,11 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
     return a * b;
 }
 
+// A mean is kept in 32 bits, off by up to 2^-24 of itself, and so are all u's of the row by that times r: of nearer rows by 2^-23 at most, the size of u's own
+// roundings.  Of rows beyond this their mean is asked for (16384 x 4096 with addend, all rows beyond it: 118 us, otherwise 91.5; 8192 x 11008 112, 99.5).
+constexpr float kNormFar = 2.f;
+__device__ __forceinline__ bool far_from_zero(const floatx2& st) { return fabsf(st.x) * st.y > kNormFar; }
+
 // `otherwise` in the place of a piece's elements beyond cols (of bf16 twice)
 template <class T>
 __device__ __forceinline__ void fill_beyond(uintx4& w, const ActPlace& p, int cols, unsigned otherwise) {
@@ -138,9 +144,6 @@ __device__ __forceinline__ void fill_beyond(uintx4& w, const ActPlace& p, int co
         }
     }
 }
-// Whether the mean of a row may leave 32 bits when it is multiplied by r.
-constexpr float kNormFar = 2.f;
-__device__ __forceinline__ bool far_from_zero(const floatx2& st) { return fabsf(st.x) * st.y > kNormFar; }
 
 template <class T, int WAVES, int PIECES, int LANES, bool ADD, bool STREAM>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_kernel(NormDev a) {
@@ -231,22 +234,70 @@ __device__ __forceinline__ void put_sum(void* out, int dtype, int accumulate, in
     }
 }
 
-// dw and db of four pieces of columns, all rows: a lane has a piece of every 16th row of its wavefront's
+// The means of what the kept means of rows far from zero leave of their u's, 0 of others': shift[row], four rows of a wavefront at a time.
+constexpr int64_t kNormFewRows = 1024;
+template <class T, int THREADS>
+__device__ __forceinline__ void far_shifts(const NormGradDev& a, float* shift) {
+    constexpr int N = kPiece<T>, W = THREADS / 64, ROWS = 4, AHEAD = 4;
+    const int lane = threadIdx.x & 63;
+    for (int row0 = ROWS * (threadIdx.x >> 6); row0 < (int)a.rows; row0 += ROWS * W) {
+        floatx2 st[ROWS];
+        float rest[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) st[i] = as_global(a.stats)[min(row0 + i, (int)a.rows - 1)], rest[i] = 0.f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < a.cols; c0 += AHEAD * 64 * N) {
+            uintx4 raw[ROWS][AHEAD];
+            ActPlace p[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    p[j].row = min(row0 + i, (int)a.rows - 1), p[j].col = c0 + N * (lane + 64 * j), p[j].in = p[j].col < a.cols;
+                    raw[i][j] = load_raw<false>(static_cast<const T*>(a.x), a.ld_x, p[j]);
+                }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    float x[N], sum = 0.f;
+                    widen<T>(raw[i][j], x);
+                    if (p[j].col + N > a.cols)
+#pragma unroll
+                        for (int k = 0; k < N; ++k) x[k] = p[j].col + k < a.cols ? x[k] : st[i].x;
+#pragma unroll
+                    for (int k = 0; k < N; ++k) sum += x[k] - st[i].x;
+                    rest[i] += sum;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            rest[i] = lanes_sum<64>(rest[i]);
+            if (lane == 0 && row0 + i < (int)a.rows) shift[row0 + i] = far_from_zero(st[i]) ? rest[i] * st[i].y / (float)a.cols : 0.f;
+        }
+    }
+}
+
+// dw and db of four pieces of columns, all rows: a lane has a piece of every 16th row of its wavefront's.  Where rows are far from zero each workgroup reads all of
+// them once more, and its pieces of dy: the calls on such rows take longer (1000 x 515 in fp32 112 us in place of 10, 64 x 8192 49 and 9.3), the others one launch less.
 template <class T, int THREADS>
 __device__ __forceinline__ void norm_columns(const NormGradDev& a, int block) {
     constexpr int N = kPiece<T>, W = THREADS / 64;
     __shared__ float joined[W][4][2 * N];
+    __shared__ float shift[kNormFewRows];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     ActPlace p;
     p.col = N * (4 * block + (lane & 3)), p.in = p.col < a.cols;
     float s[2 * N];
 #pragma unroll
     for (int k = 0; k < 2 * N; ++k) s[k] = 0.f;
+    bool far = false;
 #pragma unroll 4
     for (int row = 16 * wv + (lane >> 2); row < (int)a.rows; row += 16 * W) {
         p.row = row;
         const uintx4 raw_x = load_raw<false>(static_cast<const T*>(a.x), a.ld_x, p), raw_dy = load_raw<false>(static_cast<const T*>(a.dy), a.ld_dy, p);
         const floatx2 st = as_global(a.stats)[row];
+        far |= far_from_zero(st);
         float u[N], g[N];
         widen<T>(raw_x, u);
         widen<T>(raw_dy, g);
@@ -254,6 +305,18 @@ __device__ __forceinline__ void norm_columns(const NormGradDev& a, int block) {
         for (int k = 0; k < N; ++k) {
             s[k] = fmaf(g[k], (u[k] - st[0]) * st[1], s[k]);
             s[N + k] += g[k];
+        }
+    }
+    if (__syncthreads_or(far)) {
+        far_shifts<T, THREADS>(a, shift);
+        __syncthreads();
+#pragma unroll 4
+        for (int row = 16 * wv + (lane >> 2); row < (int)a.rows; row += 16 * W) {
+            p.row = row;
+            float g[N];
+            widen<T>(load_raw<false>(static_cast<const T*>(a.dy), a.ld_dy, p), g);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] = fmaf(g[k], -shift[row], s[k]);
         }
     }
 #pragma unroll
@@ -273,10 +336,12 @@ __device__ __forceinline__ void norm_columns(const NormGradDev& a, int block) {
     }
 }
 
-template <class T, int WAVES, int PIECES, int LANES, bool PAST, bool STREAM>
+enum NormMode { NORM_MANY, NORM_STREAM, NORM_FEW };     // NORM_STREAM: with the non-temporal hint; NORM_FEW: sums of columns beside the rows
+template <class T, int WAVES, int PIECES, int LANES, bool PAST, NormMode MODE>
 __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(NormGradDev a) {
     constexpr int N = kPiece<T>;
-    if constexpr (!STREAM)
+    constexpr bool STREAM = MODE == NORM_STREAM;
+    if constexpr (MODE == NORM_FEW)
         if ((int)blockIdx.x >= a.row_blocks) {
             norm_columns<T, kNormThreads<WAVES>>(a, blockIdx.x - a.row_blocks);
             return;
@@ -312,8 +377,19 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
         const floatx2 st = stats;
         uintx4 past[PIECES];
         float u[PIECES][N], g[PIECES][N], sums[2] = {0.f, 0.f};
+        float shift = 0.f;          // the mean of what the kept mean leaves of the u's
         unsigned beyond = 0;        // (beyond the columns g is 0, and u finite where the row's elements are)
         if (far_from_zero(st)) {
+            float rest[1] = {0.f};
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                float x[N];
+                widen<T>(raw_x[i], x);
+#pragma unroll
+                for (int k = 0; k < N; ++k) rest[0] += p[i].col + k < a.cols ? (x[k] - st.x) * st.y : 0.f;
+            }
+            row_sums<WAVES, LANES, true>(rest, shared, turn);
+            shift = rest[0] * inv_n;
             const PSGD_GLOBAL T* first = as_global(static_cast<const T*>(a.x)) + row * a.ld_x;
             if constexpr (sizeof(T) == 4) beyond = *reinterpret_cast<const PSGD_GLOBAL unsigned*>(first);
             else beyond = *reinterpret_cast<const PSGD_GLOBAL unsigned short*>(first) * 0x10001u;
@@ -326,7 +402,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
             widen<T>(raw_dy[i], g[i]);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                u[i][k] = (u[i][k] - st.x) * st.y;
+                u[i][k] = fmaf(u[i][k] - st.x, st.y, -shift);
                 dw[i][k] = fmaf(g[i][k], u[i][k], dw[i][k]);
                 db[i][k] += g[i][k];
                 g[i][k] *= w[i][k];
@@ -352,7 +428,7 @@ __global__ __launch_bounds__(kNormThreads<WAVES>) void norm_backward_kernel(Norm
             store_piece<STREAM>(static_cast<T*>(a.dx), a.ld_dx, p[i], a.cols, g[i]);
         }
     }
-    if (!a.part) return;
+    if (MODE == NORM_FEW || !a.part) return;
     constexpr int SPAN = LANES * WAVES * PIECES * N;
     if constexpr (WAVES == 1) {         // the sums of a wavefront's rows, and then the four wavefronts' in their order
         __shared__ float joined[2 * SPAN];
@@ -437,9 +513,9 @@ static int norm_blocks(int64_t rows, const NormShape& v, int most) {
 }
 static int forward_blocks(const NormShape& v, bool add) { return add || v.waves >= 8 ? 512 : 1024; }
 static int backward_blocks(const NormShape& v) { return v.waves == 1 && v.pieces < 4 ? 512 : 256; }
-// Few rows: the sums of columns are made beside the rows, in one launch, from another reading of them.  (1000 x 515 in fp32 5.7 us, with sums of workgroups and a
-// second launch 9.0; 1024 x 4096 in bf16 13.9, 14.6; 1024 x 8192 28.0, 19.5; and what the host takes for a launch, 3 us of 12.5.)
-constexpr int64_t kNormFewRows = 1024, kNormFewBytes = 9 << 20;
+// Few rows: the sums of columns are made beside the rows, in one launch, from another reading of them.  (Calls of 1000 x 515 in fp32 9.8 us, with sums of workgroups and a
+// second launch 12.3; 200 x 1000 in bf16 9.6, 12.6; of 1024 x 4096, 8 MB, 14.9 and 15.1, where nothing is gained that rows far from zero would not cost.)
+constexpr int64_t kNormFewBytes = 9 << 18;
 // From this many bytes in a call on activations have the non-temporal hint (as those of act.hip).
 constexpr int64_t kNormStream = 96 << 20;
 
@@ -486,11 +562,11 @@ static hipError_t launch_norm_as(const NormDev& a, const NormShape& v, hipStream
         return hipGetLastError();
     });
 }
-template <class T, bool PAST, bool STREAM>
+template <class T, bool PAST, NormMode MODE>
 static hipError_t launch_backward_as(const NormGradDev& a, const NormShape& v, hipStream_t st) {
     const int per = 4 * kPiece<T>, blocks = a.row_blocks + (a.dw || a.db ? (a.cols + per - 1) / per : 0);
     return norm_dispatch<T, true>(v, [&](auto waves, auto pieces, auto lanes) {
-        hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, lanes.value, PAST, STREAM>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
+        hipLaunchKernelGGL((norm_backward_kernel<T, waves.value, pieces.value, lanes.value, PAST, MODE>), dim3(blocks), dim3(kNormThreads<waves.value>), 0, st, a);
         return hipGetLastError();
     });
 }
@@ -573,7 +649,8 @@ int psgd_norm_backward(void* workspace, void* stream, int64_t rows, int64_t cols
     forget_errors();
     if (rows != 0) {
         hipError_t e;
-#define PSGD_NORM(T, PAST) (stream_it ? launch_backward_as<T, PAST, true>(a, v, st) : launch_backward_as<T, PAST, false>(a, v, st))
+#define PSGD_NORM(T, PAST) \
+    (few ? launch_backward_as<T, PAST, NORM_FEW>(a, v, st) : stream_it ? launch_backward_as<T, PAST, NORM_STREAM>(a, v, st) : launch_backward_as<T, PAST, NORM_MANY>(a, v, st))
         if (dtype == PSGD_F32) e = dtotal ? PSGD_NORM(float, true) : PSGD_NORM(float, false);
         else e = dtotal ? PSGD_NORM(bf16_t, true) : PSGD_NORM(bf16_t, false);
 #undef PSGD_NORM
