@@ -120,3 +120,21 @@ def test_rows_without_variance_far_from_zero(rows, cols, dtype):
     want = 1e6 * (g - g.mean(1, keepdim=True))
     assert ((dx.double() - want).abs() <= 1e6 * STEPS * (g.abs() + g.abs().mean(1, keepdim=True)) + UNIT[dtype] * 1.01 * want.abs()).all()
     assert (dw == 0).all() and ((db.double() - g.sum(0)).abs() <= (rows / 256 + 60) * 2.0 ** -24 * g.abs().sum(0)).all()
+
+
+# several rows to a workgroup, the next on its way while one is added up: of every number of wavefronts and pieces that a row takes
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(9000, 60), (9000, 100), (9000, 250), (6000, 500), (6000, 1000), (6000, 1500), (4000, 2040), (1500, 2500), (1500, 4096), (1500, 8000),
+                                       (1500, 10001), (1500, 12296), (1500, 16384)])
+def test_many_rows(rows, cols, dtype):
+    backward(rows, cols, dtype, past=True, accumulate=True)
+
+
+# just beyond the 96 MiB from which on loads and stores have the non-temporal hint
+@pytest.mark.parametrize("add,past", [(True, True), (False, False)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [60, 500, 1001, 3001, 6001, 9001, 12297, 16384])
+def test_large(cols, dtype, add, past):
+    size = 4 if dtype == "f32" else 2
+    rows = (96 << 20) // (cols * size * (4 if add else 2)) + 1001
+    backward(rows, cols, dtype, add=add, past=past)
