@@ -390,7 +390,8 @@ int psgd_norm(void *stream, int64_t rows, int64_t cols, int dtype, const void *x
               void *total /* nullable */, int64_t ld_total, void *y, int64_t ld_y, float *stats /* nullable */);
 /* With u = (x - mean) r and g = dy weight:  dx = r (g - mean_c g - u mean_c(g u)) + dtotal;  dweight = sum_rows dy u, dbias = sum_rows dy,
  * written or, with accumulate != 0, added to.  x: what was normalised (total, where there was one); stats: psgd_norm's; dtotal: the gradient that reaches
- * it past the norm, or NULL.  dx may take the place of dy, x or dtotal.  dweight, dbias: cols elements of g_dtype, each nullable;
+ * it past the norm, or NULL.  u is good to 2^-23 and its own roundings however far from zero a row lies: of rows with |mean| r > 2 what the kept mean's rounding leaves
+ * of it is taken out.  dx may take the place of dy, x or dtotal.  dweight, dbias: cols elements of g_dtype, each nullable;
  * without either the workspace may be NULL. */
 size_t psgd_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int dtype);
 int psgd_norm_backward(void *workspace, void *stream, int64_t rows, int64_t cols, int dtype, const void *dy, int64_t ld_dy,

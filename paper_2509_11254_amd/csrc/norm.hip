@@ -493,7 +493,9 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* part, int64
 // Wavefronts to a row and pieces to a lane.  One wavefront needs no barrier, and has a row of up to four pieces to a lane; wider rows have four wavefronts
 // or eight with as few pieces as do (16384 x 4096 with addend, in us, of (4, 2), (8, 1), (2, 4), each with its best grid: forward 90.0, 90.7, 92.9, backward 95.8, 90.8,
 // 98.9; 8192 x 8192 of (4, 4), (8, 2), (16, 1): 93.8, 91.2, 106.4, 96.2, 93.3, 93.2; 8192 x 11008 without one of (8, 3), (16, 2): 65.9, 95.4, 99.0, 167;
-// 16384 x 2048 of (1, 4), (2, 2), (4, 1): 46.2, 46.6, 47.2, 54.0, 54.7, 52.2).  Rows of up to 512 bytes lie beside each other in a wavefront (60000 rows in bf16, forward and
+// 16384 x 2048 of (1, 4), (2, 2), (4, 1): 46.2, 46.6, 47.2, 54.0, 54.7, 52.2, the last with a grid of its own, and 67.1 with the others').  Beyond 12288 columns
+// in bf16 and 8192 in fp32 the backward pass keeps part of a row in scratch: 8192 x 16384 in bf16 322 us, 3.3 TB/s, 8192 x 11008 and 4096 x 16384 in fp32 404 and 525, 3.6 and 2.0, with
+// what comes past the norm.  Rows of up to 512 bytes lie beside each other in a wavefront (60000 rows in bf16, forward and
 // backward, in us, with a wavefront each and so: of 64 columns 21.7 and 32.8, 7.9 and 12.9; of 256 22.9 and 33.8, 13.0 and 23.7).
 struct NormShape { int waves, pieces, lanes = 64; };
 static NormShape norm_variant(int64_t cols, int dtype, bool backward) {
